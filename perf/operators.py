@@ -1,0 +1,569 @@
+"""The operators on shared caches whose speed counts: page bookkeeping of forked block tables and attention over a
+prefix that several sequences of a batch share.
+
+    attn     murmur_shared_plan (for block pools it finds what the lists share), then murmur_decode_attn_shared
+    fork     murmur_paged_fork: rows of a block table become copies of their parents' rows, blocks nobody names go free
+    step     murmur_paged_step_shared: one decode step's freeing, taking, copying on write and appending
+    compact  murmur_paged_compact: the blocks in use move to the front of the pool
+
+A batch is `groups` groups of sequences.  The sequences of a group are hypotheses of one audio chunk: they share its
+prompt, its speech and their outputs up to where each of them left the first one (at most `back` tokens ago); with
+`draft` they are consecutive tokens of one sequence that a draft proposed.  With the `ranges` form every sequence has
+a cache of its own and a group has its prompt in common.  Lengths, tables and what is shared come from the case
+alone; keys, values, queries and the order of the pool's blocks from the seed.  Rows that no list of an attention
+case names are bf16 NaN, so a stray read shows in the outputs.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+D = 128
+OFF = -1
+
+DEFAULTS = dict(op="attn", form="paged", layers=1, per_call=1, groups=12, width_lo=8, width_hi=8, prompt=32,
+                prompt_mid=0, speech_lo=2250, speech_hi=2250, out_lo=600, out_hi=1200, w_s=OFF, delay=0, sink_s=0,
+                w_o=OFF, sink_o=0, back=48, draft=False, block=16, hq=28, hkv=4, out_f32=False, spare=64)
+
+
+def _case(**kw):
+    return dict(DEFAULTS, **kw)
+
+
+def listed():
+    evict = dict(w_s=562, delay=512, w_o=256)
+    minute = dict(speech_lo=450, speech_hi=450, out_lo=72, out_hi=72, w_s=128, delay=72, w_o=32)
+    return [
+        # The smallest call: four hypotheses of one minute, one layer.  Launches and round trips.
+        _case(name="minute_beams4", groups=1, width_lo=4, width_hi=4, back=12, out_f32=True, **minute),
+        # The headline batch with eight hypotheses a chunk, one attention call per layer of the decoder.
+        _case(name="chunks12_beams8", layers=28, **evict),
+        # An hour in one pass without eviction, five hypotheses: one long prefix.
+        _case(name="hour_beams5", layers=28, groups=1, width_lo=5, width_hi=5, speech_lo=27000, speech_hi=27000,
+              out_lo=8064, out_hi=8064, back=200, out_f32=True),
+        # 64 short chunks behind one long prompt (a glossary, earlier text), caches of their own, range tables.
+        _case(name="prompt4096_x64", form="ranges", layers=4, groups=1, width_lo=64, width_hi=64, prompt=4096,
+              speech_lo=300, speech_hi=450, out_lo=1, out_hi=90),
+        # Checking six drafted tokens of each of 16 chunks, all layers in one call: hardly anything but the prefix.
+        _case(name="drafts16_stack", layers=28, per_call=28, groups=16, width_lo=6, width_hi=6, draft=True,
+              speech_lo=1800, speech_hi=2250, out_lo=200, out_hi=1200),
+        # Groups of one to sixteen, odd lengths, sixteen query heads on one KV head: a batch at all stages.
+        _case(name="ragged_groups", layers=2, groups=23, width_lo=1, width_hi=16, prompt=17, prompt_mid=5,
+              speech_lo=211, speech_hi=2250, out_lo=1, out_hi=1500, back=300, block=8, hq=16, hkv=1),
+        # Reordering the hypotheses of the headline batch after a token.
+        _case(name="fork_12x8", op="fork", **evict),
+        # The same for 64 chunks of sixteen hypotheses at every stage of their decode.
+        _case(name="fork_64x16", op="fork", groups=64, width_lo=16, width_hi=16, out_lo=1, out_hi=2700, back=400),
+        # A token of one minute's four hypotheses in one layer: the bookkeeping alone.
+        _case(name="step_minute", op="step", groups=1, width_lo=4, width_hi=4, back=12, **minute),
+        # A token of the headline batch right after a fork, all layers: copies of half filled blocks.
+        _case(name="step_12x8", op="step", layers=28, **evict),
+        # A small pool after many releases.
+        _case(name="compact_minute", op="compact", groups=1, width_lo=4, width_hi=4, layers=2, spare=40, **minute),
+        # The headline batch's pool with half as many free blocks as used ones scattered in it.
+        _case(name="compact_12x8", op="compact", layers=28, spare=900, **evict),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _size(c):
+    """(bytes of the path, rows that the plain form gathers)."""
+    lay = _layout(c)
+    return work(c)["bytes"], c["layers"] * int(sum(len(p) for p in lay["kept"])) if c["op"] == "attn" else 0
+
+
+def draw(rng):
+    """One more case: any of the operators, 1 to 64 groups of 1 to 64 sequences, a minute to an hour, 1 to 28 layers,
+    blocks of 1 to 64 rows, any policy."""
+    sizes = [_size(c) for c in listed()]
+    most = max(s[0] for s in sizes), max(s[1] for s in sizes)
+    while True:
+        op = rng.choice(["attn", "attn", "attn", "attn", "fork", "step", "step", "compact"])
+        hq, hkv = rng.choice([(28, 4), (28, 4), (28, 4), (16, 4), (16, 1), (8, 2), (4, 4)])
+        layers = _log_int(rng, 1, 28)
+        width_hi = _log_int(rng, 1, 64)
+        speech_hi = _log_int(rng, 100, 27000)
+        out_hi = _log_int(rng, 2, 8000)
+        c = _case(op=op, hq=hq, hkv=hkv, layers=layers, per_call=rng.choice([1, 1, layers]),
+                  groups=_log_int(rng, 1, 64), width_hi=width_hi, width_lo=rng.choice([width_hi, rng.randint(1, width_hi)]),
+                  prompt=rng.choice([rng.randint(1, 64), _log_int(rng, 1, 5000)]),
+                  prompt_mid=rng.choice([0, 0, rng.randint(1, 40)]),
+                  speech_hi=speech_hi, speech_lo=rng.choice([speech_hi, rng.randint(speech_hi // 3, speech_hi)]),
+                  out_hi=out_hi, out_lo=rng.choice([out_hi, rng.randint(1, out_hi)]), back=_log_int(rng, 1, 600),
+                  block=rng.choice([1, 4, 8, 16, 16, 16, 32, 64]), out_f32=rng.random() < 0.5,
+                  draft=op == "attn" and rng.random() < 0.2, spare=_log_int(rng, 40, 1500))
+        if op == "attn" and rng.random() < 0.25:
+            c.update(form="ranges", draft=False)
+        if rng.random() < 0.5:  # speech eviction
+            c.update(w_s=_log_int(rng, 32, max(33, speech_hi)), delay=rng.choice([0, 256, 512]),
+                     sink_s=rng.choice([0, 0, rng.randint(1, 64)]))
+        if rng.random() < 0.5:  # output eviction
+            c.update(w_o=_log_int(rng, 16, max(17, out_hi)), sink_o=rng.choice([0, 4, 8]))
+        lay = _layout(c)
+        if c["form"] == "ranges":
+            cache = len(lay["seg"]) * int(lay["seg"].sum(axis=1).max())
+        else:
+            cache = lay["n_blocks"] * c["block"]
+        if c["op"] == "fork":
+            cache = lay["table"].size // 64
+        if cache * layers * hkv * D * 4 > 12e9:
+            continue
+        size = _size(c)
+        if all(a <= b for a, b in zip(size, most)):
+            return c
+
+
+# ---- lengths, policies, tables and what is shared (plain numpy, from the case alone) --------------------------------
+
+def _window(seg, c):
+    """First speech token of the window and first output token of the window at step out_len, per sequence."""
+    ls, j = seg[:, 1].astype(np.int64), seg[:, 3].astype(np.int64)
+    lo = np.clip(j - max(c["delay"], 1) + 1, 0, np.maximum(ls - c["w_s"], 0)) if c["w_s"] != OFF else np.zeros_like(ls)
+    out = np.maximum(j - c["w_o"], 0) if c["w_o"] != OFF else np.zeros_like(j)
+    return lo, out
+
+
+def _kept(seg, c):
+    """Retained positions of every sequence, ascending."""
+    lo, out = _window(seg, c)
+    got = []
+    for b in range(len(seg)):
+        p0, ls, p1, j = (int(x) for x in seg[b])
+        t, o = np.arange(ls), np.arange(j)
+        speech = np.ones(ls, bool) if c["w_s"] == OFF else (t < c["sink_s"]) | ((t >= lo[b]) & (t < lo[b] + c["w_s"]))
+        outs = np.ones(j, bool) if c["w_o"] == OFF else (o < c["sink_o"]) | (o >= out[b])
+        got.append(np.flatnonzero(np.concatenate([np.ones(p0, bool), speech, np.ones(p1, bool), outs])))
+    return got
+
+
+def _freed(seg, c):
+    """The positions that no step from out_len on retains: [B, 2, 2] (first, end) in speech and outputs."""
+    lo, out = _window(seg, c)
+    first = seg[:, 0] + np.minimum(c["sink_s"], seg[:, 1])
+    speech = np.stack([first, np.maximum(first, seg[:, 0] + lo)], 1)
+    out0 = seg[:, :3].sum(axis=1)
+    outs = np.stack([out0 + c["sink_o"], np.maximum(out0 + c["sink_o"], out0 + out)], 1)
+    return np.stack([speech, outs], 1)
+
+
+def _layout(c):
+    rng = np.random.default_rng([c["groups"], c["width_hi"], c["speech_hi"], c["out_hi"], c["back"], c["block"]])
+    n = c["groups"]
+    width = rng.integers(c["width_lo"], c["width_hi"], size=n, endpoint=True)
+    speech = rng.integers(c["speech_lo"], c["speech_hi"], size=n, endpoint=True)
+    out = rng.integers(c["out_lo"], c["out_hi"], size=n, endpoint=True)
+    group = np.concatenate([[0], np.cumsum(width)]).astype(np.int32)
+    B, bs = int(group[-1]), c["block"]
+    of = np.repeat(np.arange(n), width)
+    rank = np.arange(B) - group[of]
+    seg = np.stack([np.full(n, c["prompt"]), speech, np.full(n, c["prompt_mid"]), out], axis=1).astype(np.int32)[of]
+    if c["form"] == "ranges":  # chunks of their own behind the group's prompt
+        seg[:, 1] = rng.integers(c["speech_lo"], c["speech_hi"], size=B, endpoint=True)
+        seg[:, 3] = rng.integers(c["out_lo"], c["out_hi"], size=B, endpoint=True)
+    if c["draft"]:
+        seg[:, 3] += rank.astype(np.int32)
+    lay = {"seg": seg, "group": group, "of": of, "kept": _kept(seg, c)}
+    if c["form"] == "ranges":
+        return lay
+    # where each sequence left the first one of its group: it has blocks of its own from there on
+    total = seg.sum(axis=1).astype(np.int64)
+    back = np.where((rank == 0) | c["draft"], 0, rng.integers(1, c["back"], size=B, endpoint=True))
+    if c["op"] == "step":  # forked at the token before this one: it shares every block so far
+        back = np.where(rng.random(B) < 0.5, 0, back)
+    held = -(-total // bs) if c["op"] != "step" else -(-(total - 1) // bs)
+    left = np.where(back > 0, np.maximum(seg[:, :3].sum(axis=1), total - back) // bs, held)
+    if c["draft"]:
+        left[rank == 0], held = 0, np.maximum.reduceat(held, group[:-1])[of]  # the first row holds the drafted rows too
+        left[rank > 0] = held[rank > 0]
+    left[rank == 0] = 0
+    own_blocks = held - np.minimum(left, held)
+    width_t = int((-(-total // bs)).max()) if not c["draft"] else int(held.max())
+    col = np.arange(width_t)
+    first = np.concatenate([[0], np.cumsum(own_blocks)])
+    mine = (col >= left[:, None]) & (col < held[:, None])
+    table = np.where(mine, first[:-1, None] + col - left[:, None], -1)
+    lead = table[group[:-1]][of]
+    table = np.where((col < np.minimum(left, held)[:, None]), lead, table)
+    if c["op"] != "attn":  # what left the windows is free already (for a step: before it)
+        at = seg.copy()
+        if c["op"] == "step":
+            at[:, 3] -= 1
+        fr = _freed(at, c)
+        lo, hi = -(-fr[:, :, 0] // bs), fr[:, :, 1] // bs
+        gone = ((col >= lo[:, :, None]) & (col < hi[:, :, None])).any(axis=1)
+        table = np.where(gone, -1, table)
+    used = np.unique(table[table >= 0])
+    table = np.where(table >= 0, np.searchsorted(used, table), -1).astype(np.int32)
+    lay.update(table=table, n_used=len(used), n_blocks=len(used) + c["spare"] + B)
+    return lay
+
+
+def _parents(c, lay):
+    """For every sequence the one that it continues (of its group), or -1: ended."""
+    rng = np.random.default_rng([7, c["groups"], c["width_hi"], c["out_hi"]])
+    g, of = lay["group"], lay["of"]
+    w = g[1:] - g[:-1]
+    pick = g[of] + np.minimum((rng.random(len(of)) ** 2 * w[of]).astype(np.int64), w[of] - 1)
+    pick = np.where(rng.random(len(of)) < 0.4, np.arange(len(of)), pick)
+    return np.where(rng.random(len(of)) < 0.04, -1, pick).astype(np.int32)
+
+
+def _copied_rows(c, lay):
+    """Rows that a step copies: sequences whose token goes into a block that others hold too."""
+    total, bs, t = lay["seg"].sum(axis=1) - 1, c["block"], lay["table"]
+    cur = t[np.arange(len(t)), total // bs]
+    ref = np.bincount(t[t >= 0].ravel(), minlength=lay["n_blocks"])
+    rows, seen = 0, {}
+    for b in np.flatnonzero(cur >= 0):
+        x = int(cur[b])
+        seen[x] = seen.get(x, 0) + 1
+        rows += int(total[b] % bs) if ref[x] > 1 and seen[x] < ref[x] else 0
+    return rows
+
+
+def work(c):
+    lay = _layout(c)
+    B, row = len(lay["seg"]), c["layers"] * c["hkv"] * 2 * D * 2  # a position's K and V in all layers
+    if c["op"] == "attn":
+        counts = np.array([len(p) for p in lay["kept"]])
+        named = int(counts.sum()) - sum(int(s) * (int(w) - 1) for s, w in zip(_shared(c, lay), lay["group"][1:] - lay["group"][:-1]))
+        io = c["layers"] * B * c["hq"] * ((4 if c["out_f32"] else 2) * D + 2 * D + 4)
+        lists = B * 48 if c["form"] == "ranges" else int(counts.sum()) * 4
+        return {"bytes": named * row + io + lists + B * 8, "flops": int(counts.sum()) * c["layers"] * c["hq"] * D * 4}
+    book = 8 * lay["table"].size + 8 * lay["n_blocks"]  # tables and counts, read and written
+    if c["op"] == "fork":
+        return {"bytes": book + 4 * B, "flops": 0}
+    if c["op"] == "step":
+        return {"bytes": 2 * row * (_copied_rows(c, lay) + B) + 36 * B + 8 * B, "flops": 0}
+    moved = int(np.sum(_order(c, lay, 0)[:lay["n_used"]] >= lay["n_used"]))
+    return {"bytes": 2 * row * moved * c["block"] + book + 4 * lay["n_blocks"], "flops": 0}
+
+
+def _shared(c, lay):
+    """Leading entries that the lists of each group have in common."""
+    if c["form"] == "ranges":
+        return np.array([c["prompt"]] * c["groups"])
+    got = []
+    for lo, hi in zip(lay["group"][:-1], lay["group"][1:]):
+        rows = [lay["table"][b][lay["kept"][b] // c["block"]].astype(np.int64) * c["block"] + lay["kept"][b] % c["block"]
+                for b in range(lo, hi)]
+        n = min(len(r) for r in rows)
+        same = np.all([r[:n] == rows[0][:n] for r in rows], axis=0)
+        got.append(int(n if same.all() else np.argmin(same)))
+    return np.array(got)
+
+
+def _order(c, lay, seed):
+    """The physical block of every block number of the layout: a random placement in the pool."""
+    return np.random.default_rng([seed, 11]).permutation(lay["n_blocks"])
+
+
+# ---- inputs ---------------------------------------------------------------------------------------------------------
+
+def _gen(seed, *extra):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(int(np.random.SeedSequence([seed, *extra]).generate_state(1, np.uint64)[0] >> 1))
+    return g
+
+
+def _i32(x):
+    return torch.from_numpy(np.ascontiguousarray(x, dtype=np.int32)).cuda()
+
+
+def _randn(seed, which, *shape):
+    return torch.randn(shape, generator=_gen(seed, which), device="cuda", dtype=torch.bfloat16)
+
+
+def prepare(c, seed):
+    lay = _layout(c)
+    B, nl, hq, hkv, bs = len(lay["seg"]), c["layers"], c["hq"], c["hkv"], c["block"]
+    s = {"case": c, "B": B, "seg": _i32(lay["seg"]), "group": _i32(lay["group"]), "of": torch.from_numpy(lay["of"]).cuda()}
+    s["pol"] = _i32([[c["w_s"], c["delay"], c["sink_s"], c["w_o"], c["sink_o"]]])
+    if c["form"] == "paged":
+        order = _order(c, lay, seed)
+        table = np.where(lay["table"] >= 0, order[lay["table"]], -1).astype(np.int32)
+        n_blocks, used = lay["n_blocks"], lay["n_used"]
+        ref = np.bincount(table[table >= 0].ravel(), minlength=n_blocks)
+        # table, counts, free stack and its top in one buffer, so that a pass starts from all of them at once
+        book = np.zeros(table.size + 2 * n_blocks + 1, dtype=np.int32)
+        book[:table.size], book[table.size:table.size + n_blocks] = table.ravel(), ref
+        book[table.size + n_blocks:][:n_blocks - used], book[-1] = order[used:], n_blocks - used
+        s.update(book0=_i32(book), book=_i32(book), shape=table.shape, n_blocks=n_blocks)
+    if c["op"] == "fork":
+        s["parent"] = _i32(_parents(c, lay))
+        return s
+    if c["op"] in ("step", "compact"):
+        s["k"], s["v"] = (_randn(seed, w, nl, n_blocks * bs, hkv, D) for w in (1, 2))
+        s["k_new"], s["v_new"] = (_randn(seed, w, nl, B, hkv, D) for w in (3, 4))
+        s["copied"], s["map"] = _i32(np.full(B, -1)), _i32(np.full(n_blocks, -1))
+        return s
+
+    keep = max(len(p) for p in lay["kept"])
+    s.update(keep=keep, count=_i32([len(p) for p in lay["kept"]]), q=_randn(seed, 5, nl, B, hq, D), scale=D ** -0.5)
+    s["out"] = torch.zeros((nl, B, hq, D), dtype=torch.float32 if c["out_f32"] else torch.bfloat16, device="cuda")
+    s["lse"] = torch.zeros((nl, B, hq), dtype=torch.float32, device="cuda")
+    if c["form"] == "ranges":
+        seg = lay["seg"].astype(np.int64)
+        lo, out = _window(lay["seg"], c)
+        out0 = seg[:, :3].sum(axis=1)
+        pieces = []  # (first, length) of the prompt, the speech, the second prompt and the outputs that are kept
+        for b in range(B):
+            p0, ls, p1, j = (int(x) for x in seg[b])
+            sink, w = (min(c["sink_s"], ls), c["w_s"]) if OFF != c["w_s"] < ls else (ls, 0)
+            l0 = max(int(lo[b]), sink)
+            so, o0 = (min(c["sink_o"], j), max(int(out[b]), min(c["sink_o"], j))) if OFF != c["w_o"] < j else (j, j)
+            pieces.append([(0, p0), (p0, sink), (p0 + l0, max(int(lo[b]) + w - l0, 0)), (p0 + ls, p1),
+                           (int(out0[b]), so), (int(out0[b]) + o0, j - o0)])
+        s["ranges"], s["shared"] = _i32(pieces), _i32([c["prompt"]] * c["groups"])
+        s["idx"] = None
+        length = int(-(-seg.sum(axis=1).max() // 8) * 8)
+        shape = (nl, B, hkv, length, D)
+        live = torch.zeros((B, length), dtype=torch.bool, device="cuda")
+        live[torch.from_numpy(np.repeat(np.arange(B), [len(p) for p in lay["kept"]])).cuda(),
+             torch.from_numpy(np.concatenate(lay["kept"])).cuda()] = True
+        dead = ~live.view(1, B, 1, length, 1)
+    else:
+        rows = [table[b][p // bs].astype(np.int64) * bs + p % bs for b, p in enumerate(lay["kept"])]
+        idx = np.full((B, keep), -1, dtype=np.int32)
+        for b in range(B):
+            idx[b, :len(rows[b])] = rows[b]
+        s["idx"], s["ranges"] = _i32(idx), None
+        s["shared"] = _i32(np.zeros(c["groups"]))
+        shape = (nl, n_blocks * bs, hkv, D)
+        live = torch.zeros(n_blocks * bs, dtype=torch.bool, device="cuda")
+        live[torch.from_numpy(np.concatenate(rows)).cuda()] = True
+        dead = ~live.view(1, -1, 1, 1)
+    for name, which in (("k", 1), ("v", 2)):
+        x = _randn(seed, which, *shape)
+        if c["form"] == "ranges":  # the group's prompt, in every sequence's cache
+            x[:, :, :, :c["prompt"]] = x[:, torch.from_numpy(lay["group"][:-1][lay["of"]].astype(np.int64)).cuda(), :, :c["prompt"]]
+        s[name] = x.masked_fill_(dead, float("nan"))
+    return s
+
+
+def _book(s, book):
+    """The parts of a bookkeeping buffer: table, counts, free stack, its top."""
+    n, size = s["n_blocks"], s["shape"][0] * s["shape"][1]
+    return book[:size].view(s["shape"]), book[size:size + n], book[size + n:size + 2 * n], book[size + 2 * n:]
+
+
+# ---- the operators in plain form ------------------------------------------------------------------------------------
+
+def _first(flat, mask, n):
+    """Whether each masked entry is the first one of its value (values below n)."""
+    at = torch.arange(flat.numel(), device=flat.device)
+    value = torch.where(mask, flat, n).long()
+    first = torch.full((n + 1,), flat.numel(), device=flat.device).scatter_reduce(0, value, at, "amin")
+    return mask & (first[value] == at)
+
+
+def _push(stack, top, values, mask):
+    """The stack with the masked values on top in their order, and its new top."""
+    at = torch.where(mask, top.long() + mask.cumsum(0) - 1, stack.numel())
+    longer = torch.cat([stack, stack.new_zeros(1)]).scatter(0, at, values)
+    return longer[:-1], (top + mask.sum()).int()
+
+
+def _plain_fork(s):
+    table, ref, stack, top = _book(s, s["book0"])
+    n, parent = s["n_blocks"], s["parent"].long()
+    new = torch.where(parent[:, None] >= 0, table[parent.clamp(min=0)], -1)
+    change = torch.zeros(n + 1, dtype=torch.int32, device=ref.device)
+    one = torch.ones_like(new.flatten())
+    change.scatter_add_(0, torch.where(new >= 0, new, n).flatten().long(), one)
+    change.scatter_add_(0, torch.where(table >= 0, table, n).flatten().long(), -one)
+    after = ref + change[:n]
+    old = table.flatten()
+    dead = (old >= 0) & (after[old.clamp(min=0).long()] == 0)
+    stack, top = _push(stack, top, old, _first(old, dead, n))
+    return [new, after, stack, top]
+
+
+def _plain_step(s):
+    c = s["case"]
+    table, ref, stack, top = _book(s, s["book0"])
+    n, bs, B = s["n_blocks"], c["block"], s["B"]
+    seg = s["seg"].long()
+    col = torch.arange(table.shape[1], device=table.device)
+    # what no step from this one on retains
+    first = seg[:, 0] + seg[:, 1].clamp(max=c["sink_s"])
+    room = (seg[:, 1] - c["w_s"]).clamp(min=0)
+    window = torch.minimum((seg[:, 3] - max(c["delay"], 1) + 1).clamp(min=0), room) if c["w_s"] != OFF else 0 * room
+    outs = seg[:, :3].sum(1)
+    behind = (seg[:, 3] - c["w_o"]).clamp(min=0) if c["w_o"] != OFF else 0 * room
+    lo = torch.stack([first, outs + c["sink_o"]], 1)
+    hi = torch.stack([seg[:, 0] + window, outs + behind], 1)
+    gone = ((col >= ((lo + bs - 1) // bs)[:, :, None]) & (col < (hi // bs)[:, :, None])).any(1) & (table >= 0)
+    less = torch.zeros(n + 1, dtype=torch.int32, device=ref.device)
+    flat = table.flatten()
+    less.scatter_add_(0, torch.where(gone.flatten(), flat, n).long(), torch.ones_like(flat))
+    ref = ref - less[:n]
+    dead = gone.flatten() & (ref[flat.clamp(min=0).long()] == 0)
+    stack, top = _push(stack, top, flat, _first(flat, dead, n))
+    table = torch.where(gone, -1, table)
+    # the current token's block: a new one, or a copy of one that others keep
+    pos = seg.sum(1) - 1
+    blk, slot = pos // bs, pos % bs
+    cur = table.gather(1, blk[:, None])[:, 0]
+    row = torch.arange(B, device=table.device)
+    before = (pos[None] < pos[:, None]) | ((pos[None] == pos[:, None]) & (row[None] < row[:, None]))
+    ahead = (before & (cur[None] == cur[:, None])).sum(1)
+    copy = (cur >= 0) & (ahead < ref[cur.clamp(min=0).long()] - 1)
+    take = copy | (cur < 0)
+    got = torch.where(take, stack[(top.long() - take.cumsum(0)).clamp(min=0)], cur)
+    top = (top - take.sum()).int()
+    table = table.scatter(1, blk[:, None], got[:, None])
+    change = torch.zeros(n + 1, dtype=torch.int32, device=ref.device)
+    change.scatter_add_(0, torch.where(take, got, n).long(), torch.ones_like(got))
+    change.scatter_add_(0, torch.where(copy, cur, n).long(), -torch.ones_like(got))
+    ref = ref + change[:n]
+    # rows before the token into the copies, then the token itself
+    at = torch.arange(bs, device=table.device)
+    here = got.long() * bs + slot
+    wanted = copy[:, None] & (at < slot[:, None])
+    src = torch.where(wanted, cur.long()[:, None] * bs + at, here[:, None]).flatten()
+    dst = torch.where(wanted, got.long()[:, None] * bs + at, here[:, None]).flatten()
+    k, v = s["k"], s["v"]
+    k[:, dst], v[:, dst] = k[:, src], v[:, src]
+    k[:, here], v[:, here] = s["k_new"], s["v_new"]
+    return [table, ref, stack, top, torch.where(copy, cur, -1), k, v]
+
+
+def _plain_compact(s):
+    c = s["case"]
+    table, ref, stack, top = _book(s, s["book0"])
+    n, nl = s["n_blocks"], c["layers"]
+    at = torch.arange(n, device=ref.device)
+    live = ref > 0
+    used = live.sum()
+    moves, into = live & (at >= used), ~live & (at < used)
+    order = torch.full((n + 1,), n, device=ref.device).scatter(0, torch.where(into, into.cumsum(0) - 1, n), at)
+    new = torch.where(live, torch.where(moves, order[(moves.cumsum(0) - 1).clamp(min=0)], at), -1).int()
+    table = torch.where(table >= 0, new[table.clamp(min=0).long()], -1)
+    ref = torch.zeros(n + 1, dtype=torch.int32, device=ref.device).scatter(0, torch.where(live, new, n).long(), ref)[:n]
+    stack = torch.where(at < n - used, n - 1 - at, stack).int()
+    src = torch.nonzero(moves)[:, 0]
+    dst = new[src].long()
+    k, v = (s[x].view(nl, n, -1) for x in ("k", "v"))
+    k[:, dst], v[:, dst] = k[:, src], v[:, src]
+    return [table, ref, stack, (n - used).int().view(1), new, s["k"], s["v"]]
+
+
+def _plain_attn(s):
+    c = s["case"]
+    B, keep, hkv, nl = s["B"], s["keep"], c["hkv"], c["layers"]
+    rank = torch.arange(keep, device=s["q"].device)
+    live = rank < s["count"][:, None]
+    if c["form"] == "ranges":
+        start, length = s["ranges"].long().unbind(2)
+        lo = length.cumsum(1) - length
+        inside = (rank >= lo[:, :, None]) & (rank < (lo + length)[:, :, None])
+        pos = torch.where(inside, start[:, :, None] - lo[:, :, None] + rank, 0).sum(1)
+        at = torch.arange(B, device=pos.device)[:, None]
+        k, v = (s[x][:, at, :, pos].permute(2, 0, 3, 1, 4) for x in ("k", "v"))  # [layers, B, heads, keep, D]
+        shared = s["shared"]
+    else:
+        idx = s["idx"]
+        k, v = (s[x][:, idx.clamp(min=0).long()].permute(0, 1, 3, 2, 4) for x in ("k", "v"))
+        lead = s["group"][:-1].long()[s["of"]]
+        same = ((idx == idx[lead]) & live & live[lead]).int().cumprod(1).sum(1)
+        shared = torch.full((c["groups"],), keep, device=idx.device).scatter_reduce(0, s["of"], same, "amin").int()
+    dead = ~live.view(1, B, 1, keep, 1)
+    k, v = (x.float().masked_fill_(dead, 0.0) for x in (k, v))
+    q = s["q"].float().view(nl, B, hkv, -1, D)
+    logits = torch.matmul(q, k.transpose(3, 4)) * s["scale"]
+    logits = logits.masked_fill_(dead.transpose(3, 4), -math.inf)
+    m = logits.amax(-1, keepdim=True)
+    p = torch.exp(logits - m)
+    total = p.sum(-1, keepdim=True)
+    out = torch.matmul(p, v) / total
+    lse = m + torch.log(total)
+    return [out.view(nl, B, c["hq"], D).to(s["out"].dtype), lse.view(nl, B, c["hq"]), shared]
+
+
+# ---- the same through the framework ---------------------------------------------------------------------------------
+
+def _workspace(s, *sizes):
+    """The buffers a program keeps beside its caches, made with the first call."""
+    if "ws" not in s:
+        s["ws"] = [torch.zeros(-(-n // 4) + 64, dtype=torch.int32, device="cuda") for n in sizes]
+    return s["ws"]
+
+
+def _own_pages(s, M):
+    c, B = s["case"], s["B"]
+    s["book"].copy_(s["book0"])
+    table, ref, stack, top = _book(s, s["book"])
+    n, blocks, bs, hkv, nl = s["n_blocks"], s["shape"][1], c["block"], c["hkv"], c["layers"]
+    if c["op"] == "fork":
+        size = M.murmur_paged_workspace(B, blocks, n)
+        ws, = _workspace(s, size)
+        M.murmur_paged_fork(s["parent"], B, table, blocks, ref, n, stack, top, n, ws, size)
+        return [table, ref, stack, top]
+    pool = M.make_kv(s["k"], s["v"], nl, n * bs, (n * bs * hkv * D, 0, D, hkv * D))
+    if c["op"] == "step":
+        M.murmur_paged_step_shared(s["seg"], s["pol"], 0, B, table, blocks, bs, ref, n, stack, top, n, False,
+                                   s["copied"], pool, hkv, s["k_new"], s["v_new"])
+        return [table, ref, stack, top, s["copied"], s["k"], s["v"]]
+    size = M.murmur_paged_workspace(B, blocks, n)
+    ws, = _workspace(s, size)
+    M.murmur_paged_compact(B, table, blocks, bs, ref, n, stack, top, n, s["map"], pool, hkv, ws, size)
+    return [table, ref, stack, top, s["map"], s["k"], s["v"]]
+
+
+def _own_attn(s, M):
+    c, B, keep, per, hq, hkv = s["case"], s["B"], s["keep"], s["case"]["per_call"], s["case"]["hq"], s["case"]["hkv"]
+    if "sizes" not in s:
+        s["sizes"] = M.murmur_decode_attn_shared_workspace(per, B, hq, hkv, keep, c["groups"])
+    ws, plan = _workspace(s, *s["sizes"])
+    ws_bytes, plan_bytes = s["sizes"]
+    k, v, rows = s["k"], s["v"], s["k"].shape[1]
+    M.murmur_shared_plan(s["idx"], s["ranges"], s["count"], keep, B, s["group"], c["groups"], s["shared"],
+                         c["form"] == "paged", per, hq, hkv, plan, plan_bytes)
+    dtype = M.MURMUR_DTYPE_F32 if c["out_f32"] else M.MURMUR_DTYPE_BF16
+    for layer in range(0, c["layers"], per):
+        if c["form"] == "paged":
+            kv = M.make_kv(k[layer], v[layer], per, rows, (rows * hkv * D, 0, D, hkv * D))
+        else:
+            kv = M.kv_from_tensors(k[layer:layer + per], v[layer:layer + per])
+        M.murmur_decode_attn_shared(s["q"][layer], kv, s["idx"], s["ranges"], keep, B, hq, hkv, D, s["scale"],
+                                    s["out"][layer], dtype, s["lse"][layer], plan, plan_bytes, ws, ws_bytes)
+    return [s["out"], s["lse"], s["shared"]]
+
+
+def run(s):
+    op = s["case"]["op"]
+    if own:
+        from paper_2606_01483_amd import murmur as M
+        return _own_attn(s, M) if op == "attn" else _own_pages(s, M)
+    return {"attn": _plain_attn, "fork": _plain_fork, "step": _plain_step, "compact": _plain_compact}[op](s)
+
+
+# ---- the attention in 64 bits ---------------------------------------------------------------------------------------
+
+def exact(c, seed):
+    if c["op"] != "attn":
+        return None
+    s = prepare(c, seed)
+    lay, nl, hkv, g = _layout(c), c["layers"], c["hkv"], c["hq"] // c["hkv"]
+    out = torch.empty((nl, s["B"], c["hq"], D), dtype=torch.float64, device="cuda")
+    lse = torch.empty((nl, s["B"], c["hq"]), dtype=torch.float64, device="cuda")
+    for b in range(s["B"]):
+        if c["form"] == "ranges":
+            at = torch.from_numpy(lay["kept"][b]).cuda()
+            k, v = (s[x][:, b].index_select(2, at) for x in ("k", "v"))
+        else:
+            at = s["idx"][b, :len(lay["kept"][b])].long()
+            k, v = (s[x].index_select(1, at).transpose(1, 2).contiguous() for x in ("k", "v"))
+        for layer in range(nl):
+            for h in range(hkv):
+                heads = slice(h * g, (h + 1) * g)
+                logits = (s["q"][layer, b, heads].double() @ k[layer, h].double().t().contiguous()) * s["scale"]
+                lse[layer, b, heads] = torch.logsumexp(logits, dim=-1)
+                out[layer, b, heads] = torch.softmax(logits, dim=-1) @ v[layer, h].double()
+    return [out, lse, None]
