@@ -531,8 +531,8 @@ def _own_attn(s, M):
             kv = M.make_kv(k[layer], v[layer], per, rows, (rows * hkv * D, 0, D, hkv * D))
         else:
             kv = M.kv_from_tensors(k[layer:layer + per], v[layer:layer + per])
-        M.murmur_decode_attn_shared(s["q"][layer], kv, s["idx"], s["ranges"], keep, B, hq, hkv, D, s["scale"],
-                                    s["out"][layer], dtype, s["lse"][layer], plan, plan_bytes, ws, ws_bytes)
+        M.murmur_decode_attn_shared(s["q"][layer], kv, s["idx"], s["ranges"], keep, B, c["groups"], hq, hkv, D,
+                                    s["scale"], s["out"][layer], dtype, s["lse"][layer], plan, plan_bytes, ws, ws_bytes)
     return [s["out"], s["lse"], s["shared"]]
 
 
