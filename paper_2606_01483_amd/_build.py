@@ -1,7 +1,7 @@
 """Build libmurmur.so for gfx950 (MI355X) from csrc/.
 
-kernels.hip is compiled by hipcc for gfx950 only; api.cpp (host-only C ABI
-layer) by g++.  The shared object lands next to this file, where the ctypes
+kernels.hip is compiled by hipcc for gfx950 only; api.cpp and shared.cpp
+(host-only C ABI layer) by g++.  The shared object lands next to this file, where the ctypes
 binding loads it, and beside it the _pycall module, the argument converter of the
 per-step calls (pycall.cpp), where Python's headers are there to build it; the
 binding does without it.  Packed-fp32 instruction selection is disabled for
@@ -70,16 +70,18 @@ def build(verbose: bool = False) -> str:
     hipcc = _hipcc()
     k_obj = os.path.join(BUILD_DIR, "kernels.o")
     a_obj = os.path.join(BUILD_DIR, "api.o")
+    s_obj = os.path.join(BUILD_DIR, "shared.o")
     steps = [
         [hipcc, *KERNEL_FLAGS, "-c", os.path.join(CSRC, "kernels.hip"), "-o", k_obj],
         ["g++", *COMMON_FLAGS, "-Wextra", "-c", os.path.join(CSRC, "api.cpp"), "-o", a_obj],
+        ["g++", *COMMON_FLAGS, "-Wextra", "-c", os.path.join(CSRC, "shared.cpp"), "-o", s_obj],
     ]
     for cmd in steps:
         if verbose:
             print(" ".join(cmd), flush=True)
         _run(cmd)
     tmp = LIB + ".tmp"
-    link = [hipcc, f"--offload-arch={ARCH}", "-shared", "-fPIC", k_obj, a_obj, "-o", tmp]
+    link = [hipcc, f"--offload-arch={ARCH}", "-shared", "-fPIC", k_obj, a_obj, s_obj, "-o", tmp]
     if verbose:
         print(" ".join(link), flush=True)
     _run(link)

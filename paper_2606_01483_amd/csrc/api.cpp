@@ -12,15 +12,12 @@
 #include "murmur.h"
 #include "policy.h"
 
-#define MURMUR_EXPORT extern "C" __attribute__((visibility("default")))
-
 static_assert(sizeof(murmur_seg) == 4 * sizeof(int32_t), "the kernels read murmur_seg as four int32");
 static_assert(sizeof(murmur_policy) == 5 * sizeof(int32_t), "the kernels read murmur_policy as five int32");
 
 namespace murmur {
-namespace {
 
-thread_local char g_last_error[512];
+static thread_local char g_last_error[512];
 
 int fail(int code, const char *fmt, ...) {
     va_list ap;
@@ -34,12 +31,6 @@ int ok() {
     g_last_error[0] = '\0';
     return MURMUR_OK;
 }
-
-bool aligned(const void *p, size_t n) { return ((uintptr_t)p % n) == 0; }
-
-size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
-}  // namespace
 
 size_t ticket_region(size_t ws_bytes) { return round_up(4 * kTicketStride * ((ws_bytes + 1023) / 1024), 256); }
 

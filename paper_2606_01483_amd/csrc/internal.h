@@ -7,7 +7,16 @@
 
 #include "murmur.h"
 
+#define MURMUR_EXPORT extern "C" __attribute__((visibility("default")))
+
 namespace murmur {
+
+// Status and error text of an entry point (api.cpp): fail() formats the text of
+// murmur_last_error and returns `code`, ok() clears it.
+int fail(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
+int ok();
+inline bool aligned(const void *p, size_t n) { return ((uintptr_t)p % n) == 0; }
+inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 constexpr int kHeadDim = 128;     // head_dim supported by the attention kernel
 constexpr int kMaxGroup = 16;     // query heads per KV head (MFMA tile height)
@@ -170,6 +179,98 @@ int launch_paged_step(const murmur_seg *seg, const murmur_policy *pol, int32_t p
 int launch_paged_append(const murmur_seg *seg, int32_t B, const int32_t *bt, int32_t max_blocks, int32_t log2_bs,
                         const murmur_kv &pool, int32_t Hkv, const void *k_new, const void *v_new,
                         murmur_stream_t stream);
+
+// ---- shared pages and shared prefixes (shared.cpp; pages.hpp and shared_attn.hpp) ----
+
+// Workspace of murmur_paged_fork and murmur_paged_compact, int32 words.  The
+// header holds fork's ticket (zero between calls) and compact's number of moves.
+// After it, for fork, one count per row (rounded up to 64) and the changed entries
+// (ForkEntry) of every row; for compact the source and then the destination
+// blocks of at most n_blocks / 2 moves each.
+constexpr int kForkHeader = 64;
+struct ForkEntry {
+    int32_t col, fresh, old, unused;
+};
+int launch_paged_fork(const int32_t *parent, int32_t B, int32_t *bt, int32_t max_blocks, int32_t *ref,
+                      int32_t n_blocks, int32_t *stack, int32_t *top, int32_t *ws, murmur_stream_t stream);
+int launch_paged_step_shared(const murmur_seg *seg, const murmur_policy *pol, int32_t pol_per_seq, int32_t B,
+                             int32_t *bt, int32_t max_blocks, int32_t log2_bs, int32_t *ref, int32_t n_blocks,
+                             int32_t *stack, int32_t *top, int32_t full_scan, int32_t *copied,
+                             murmur_stream_t stream);
+int launch_paged_append_shared(const murmur_seg *seg, int32_t B, const int32_t *bt, int32_t max_blocks,
+                               int32_t log2_bs, const int32_t *copied, const murmur_kv &pool, int32_t Hkv,
+                               const void *k_new, const void *v_new, murmur_stream_t stream);
+int launch_paged_compact(int32_t B, int32_t *bt, int32_t max_blocks, int32_t log2_bs, int32_t *ref, int32_t n_blocks,
+                         int32_t *stack, int32_t *top, int32_t *map, const murmur_kv *pool, int32_t Hkv, int32_t *ws,
+                         murmur_stream_t stream);
+
+// The schedule of an attention over shared prefixes, written by
+// murmur_shared_plan into the caller's plan buffer (int32 words, in this order):
+//   PlanHeader;
+//   PlanSeq [B]: where a sequence's partials lie;
+//   PlanItem [n_wg]: prefix work, one workgroup each;
+//   PlanChunk [kSharedWaves * n_wg]: remainders, one wavefront each, the
+//     kSharedWaves of a workgroup side by side;
+//   first differing rank [B][n_scan] of each sequence's list against its group's
+//     first one, per kScanLen entries.
+// Workgroups 0 .. n_items-1 of a (layer, KV head) take the items and the next
+// n_rest the chunks.  n_wg bounds their number whatever the lists hold (see
+// shared_caps).
+constexpr int kSharedWaves = 8;
+constexpr int kSharedRows = 64;     // query rows of one prefix item: four MFMA row tiles
+constexpr int kSharedMaxPasses = 16;  // passes of kWaveTile positions per wavefront, at most
+constexpr int kScanLen = 4096;
+constexpr int32_t kPlanMagic = 0x6d75726d;
+struct PlanHeader {
+    int32_t magic, n_items, n_rest, bad;  // bad: the groups are not in order; every output is NaN
+    int32_t B, max_keep, n_layers, Hq, Hkv, n_groups;  // what the plan was made for
+    int32_t rows, passes, unused[4];  // partial rows per (layer, KV head); passes per wavefront
+};
+struct PlanSeq {
+    int32_t state;  // 0: not in any group (outputs untouched), 1: computed, 2: invalid count (NaN outputs)
+    int32_t pre_row, pre_stride, n_pre;  // partials over the prefix: rows pre_row + i * pre_stride + head
+    int32_t rest_row, n_rest;            // over the rest: rows rest_row + i * G + head
+    int32_t first_chunk, common;         // common: positions that the group shares
+};
+struct PlanItem {
+    int32_t seq0, n_seq, list, r0, r1, row, unused[2];  // list: the sequence whose list is read; row: partial row
+};
+struct PlanChunk {
+    int32_t seq, r0, r1, row;
+};
+struct SharedCaps {
+    int32_t per_round;  // workgroups per (layer, KV head) of one dispatch round
+    int32_t n_wg, n_scan;
+    int64_t rows;       // partial rows per (layer, KV head)
+    size_t plan_bytes, ws_bytes, scan_offset, chunk_offset, item_offset;
+};
+SharedCaps shared_caps(int32_t n_layers, int32_t B, int32_t Hq, int32_t Hkv, int32_t max_keep, int32_t n_groups);
+
+struct SharedPlanLaunch {
+    const int32_t *idx, *ranges, *count, *group;
+    int32_t *shared;
+    int32_t max_keep, B, n_groups, find, n_layers, Hq, Hkv;
+    uint8_t *plan;
+    SharedCaps caps;
+};
+int launch_shared_plan(const SharedPlanLaunch &p, murmur_stream_t stream);
+
+struct SharedAttnLaunch {
+    const uint16_t *q, *k, *v;
+    int64_t s_layer, s_b, s_h, s_pos;
+    const int32_t *idx, *ranges;
+    void *out;
+    float *lse;
+    const uint8_t *plan;
+    size_t item_offset, chunk_offset;
+    float *part_o;   // [layers * KV heads][rows][128], then the pairs
+    float *part_ml;  // [layers * KV heads][rows][2]  (running max in log2 units, sum)
+    int64_t rows_cap;
+    int32_t max_len, max_keep, B, Hq, Hkv, G, NL, n_groups, n_wg, out_f32;
+    float scale_log2;
+};
+int launch_decode_attn_shared(const SharedAttnLaunch &a, murmur_stream_t stream);
+
 int read_and_clear_device_error(murmur_stream_t stream, int32_t *code);
 const char *hip_error_text(int err);
 

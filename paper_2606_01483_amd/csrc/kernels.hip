@@ -13,6 +13,8 @@
 //   the last workgroup of each (layer, sequence, KV head).
 //   paged_step_kernel, paged_append_kernel: the device block manager of the
 //   paged cache (freeing behind the windows, appending the current token).
+//   pages.hpp, shared_attn.hpp (at the end): shared pages, and the attention over
+//   what a group of sequences shares.
 //
 // Attention data flow per 64-wide wavefront and pass of 32 retained positions:
 //   K, V rows --global_load_lds_dwordx4--> LDS stage (XOR-swizzled 16 B chunks)
@@ -2348,3 +2350,6 @@ int read_and_clear_device_error(murmur_stream_t stream, int32_t *code) {
 const char *hip_error_text(int err) { return hipGetErrorString((hipError_t)err); }
 
 }  // namespace murmur
+
+#include "pages.hpp"
+#include "shared_attn.hpp"

@@ -137,6 +137,11 @@ ENTRY(decode_step)
 ENTRY(decode_step_static)
 ENTRY(decode_step_ring)
 ENTRY(paged_step)
+ENTRY(paged_fork)
+ENTRY(paged_step_shared)
+ENTRY(paged_compact)
+ENTRY(shared_plan)
+ENTRY(decode_attn_shared)
 
 PyObject *structures(PyObject *, PyObject *const *args, Py_ssize_t n) {
     if (n != 2 || !PyType_Check(args[0]) || !PyType_Check(args[1])) {
@@ -155,7 +160,9 @@ PyObject *structures(PyObject *, PyObject *const *args, Py_ssize_t n) {
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {METHOD(evict_compact),      METHOD(evict_compact_paged), METHOD(decode_attn),
                            METHOD(decode_step),        METHOD(decode_step_static),  METHOD(decode_step_ring),
-                           METHOD(paged_step),         METHOD(structures),          {nullptr, nullptr, 0, nullptr}};
+                           METHOD(paged_step),         METHOD(paged_fork),          METHOD(paged_step_shared),
+                           METHOD(paged_compact),      METHOD(shared_plan),         METHOD(decode_attn_shared),
+                           METHOD(structures),         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_pycall", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -546,3 +546,101 @@ class DevicePagedBatch:
         M.murmur_decode_attn(self.q[i], self.kv, self.idx, None, self.count, self.max_keep, self.B, self.Hq, self.Hkv,
                              self.D, self.wl.scale, self.split_len, self.out, self.out_dtype, self.lse, self.ws,
                              self.ws_bytes, stream)
+
+
+class BeamBatch:
+    """Decode steps of several hypotheses per chunk on one paged pool: every chunk of the workload is decoded by
+    `width` sequences (neighbours in the batch) whose block tables share blocks up to where they parted.  A step is
+    murmur_paged_fork (each sequence continues its parent), murmur_paged_step_shared, murmur_evict_compact_paged,
+    murmur_shared_plan and murmur_decode_attn_shared: no host work, so a run of steps can be captured into one HIP
+    graph.
+
+    Memory plumbing only: the pool [NL][n_blocks * block_size][Hkv][D], the block table [chunks * width][max_blocks],
+    reference counts, free stack, workspaces and outputs.  The host prefill gives every position before step 0's
+    current token of each chunk a block, which all of its sequences name.  What the hypotheses are is the caller's:
+    step() takes their parents, queries and current-token K/V."""
+
+    def __init__(self, wl: Workload, width: int, block_size: int, n_blocks: int, device: str = "cuda",
+                 out_dtype: int = M.MURMUR_DTYPE_F32):
+        if np.ndim(wl.policy) == 3:
+            raise ValueError("paged steps take per-sequence policies")
+        self.wl, self.width, self.bs, self.n_blocks = wl, int(width), int(block_size), int(n_blocks)
+        self.rows, self.out_dtype = self.n_blocks * self.bs, out_dtype
+        chunks, NL, Hq, Hkv, D = wl.batch, wl.n_layers, wl.hq, wl.hkv, wl.head_dim
+        self.groups, self.B, self.NL, self.Hq, self.Hkv, self.D = chunks, chunks * self.width, NL, Hq, Hkv, D
+        self.max_blocks = int((-(-wl.seg(wl.steps - 1).sum(axis=1) // self.bs)).max())
+        self.max_keep = int(max(int(retained_counts(wl, s).max()) for s in range(wl.steps)))
+        dev = torch.device(device)
+        table = np.full((self.B, self.max_blocks), -1, dtype=np.int32)
+        ref = np.zeros(self.n_blocks, dtype=np.int32)
+        stack = list(range(self.n_blocks))
+        k = np.zeros((NL, self.rows, Hkv, D), dtype=np.uint16)
+        v = np.zeros_like(k)
+        seg0 = wl.seg(0)
+        for c in range(chunks):
+            n = int(seg0[c].sum()) - 1
+            for blk in range(-(-n // self.bs)):
+                if not stack:
+                    raise MemoryError("the pool cannot hold the prefill")
+                phys = stack.pop()
+                table[c * self.width:(c + 1) * self.width, blk] = phys
+                ref[phys] = self.width
+                lo, hi = blk * self.bs, min((blk + 1) * self.bs, n)
+                r0 = phys * self.bs
+                k[:, r0:r0 + hi - lo] = wl.k[:, c, :, lo:hi].transpose(0, 2, 1, 3)
+                v[:, r0:r0 + hi - lo] = wl.v[:, c, :, lo:hi].transpose(0, 2, 1, 3)
+
+        def i32(x):
+            return torch.from_numpy(np.ascontiguousarray(x, dtype=np.int32)).to(dev)
+
+        self.k = torch.from_numpy(k).view(torch.bfloat16).to(dev)
+        self.v = torch.from_numpy(v).view(torch.bfloat16).to(dev)
+        self.kv = M.make_kv(self.k, self.v, NL, self.rows, (self.rows * Hkv * D, 0, D, Hkv * D))
+        self.bt, self.ref = i32(table), i32(ref)
+        self.stack, self.top = i32(stack + [0] * (self.n_blocks - len(stack))), i32([len(stack)])
+        self.pol = i32(np.repeat(np.asarray(wl.policy), self.width, axis=0))
+        self.seg = i32(np.stack([np.repeat(wl.seg(s), self.width, axis=0) for s in range(wl.steps)]))
+        self.group = i32(np.arange(chunks + 1) * self.width)
+        self.shared, self.copied, self.map = i32(np.zeros(chunks)), i32(np.zeros(self.B)), i32(np.zeros(self.n_blocks))
+        self.idx, self.count = i32(np.full((self.B, self.max_keep), -1)), i32(np.zeros(self.B))
+        odt = torch.bfloat16 if out_dtype == M.MURMUR_DTYPE_BF16 else torch.float32
+        self.out = torch.zeros((NL, self.B, Hq, D), dtype=odt, device=dev)
+        self.lse = torch.zeros((NL, self.B, Hq), dtype=torch.float32, device=dev)
+        self.pages_bytes = M.murmur_paged_workspace(self.B, self.max_blocks, self.n_blocks)
+        self.ws_bytes, self.plan_bytes = M.murmur_decode_attn_shared_workspace(NL, self.B, Hq, Hkv, self.max_keep, chunks)
+        self.pages_ws = torch.zeros(self.pages_bytes // 4, dtype=torch.int32, device=dev)
+        self.plan = torch.zeros(self.plan_bytes // 4, dtype=torch.int32, device=dev)
+        self.ws = torch.zeros(self.ws_bytes // 4, dtype=torch.int32, device=dev)
+
+    def state(self) -> tuple:
+        """Copies of everything a step changes (pool, table, counts, stack, top)."""
+        return tuple(t.clone() for t in (self.k, self.v, self.bt, self.ref, self.stack, self.top))
+
+    def restore(self, st: tuple) -> None:
+        for t, s in zip((self.k, self.v, self.bt, self.ref, self.stack, self.top), st):
+            t.copy_(s)
+
+    def fork(self, parent, stream=None) -> None:
+        """Sequence b continues what sequence parent[b] was (int32 [B] on the device; -1 ends it)."""
+        M.murmur_paged_fork(parent, self.B, self.bt, self.max_blocks, self.ref, self.n_blocks, self.stack, self.top,
+                            self.n_blocks, self.pages_ws, self.pages_bytes, stream)
+
+    def compact(self, stream=None) -> None:
+        """Moves the blocks in use to the front of the pool."""
+        M.murmur_paged_compact(self.B, self.bt, self.max_blocks, self.bs, self.ref, self.n_blocks, self.stack, self.top,
+                               self.n_blocks, self.map, self.kv, self.Hkv, self.pages_ws, self.pages_bytes, stream)
+
+    def step(self, i: int, parent, q, k_new, v_new, stream=None) -> None:
+        """Step i: fork, then the current token (k_new, v_new [NL, B, Hkv, D]) and its attention (q [NL, B, Hq, D])."""
+        if parent is not None:
+            self.fork(parent, stream)
+        M.murmur_paged_step_shared(self.seg[i], self.pol, 1, self.B, self.bt, self.max_blocks, self.bs, self.ref,
+                                   self.n_blocks, self.stack, self.top, self.n_blocks, i == 0, self.copied, self.kv,
+                                   self.Hkv, k_new, v_new, stream)
+        M.murmur_evict_compact_paged(self.seg[i], self.pol, 1, self.B, self.bt, self.max_blocks, self.bs, self.idx,
+                                     self.max_keep, self.count, None, stream)
+        M.murmur_shared_plan(self.idx, None, self.count, self.max_keep, self.B, self.group, self.groups, self.shared,
+                             True, self.NL, self.Hq, self.Hkv, self.plan, self.plan_bytes, stream)
+        M.murmur_decode_attn_shared(q, self.kv, self.idx, None, self.max_keep, self.B, self.groups, self.Hq, self.Hkv,
+                                    self.D, self.wl.scale, self.out, self.out_dtype, self.lse, self.plan,
+                                    self.plan_bytes, self.ws, self.ws_bytes, stream)

@@ -22,6 +22,7 @@ MURMUR_DEVERR_CAPACITY = 16
 MURMUR_POL_PER_SEQ, MURMUR_POL_PER_LAYER = 1, 2
 MURMUR_DEVERR_BLOCK = 32
 MURMUR_DEVERR_POOL = 64
+MURMUR_DEVERR_PARENT, MURMUR_DEVERR_GROUP = 128, 256
 N_PIECES = 6
 SPLIT_UNIT = 128
 
@@ -61,6 +62,7 @@ _lib = None
 # it does not take, or a build without it, goes through ctypes.  Both call the same library.
 _PER_STEP = ("evict_compact", "evict_compact_paged", "decode_attn", "decode_step", "decode_step_static",
              "decode_step_ring", "paged_step")
+_PER_STEP_SHARED = ("paged_fork", "paged_step_shared", "paged_compact", "shared_plan", "decode_attn_shared")
 try:
     from . import _pycall
     _pycall.structures(murmur_kv, murmur_ring)
@@ -114,6 +116,23 @@ def _load():
     lib.murmur_decode_step_ring.argtypes = [vp, vp, i32, ctypes.POINTER(murmur_ring), vp, ctypes.POINTER(murmur_kv),
                                             vp, vp, vp, i32, i32, i32, i32, i32, ctypes.c_float, i32, vp, i32, vp,
                                             vp, sz, vp]
+    szp, kvp = ctypes.POINTER(sz), ctypes.POINTER(murmur_kv)
+    lib.murmur_paged_workspace.restype = ctypes.c_int
+    lib.murmur_paged_workspace.argtypes = [i32, i32, i32, szp]
+    lib.murmur_paged_fork.restype = ctypes.c_int
+    lib.murmur_paged_fork.argtypes = [vp, i32, vp, i32, vp, i32, vp, vp, i32, vp, sz, vp]
+    lib.murmur_paged_step_shared.restype = ctypes.c_int
+    lib.murmur_paged_step_shared.argtypes = [vp, vp, i32, i32, vp, i32, i32, vp, i32, vp, vp, i32, i32, vp, kvp, i32,
+                                             vp, vp, vp]
+    lib.murmur_paged_compact.restype = ctypes.c_int
+    lib.murmur_paged_compact.argtypes = [i32, vp, i32, i32, vp, i32, vp, vp, i32, vp, kvp, i32, vp, sz, vp]
+    lib.murmur_decode_attn_shared_workspace.restype = ctypes.c_int
+    lib.murmur_decode_attn_shared_workspace.argtypes = [i32, i32, i32, i32, i32, i32, szp, szp]
+    lib.murmur_shared_plan.restype = ctypes.c_int
+    lib.murmur_shared_plan.argtypes = [vp, vp, vp, i32, i32, vp, i32, vp, i32, i32, i32, i32, vp, sz, vp]
+    lib.murmur_decode_attn_shared.restype = ctypes.c_int
+    lib.murmur_decode_attn_shared.argtypes = [vp, kvp, vp, vp, i32, i32, i32, i32, i32, i32, ctypes.c_float, vp, i32,
+                                              vp, vp, sz, vp, sz, vp]
     f64p = ctypes.POINTER(ctypes.c_double)
     lib.murmur_plan_chunks.restype = ctypes.c_int
     lib.murmur_plan_chunks.argtypes = [f64p, f64p, i32, ctypes.c_double, ctypes.c_double, ctypes.c_double, i32p,
@@ -126,7 +145,7 @@ def _load():
     lib.murmur_device_error.argtypes = [vp, i32p]
     # (C function, its address, the converter) of each per-step entry point
     lib.per_step = {n: (getattr(lib, "murmur_" + n), ctypes.cast(getattr(lib, "murmur_" + n), vp).value,
-                        getattr(_pycall, n, None)) for n in _PER_STEP}
+                        getattr(_pycall, n, None)) for n in _PER_STEP + _PER_STEP_SHARED}
     _lib = lib
     return lib
 
@@ -342,6 +361,63 @@ def murmur_decode_step_ring(seg_dev, pol_dev, pol_per_seq: int, ring: murmur_rin
     """Eviction, attention and the current token's append on ring storage, in one launch."""
     _call("decode_step_ring", seg_dev, pol_dev, pol_per_seq, ring, q_dev, kv, idx_dev, count_dev, ranges_dev, max_keep,
           B, Hq, Hkv, D, float(scale), split_len, out_dev, out_dtype, lse_dev, ws_dev, ws_bytes, _stream(stream))
+
+
+def murmur_paged_workspace(B: int, max_blocks: int, n_blocks: int) -> int:
+    """Bytes of the workspace of murmur_paged_fork and murmur_paged_compact (zero-filled once)."""
+    nbytes = ctypes.c_size_t(0)
+    _check(_load().murmur_paged_workspace(B, max_blocks, n_blocks, ctypes.byref(nbytes)))
+    return int(nbytes.value)
+
+
+def murmur_paged_fork(parent_dev, B: int, block_table_dev, max_blocks: int, ref_dev, n_blocks: int, free_stack_dev,
+                      free_top_dev, capacity: int, ws_dev, ws_bytes: int, stream=None) -> None:
+    """Rows of the block table become copies of their parents' (-1: empty); blocks nobody names go free."""
+    _call("paged_fork", parent_dev, B, block_table_dev, max_blocks, ref_dev, n_blocks, free_stack_dev, free_top_dev,
+          capacity, ws_dev, ws_bytes, _stream(stream))
+
+
+def murmur_paged_step_shared(seg_dev, pol_dev, pol_per_seq: int, B: int, block_table_dev, max_blocks: int,
+                             block_size: int, ref_dev, n_blocks: int, free_stack_dev, free_top_dev, capacity: int,
+                             full_scan: bool, copied_dev, pool: murmur_kv | None = None, Hkv: int = 0, k_new_dev=None,
+                             v_new_dev=None, stream=None) -> None:
+    """murmur_paged_step on shared pages: free, take, copy on write, append the current K/V."""
+    _call("paged_step_shared", seg_dev, pol_dev, pol_per_seq, B, block_table_dev, max_blocks, block_size, ref_dev,
+          n_blocks, free_stack_dev, free_top_dev, capacity, int(bool(full_scan)), copied_dev, pool, Hkv, k_new_dev,
+          v_new_dev, _stream(stream))
+
+
+def murmur_paged_compact(B: int, block_table_dev, max_blocks: int, block_size: int, ref_dev, n_blocks: int,
+                         free_stack_dev, free_top_dev, capacity: int, map_dev, pool: murmur_kv | None, Hkv: int, ws_dev,
+                         ws_bytes: int, stream=None) -> None:
+    """The blocks in use move to the front of the pool; map_dev int32 [n_blocks]: their new numbers."""
+    _call("paged_compact", B, block_table_dev, max_blocks, block_size, ref_dev, n_blocks, free_stack_dev, free_top_dev,
+          capacity, map_dev, pool, Hkv, ws_dev, ws_bytes, _stream(stream))
+
+
+def murmur_decode_attn_shared_workspace(n_layers: int, B: int, Hq: int, Hkv: int, max_keep: int,
+                                        n_groups: int) -> tuple[int, int]:
+    """(workspace bytes, plan bytes) of murmur_decode_attn_shared."""
+    ws, plan = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check(_load().murmur_decode_attn_shared_workspace(n_layers, B, Hq, Hkv, max_keep, n_groups, ctypes.byref(ws),
+                                                       ctypes.byref(plan)))
+    return int(ws.value), int(plan.value)
+
+
+def murmur_shared_plan(idx_dev, ranges_dev, count_dev, max_keep: int, B: int, group_dev, n_groups: int, shared_dev,
+                       find_shared: bool, n_layers: int, Hq: int, Hkv: int, plan_dev, plan_bytes: int,
+                       stream=None) -> None:
+    """The work of murmur_decode_attn_shared over these lists; with find_shared, what each group shares too."""
+    _call("shared_plan", idx_dev, ranges_dev, count_dev, max_keep, B, group_dev, n_groups, shared_dev,
+          int(bool(find_shared)), n_layers, Hq, Hkv, plan_dev, plan_bytes, _stream(stream))
+
+
+def murmur_decode_attn_shared(q_dev, kv: murmur_kv, idx_dev, ranges_dev, max_keep: int, B: int, n_groups: int, Hq: int,
+                              Hkv: int, D: int, scale: float, out_dev, out_dtype: int, lse_dev, plan_dev,
+                              plan_bytes: int, ws_dev, ws_bytes: int, stream=None) -> None:
+    """murmur_decode_attn, reading what the sequences of a group share once (see murmur_shared_plan)."""
+    _call("decode_attn_shared", q_dev, kv, idx_dev, ranges_dev, max_keep, B, n_groups, Hq, Hkv, D, float(scale),
+          out_dev, out_dtype, lse_dev, plan_dev, plan_bytes, ws_dev, ws_bytes, _stream(stream))
 
 
 def murmur_plan_chunks(seg_start, seg_end, audio_len: float, max_chunk: float = 300.0,

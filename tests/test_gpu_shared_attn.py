@@ -1,0 +1,496 @@
+"""Attention over shared prefixes on the GPU (murmur_shared_plan, murmur_decode_attn_shared) against Equation 1 in
+fp64, within bounds derived from the inputs (tests/_shared.py)."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from oracle import paged as OP
+from oracle import shared as OS
+from paper_2606_01483_amd import murmur as M
+from paper_2606_01483_amd import workloads as W
+from paper_2606_01483_amd.decode import BeamBatch
+from _shared import attn_bounds
+
+pytestmark = pytest.mark.gpu
+D = 128
+
+
+def announce(msg):
+    print(f"\n[case] {msg}", flush=True)
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    M.lib()
+    yield
+    torch.cuda.synchronize()
+    assert M.murmur_device_error() == 0
+
+
+def i32(x):
+    return torch.from_numpy(np.ascontiguousarray(x, dtype=np.int32)).cuda()
+
+
+def bf16(rng, *shape, lift=1.0):
+    return torch.from_numpy(rng.standard_normal(shape, dtype=np.float32) * lift).to(torch.bfloat16).cuda()
+
+
+class Case:
+    """Lists over one pool: group p has `width` sequences, `common` entries alike and `rests` of their own."""
+
+    def __init__(self, seed, groups, NL=1, hq=28, hkv=4, scale=D ** -0.5, f32=True, spare=0, layout="flash", lift=1.0,
+                 extra_keep=0):
+        rng = self.rng = np.random.default_rng(seed)
+        self.NL, self.hq, self.hkv, self.scale = NL, hq, hkv, scale
+        lists, starts, common = [], [0], []
+        need = sum(c + sum(r) for c, r in groups)
+        rows = self.rows = need + 11
+        order = list(rng.permutation(rows)[:need])
+        for c, rests in groups:
+            lead = [order.pop() for _ in range(c)]
+            lists += [lead + [order.pop() for _ in range(r)] for r in rests]
+            starts.append(len(lists))
+            common.append(c if len(rests) != 1 else c + rests[0])
+        self.n_listed = len(lists)
+        lists += [[0]] * spare  # sequences behind the last group
+        self.lists, self.B, self.n_groups = lists, len(lists), len(groups)
+        self.starts, self.common = np.array(starts), np.array(common)
+        self.keep = max([1] + [len(x) for x in lists]) + extra_keep
+        idx = np.full((self.B, self.keep), -1, dtype=np.int32)
+        for b, x in enumerate(lists):
+            idx[b, :len(x)] = x
+        self.idx, self.count = i32(idx), i32([len(x) for x in lists])
+        self.group, self.shared = i32(starts), i32(np.full(max(1, len(groups)), -5))
+        self.q = bf16(rng, NL, self.B, hq, D, lift=lift)
+        self.k, self.v = bf16(rng, NL, rows, hkv, D), bf16(rng, NL, rows, hkv, D)
+        dead = torch.ones(rows, dtype=torch.bool)
+        for x in lists[:self.n_listed]:
+            dead[x] = False
+        for x in (self.k, self.v):
+            x[:, dead.cuda()] = float("nan")
+        if layout == "head":
+            self.k, self.v = (x.transpose(1, 2).contiguous().transpose(1, 2) for x in (self.k, self.v))
+            strides = (hkv * rows * D, 0, rows * D, D)
+        elif layout == "padded":
+            self.k, self.v = (torch.nn.functional.pad(x, (0, 16, 0, 1)) for x in (self.k, self.v))
+            strides = (rows * (hkv + 1) * 144, 0, 144, (hkv + 1) * 144)
+            self.full = self.k, self.v
+            self.k, self.v = (x[:, :, :hkv, :D] for x in (self.k, self.v))
+        else:
+            strides = (rows * hkv * D, 0, D, hkv * D)
+        self.kv = M.make_kv(self.k, self.v, NL, rows, strides)
+        self.f32 = f32
+        self.out = torch.full((NL, self.B, hq, D), 55.0, dtype=torch.float32 if f32 else torch.bfloat16, device="cuda")
+        self.lse = torch.full((NL, self.B, hq), 55.0, device="cuda")
+        self.sizes = M.murmur_decode_attn_shared_workspace(NL, self.B, hq, hkv, self.keep, self.n_groups)
+        self.ws, self.plan = (torch.full((n // 4,), -1, dtype=torch.int32, device="cuda") for n in self.sizes)
+
+    def make_plan(self, find=True):
+        M.murmur_shared_plan(self.idx, None, self.count, self.keep, self.B, self.group, self.n_groups, self.shared, find,
+                             self.NL, self.hq, self.hkv, self.plan, self.sizes[1])
+
+    def attend(self, lse=True):
+        M.murmur_decode_attn_shared(self.q, self.kv, self.idx, None, self.keep, self.B, self.n_groups, self.hq, self.hkv,
+                                    D, self.scale, self.out, M.MURMUR_DTYPE_F32 if self.f32 else M.MURMUR_DTYPE_BF16,
+                                    self.lse if lse else None, self.plan, self.sizes[1], self.ws, self.sizes[0])
+
+    def check(self, only=None):
+        torch.cuda.synchronize()
+        out, lse = self.out.float().cpu().numpy().astype(np.float64), self.lse.cpu().numpy().astype(np.float64)
+        q, k, v = (x.float().cpu().numpy() for x in (self.q, self.k, self.v))
+        for b in range(self.n_listed) if only is None else only:
+            for layer in range(self.NL):
+                args = q[layer, b], k[layer][self.lists[b]], v[layer][self.lists[b]], self.scale
+                want, want_lse = OS.attend(*args)
+                far, far_lse = attn_bounds(*args, want, want_lse)
+                if not self.f32:
+                    far = far + np.abs(want) * 2.0 ** -8 + far * 2.0 ** -8
+                err = np.abs(out[layer, b] - want)
+                assert (err <= far).all(), (b, layer, float((err / far).max()))
+                assert (np.abs(lse[layer, b] - want_lse) <= far_lse).all(), (b, layer)
+
+
+# (positions a group shares, the rests of its sequences)
+GROUPS = {
+    "one token": [(0, [1])],
+    "one shared token": [(1, [0, 0, 0])],
+    "single sequences": [(0, [5]), (33, [0]), (17, [20])],
+    "nothing shared": [(0, [31, 32, 33, 1])],
+    "no rest for some": [(40, [0, 1, 0, 70]), (64, [0, 0])],
+    "pass edges": [(31, [1, 2]), (32, [31, 33]), (33, [64, 65]), (255, [255, 1]), (256, [257, 0]), (257, [8, 9])],
+    "odd groups": [(100, [3] * 9), (1, [200, 5]), (700, [40, 41, 42, 43, 44]), (60, [7] * 17)],
+    "long prefix": [(5001, [17, 0, 133])],
+    "long rests": [(9, [2100, 1, 3300]), (4200, [4100, 4097])],
+    "many": [(int(c), [int(x) for x in r]) for c, r in
+             zip(np.random.default_rng(0).integers(0, 90, 70),
+                 [np.random.default_rng(i).integers(1, 50, 1 + i % 7) for i in range(70)])],
+}
+
+
+@pytest.mark.parametrize("hq,hkv", [(28, 4), (16, 1), (3, 3)])
+@pytest.mark.parametrize("name", sorted(GROUPS))
+def test_index_lists(name, hq, hkv):
+    announce(f"shared attention, {name}, {hq}/{hkv}")
+    c = Case(len(name) + hq, GROUPS[name], hq=hq, hkv=hkv)
+    c.make_plan()
+    c.attend()
+    c.check()
+    assert c.shared.cpu().tolist() == c.common.tolist()
+    assert M.murmur_device_error() == 0
+
+
+@pytest.mark.parametrize("hq,hkv,width", [(28, 4, 9), (28, 4, 10), (28, 4, 19), (16, 1, 4), (16, 1, 5), (1, 1, 64),
+                                          (1, 1, 65), (2, 2, 130), (15, 1, 9), (12, 4, 21)])
+def test_row_tiles(hq, hkv, width):
+    """Groups at and beyond the query rows of one item, several layers, bf16 outputs."""
+    announce(f"row tiles {hq}/{hkv} x {width}")
+    c = Case(width, [(300, [x % 5 for x in range(width)]), (45, [3])], NL=3, hq=hq, hkv=hkv, f32=False)
+    c.make_plan()
+    c.attend()
+    c.check()
+
+
+@pytest.mark.parametrize("layout", ["head", "padded"])
+def test_layouts(layout):
+    announce(f"pool layout {layout}")
+    c = Case(5, [(90, [10, 0, 33]), (0, [50])], NL=2, layout=layout)
+    c.make_plan()
+    c.attend()
+    c.check()
+
+
+@pytest.mark.parametrize("scale,lift", [(0.0, 1.0), (-0.7, 1.0), (1.0, 4.0), (1e-30, 1.0), (40.0, 30.0)])
+def test_scales(scale, lift):
+    """Negative and zero scales, and logits of thousands (a one-hot softmax)."""
+    announce(f"scale {scale}")
+    c = Case(6, [(200, [30, 1, 0]), (0, [3])], scale=scale, lift=lift)
+    c.make_plan()
+    c.attend()
+    c.check()
+
+
+def test_shares_given_by_the_caller():
+    """Any number up to what the lists share gives the same result; too many is an error of the sequences it is too
+    many for, or of the whole group where the first one's list is too short."""
+    announce("given shares")
+    c = Case(7, [(70, [10, 0, 5]), (40, [0, 2])], extra_keep=40)
+    for given in ([70, 40], [0, 0], [33, 1], [69, 39]):
+        c.shared.copy_(i32(given))
+        c.make_plan(find=False)
+        c.out.fill_(55)
+        c.attend()
+        c.check()
+        assert c.shared.cpu().tolist() == given
+    assert M.murmur_device_error() == 0
+    for given, bad in (([72, 40], [1]), ([81, 40], [0, 1, 2]), ([70, 41], [3, 4]), ([-1, 40], [0, 1, 2]),
+                       ([70, 1 << 30], [3, 4])):
+        c.shared.copy_(i32(given))
+        c.make_plan(find=False)
+        c.attend()
+        torch.cuda.synchronize()
+        assert M.murmur_device_error() & M.MURMUR_DEVERR_COUNT, given
+        for b in range(5):
+            assert bool(torch.isnan(c.out[:, b]).all()) == (b in bad), (given, b)
+        if given[0] != 72:  # (72 shares two entries that differ: a broken promise)
+            c.check([b for b in range(5) if b not in bad])
+
+
+def test_bad_counts():
+    """A count of zero or above max_keep is the sequence's own error; the others share as if it were not there."""
+    announce("bad counts")
+    c = Case(8, [(50, [10, 0, 5, 9]), (40, [3, 2])])
+    count = c.count.clone()
+    for bad, value in ((1, 0), (2, c.keep + 1), (3, -4)):
+        c.count[bad] = value
+        c.make_plan()
+        c.attend()
+        torch.cuda.synchronize()
+        assert M.murmur_device_error() == M.MURMUR_DEVERR_COUNT
+        assert torch.isnan(c.out[:, bad]).all() and torch.isnan(c.lse[:, bad]).all()
+        c.check([b for b in range(6) if b != bad])
+        assert c.shared.cpu().tolist() == [50, 40]
+        c.count.copy_(count)
+    c.count[4] = 0  # the first one of its group
+    c.make_plan()
+    c.attend()
+    torch.cuda.synchronize()
+    assert M.murmur_device_error() == M.MURMUR_DEVERR_COUNT
+    assert torch.isnan(c.out[:, 4]).all()
+    c.check([0, 1, 2, 3])
+    assert int(c.shared[1]) == 0
+
+
+def test_positions_outside_the_pool():
+    announce("positions outside the pool")
+    c = Case(9, [(50, [10, 0, 5]), (40, [3, 2])])
+    c.idx[2, 53] = c.rows  # in the rest of sequence 2
+    c.make_plan()
+    c.attend()
+    torch.cuda.synchronize()
+    assert M.murmur_device_error() == M.MURMUR_DEVERR_POSITION
+    assert torch.isnan(c.out[:, 2]).all()
+    c.check([0, 1, 3, 4])
+    c.idx[:3, 20] = -1  # in what sequences 0 to 2 share
+    c.make_plan()
+    c.attend()
+    torch.cuda.synchronize()
+    assert M.murmur_device_error() == M.MURMUR_DEVERR_POSITION
+    assert torch.isnan(c.out[:, :3]).all()
+    c.check([3, 4])
+
+
+@pytest.mark.parametrize("group", [[1, 3, 5], [0, 4, 3], [0, 3, 9], [0, -1, 5]])
+def test_groups_out_of_order(group):
+    announce(f"groups {group}")
+    c = Case(10, [(50, [10, 0, 5]), (40, [3, 2])])
+    c.group.copy_(i32(group))
+    c.make_plan()
+    c.attend()
+    torch.cuda.synchronize()
+    assert M.murmur_device_error() & M.MURMUR_DEVERR_GROUP
+    assert torch.isnan(c.out).all() and torch.isnan(c.lse).all()
+
+
+def test_a_plan_of_another_call():
+    announce("plan of another call")
+    c = Case(11, [(50, [10, 0, 5])], NL=2)
+    for fill in (0, -1):
+        c.plan.fill_(fill)
+        c.attend()
+        torch.cuda.synchronize()
+        assert M.murmur_device_error() == M.MURMUR_DEVERR_GROUP
+        assert torch.isnan(c.out).all()
+    one = M.make_kv(c.k, c.v, 1, c.rows, (0, 0, D, c.hkv * D))
+    c.sizes = [max(s) for s in zip(c.sizes, M.murmur_decode_attn_shared_workspace(1, c.B, c.hq, c.hkv, c.keep, 1))]
+    c.ws, c.plan = (torch.full((n // 4,), -1, dtype=torch.int32, device="cuda") for n in c.sizes)
+    c.make_plan()
+    M.murmur_decode_attn_shared(c.q, one, c.idx, None, c.keep, c.B, c.n_groups, c.hq, c.hkv, D, c.scale, c.out,
+                                M.MURMUR_DTYPE_F32, c.lse, c.plan, c.sizes[1], c.ws, c.sizes[0])
+    torch.cuda.synchronize()
+    assert M.murmur_device_error() == M.MURMUR_DEVERR_GROUP
+    c.attend()
+    c.check()
+
+
+def test_sequences_behind_the_last_group_and_empty_groups():
+    announce("sequences behind the last group, empty groups")
+    c = Case(12, [(0, []), (50, [10, 0, 5]), (0, []), (20, [3, 2]), (0, [])], spare=3)
+    c.make_plan()
+    c.attend(lse=False)
+    torch.cuda.synchronize()
+    assert (c.out[:, 5:] == 55).all() and (c.lse == 55).all()
+    c.attend()
+    c.check()
+    assert (c.lse[:, 5:] == 55).all() and c.shared.cpu().tolist() == [0, 50, 0, 20, 0]
+    assert M.murmur_device_error() == 0
+
+
+def test_ranges_of_sequence_ordered_caches():
+    """Chunks with caches of their own behind one prompt, from range tables; what is shared is read from the first
+    one's cache only (the others' copies are NaN)."""
+    announce("range tables")
+    rng = np.random.default_rng(13)
+    NL, B, hq, hkv, prompt = 2, 7, 28, 4, 75
+    seg = np.stack([np.full(B, prompt), rng.integers(0, 400, B), rng.integers(0, 6, B), rng.integers(1, 90, B)], 1).astype(np.int32)
+    pol = np.stack([np.array([50, -1, 64, 33, -1, 7, 300]), rng.integers(0, 40, B), rng.integers(0, 5, B),
+                    np.array([20, -1, 8, 5, -1, 30, 11]), rng.integers(0, 3, B)], 1).astype(np.int32)
+    L = (int(seg.sum(1).max()) + 7) // 8 * 8
+    idx, cnt = oracle.retained(seg, pol)
+    keep = idx.shape[1]
+    q, k, v = bf16(rng, NL, B, hq, D), bf16(rng, NL, B, hkv, L, D), bf16(rng, NL, B, hkv, L, D)
+    group, shared = i32([0, 4, 7]), i32([prompt, prompt - 5])
+    for x in (k, v):
+        for b in (1, 2, 3, 5, 6):
+            x[:, b, :, :prompt] = x[:, 0 if b < 4 else 4, :, :prompt]
+    whole = [x.float().cpu().numpy().transpose(0, 1, 3, 2, 4) for x in (k, v)]
+    for x in (k, v):
+        for b in (1, 2, 3, 5, 6):
+            x[:, b, :, :prompt if b < 4 else prompt - 5] = float("nan")
+    d_idx, d_cnt, d_ranges = i32(np.zeros((B, keep))), i32(np.zeros(B)), i32(np.zeros((B, 6, 2)))
+    M.murmur_evict_compact(i32(seg), i32(pol), 1, B, d_idx, keep, d_cnt, d_ranges)
+    ws_bytes, plan_bytes = M.murmur_decode_attn_shared_workspace(NL, B, hq, hkv, keep, 2)
+    ws, plan = (torch.zeros(n // 4, dtype=torch.int32, device="cuda") for n in (ws_bytes, plan_bytes))
+    kv = M.kv_from_tensors(k, v)
+    for ranges in (d_ranges, None):  # and the same positions from index lists
+        out, lse = torch.zeros((NL, B, hq, D), device="cuda"), torch.zeros((NL, B, hq), device="cuda")
+        M.murmur_shared_plan(d_idx, ranges, d_cnt, keep, B, group, 2, shared, False, NL, hq, hkv, plan, plan_bytes)
+        M.murmur_decode_attn_shared(q, kv, d_idx, ranges, keep, B, 2, hq, hkv, D, 0.11, out, M.MURMUR_DTYPE_F32, lse,
+                                    plan, plan_bytes, ws, ws_bytes)
+        torch.cuda.synchronize()
+        assert M.murmur_device_error() == 0
+        for b in range(B):
+            at = idx[b, :cnt[b]]
+            for layer in range(NL):
+                args = q[layer, b].float().cpu().numpy(), whole[0][layer, b][at], whole[1][layer, b][at], 0.11
+                want, want_lse = OS.attend(*args)
+                far, far_lse = attn_bounds(*args, want, want_lse)
+                assert (np.abs(out[layer, b].cpu().numpy() - want) <= far).all(), (b, layer)
+                assert (np.abs(lse[layer, b].cpu().numpy() - want_lse) <= far_lse).all(), (b, layer)
+
+
+def test_same_bits_every_run_and_replay():
+    """Eager runs, runs on another stream and graph replays (plan and attention captured) give the same bits, and a
+    graph replayed after the lists have changed follows them."""
+    announce("replays")
+    c = Case(14, [(600, [30, 1, 0, 90]), (80, [3] * 6)], NL=2)
+    c.make_plan()
+    c.attend()
+    c.check()
+    want = c.out.clone(), c.lse.clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.make_plan()
+        c.attend()
+    for _ in range(3):
+        c.out.fill_(0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(c.out, want[0]) and torch.equal(c.lse, want[1])
+        c.out.fill_(0)
+        other = torch.cuda.Stream()
+        other.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(other):
+            c.make_plan()
+            c.attend()
+        torch.cuda.synchronize()
+        assert torch.equal(c.out, want[0])
+    c.idx[1, 100:400] = c.idx[1, 100:400].flip(0).clone()  # sequence 1 leaves its group at 100
+    c.count[3] = 300
+    c.lists[1] = c.idx[1, :601].cpu().tolist()
+    c.lists[3] = c.lists[3][:300]
+    graph.replay()
+    c.check()
+    assert c.shared.cpu().tolist() == [100, 80]
+
+
+def test_two_calls_at_once():
+    """Two streams, one plan, a workspace each."""
+    announce("two calls at once")
+    c = Case(15, [(900, [30, 1, 0, 90])], NL=2)
+    c.make_plan()
+    c.attend()
+    c.check()
+    want = c.out.clone()
+    outs = [torch.zeros_like(c.out) for _ in range(2)]
+    spaces = [torch.empty_like(c.ws) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for s, o, w in zip(streams, outs, spaces):
+            with torch.cuda.stream(s):
+                M.murmur_decode_attn_shared(c.q, c.kv, c.idx, None, c.keep, c.B, c.n_groups, c.hq, c.hkv, D, c.scale, o,
+                                            M.MURMUR_DTYPE_F32, None, c.plan, c.sizes[1], w, c.sizes[0])
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+
+
+def test_a_pool_past_2_gib():
+    """Rows whose offsets pass 32 bits, in bytes and in elements."""
+    announce("offsets past 32 bits")
+    rows, hkv = (1 << 32) // (4 * D) + 4096, 4
+    c = Case(16, [(40, [10, 3])])
+    k, v = (torch.empty((1, rows, hkv, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    far = np.random.default_rng(1).permutation(rows - c.rows)[:c.rows]
+    far[:c.rows // 2] = rows - 1 - np.arange(c.rows // 2)  # half of them at the end
+    at = torch.from_numpy(far).cuda()
+    k[:, at], v[:, at] = c.k, c.v
+    idx = c.idx.long()
+    c.idx.copy_(torch.where(idx >= 0, at[idx.clamp(min=0)], -1).int())
+    c.kv = M.make_kv(k, v, 1, rows, (0, 0, D, hkv * D))
+    c.make_plan()
+    c.attend()
+    c.check()
+
+
+@pytest.mark.parametrize("block_size", [16, 4])
+def test_beam_decode(block_size):
+    """A beam decode of 60 steps (fork, paging with copies on write, eviction, plan, attention, a compaction now and
+    then): every hypothesis attends over its own history, as the oracle computes it over a cache of its own."""
+    announce(f"beam decode, block {block_size}")
+    rng = np.random.default_rng(17 + block_size)
+    steps, width = 60, 3
+    seg0 = np.array([[16, 100, 4, 10], [30, 70, 0, 25]], dtype=np.int32)
+    pol = np.array([[48, 20, 4, 40, 2], [-1, 0, 0, -1, 0]], dtype=np.int32)
+    wl = W.build("beams", 717, 2, seg0, pol, steps, planted=False, hq=8, hkv=2)
+    last = int((-(-wl.seg(steps - 1).sum(axis=1) // block_size)).sum())
+    bb = BeamBatch(wl, width, block_size, last * width)
+    L = int(wl.seg(steps - 1).sum(axis=1).max())
+    caches = []  # per sequence, in order: what it has written
+    for x in (wl.k, wl.v):
+        y = np.zeros((2, 6, 2, L, D), dtype=np.uint16)
+        n = min(L, x.shape[3])
+        y[:, :, :, :n] = np.repeat(x[:, :, :, :n], width, axis=1)
+        caches.append(y)
+    policy = np.repeat(pol, width, axis=0)
+    for s in range(steps):
+        parent = np.arange(6) // width * width + rng.integers(0, width, 6)
+        seg = np.repeat(wl.seg(s), width, axis=0)
+        q, kn, vn = (W.f32_to_bf16_bits(rng.standard_normal(sh)) for sh in ((2, 6, 8, D), (2, 6, 2, D), (2, 6, 2, D)))
+        up = [torch.from_numpy(x).view(torch.bfloat16).cuda() for x in (q, kn, vn)]
+        bb.step(s, i32(parent), *up)
+        if s % 9 == 8:
+            bb.compact()
+        caches = [x[:, parent].copy() for x in caches]
+        for x, new in zip(caches, (kn, vn)):
+            for b in range(6):
+                x[:, b, :, int(seg[b].sum()) - 1] = new[:, b]
+        torch.cuda.synchronize()
+        assert M.murmur_device_error() == 0, f"step {s}"
+        idx, cnt = oracle.retained(seg, policy)
+        assert np.array_equal(bb.count.cpu().numpy(), cnt)
+        lists = bb.idx.cpu().numpy()
+        if s % 9 != 8:
+            table = bb.bt.cpu().numpy()
+            assert np.array_equal(lists[:, :idx.shape[1]], OP.rows_of(idx, cnt, table, block_size))
+        assert bb.shared.cpu().tolist() == [OS.common([lists[b, :cnt[b]] for b in range(3 * g, 3 * g + 3)]) for g in range(2)]
+        want, want_lse = oracle.attend(q, *caches, idx, cnt, scale=wl.scale, n_threads=16)
+        out, lse = bb.out.cpu().numpy(), bb.lse.cpu().numpy()
+        f = W.bf16_bits_to_f32
+        for layer in range(2):
+            for b in range(6):
+                at = idx[b, :cnt[b]]
+                far, far_lse = attn_bounds(f(q[layer, b]), f(caches[0][layer, b])[:, at].transpose(1, 0, 2),
+                                           f(caches[1][layer, b])[:, at].transpose(1, 0, 2), wl.scale, want[layer, b],
+                                           want_lse[layer, b])
+                assert (np.abs(out[layer, b] - want[layer, b]) <= far).all(), (s, layer, b)
+                assert (np.abs(lse[layer, b] - want_lse[layer, b]) <= far_lse).all(), (s, layer, b)
+        used = set(bb.bt.cpu().numpy().ravel().tolist()) - {-1}
+        free = bb.stack[:int(bb.top.item())].cpu().numpy().tolist()
+        assert sorted(list(used) + free) == list(range(bb.n_blocks))
+
+
+def test_beam_decode_captured():
+    """Six steps of a beam decode in one graph, replayed three times from the starting state: the eager run's bits."""
+    announce("beam decode captured")
+    rng = np.random.default_rng(18)
+    seg0 = np.array([[16, 60, 4, 10], [30, 70, 0, 25]], dtype=np.int32)
+    wl = W.build("beams_graph", 718, 2, seg0, np.array([32, 5, 4, 16, 2], dtype=np.int32), 6, planted=False, hq=8, hkv=2)
+    bb = BeamBatch(wl, 4, 8, 200)
+    parents = [i32(np.arange(8) // 4 * 4 + rng.integers(0, 4, 8)) for _ in range(6)]
+    ins = [[bf16(rng, 2, 8, h, D) for h in (8, 2, 2)] for _ in range(6)]
+    start = bb.state()
+
+    def run():
+        for s in range(6):
+            bb.step(s, parents[s], *ins[s])
+
+    run()
+    torch.cuda.synchronize()
+    want = (bb.out.clone(), bb.lse.clone(), bb.shared.clone()) + bb.state()
+    bb.restore(start)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for _ in range(3):
+        bb.restore(start)
+        bb.out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, w in zip((bb.out, bb.lse, bb.shared, bb.k, bb.v, bb.bt, bb.ref, bb.stack, bb.top), want):
+            assert torch.equal(got, w)
+    assert M.murmur_device_error() == 0
