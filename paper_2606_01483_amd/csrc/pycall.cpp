@@ -1,4 +1,4 @@
-// Python entry to the per-step calls of libmurmur (include/murmur.h): converts
+// Python entry to the per-step calls of libmurmur (include/murmur.h, include/murmur_shared.h): converts
 // the arguments of one call in C and makes it.  murmur.py's ctypes calls did
 // the same in about 4.4 us for a decode step of 22 arguments, more than the
 // launch itself; this takes about 1.2 us.  Each function takes the C function's
@@ -11,7 +11,7 @@
 #include <tuple>
 #include <utility>
 
-#include "murmur.h"
+#include "murmur_shared.h"
 
 namespace {
 

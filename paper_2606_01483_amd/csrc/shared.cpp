@@ -1,12 +1,12 @@
 // C ABI of shared pages and of the attention over shared prefixes
-// (include/murmur.h): argument checks, buffer sizes and dispatch.  As in api.cpp,
+// (include/murmur_shared.h): argument checks, buffer sizes and dispatch.  As in api.cpp,
 // every check runs before the first HIP call.
 #include <math.h>
 
 #include <algorithm>
 
 #include "internal.h"
-#include "murmur.h"
+#include "murmur_shared.h"
 
 namespace murmur {
 namespace {

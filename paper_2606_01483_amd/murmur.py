@@ -1,4 +1,4 @@
-"""ctypes binding of libmurmur.so (include/murmur.h), one Python function per C entry point.
+"""ctypes binding of libmurmur.so (include/murmur.h, include/murmur_shared.h), one Python function per C entry point.
 
 Argument marshalling only: every step of the decode path runs in the HIP
 kernels behind the C ABI.  Device buffers are torch tensors (or raw device

@@ -1,6 +1,8 @@
 """Argument checks and sizes of the calls on shared pages and shared prefixes (no GPU: every call here is refused, or
 fails at its first HIP call, so the module is skipped where a GPU is visible)."""
 import ctypes
+import os
+import re
 
 import numpy as np
 import pytest
@@ -56,6 +58,14 @@ def route(request, monkeypatch):
         assert all(lib.per_step[n][2] is not None for n in M._PER_STEP_SHARED)
     else:
         monkeypatch.setattr(lib, "per_step", {n: (fn, at, None) for n, (fn, at, _) in lib.per_step.items()})
+
+
+def test_exports_every_declared_function():
+    header = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "murmur_shared.h")).read()
+    names = set(re.findall(r"^int (murmur_\w+)\(", header, re.M))
+    assert names == set(CALLS) | {"murmur_paged_workspace", "murmur_decode_attn_shared_workspace"}
+    for n in names:
+        assert hasattr(ctypes.CDLL(M.LIB_PATH), n) and callable(getattr(M, n)), n
 
 
 def test_every_call_is_here():
