@@ -40,8 +40,8 @@ extern "C" {
  * that does not agree with the counts) give MURMUR_DEVERR_POOL and are dropped. */
 
 /* Workspace bytes of murmur_paged_fork and murmur_paged_compact (one workspace
- * serves both): 256-byte aligned, zero-filled once before its first use, and not
- * used by two calls at the same time. */
+ * serves both, for one B, max_blocks and n_blocks): 256-byte aligned, zero-filled
+ * once before its first use, and not used by two calls at the same time. */
 int murmur_paged_workspace(int32_t B, int32_t max_blocks, int32_t n_blocks, size_t *bytes);
 
 /* Forks, reorders and ends sequences: row b of the table becomes a copy of what

@@ -182,17 +182,34 @@ int launch_paged_append(const murmur_seg *seg, int32_t B, const int32_t *bt, int
 
 // ---- shared pages and shared prefixes (shared.cpp; pages.hpp and shared_attn.hpp) ----
 
-// Workspace of murmur_paged_fork and murmur_paged_compact, int32 words.  The
-// header holds fork's ticket (zero between calls) and compact's number of moves.
-// After it, for fork, one count per row (rounded up to 64) and the changed entries
-// (ForkEntry) of every row; for compact the source and then the destination
-// blocks of at most n_blocks / 2 moves each.
-constexpr int kForkHeader = 64;
-struct ForkEntry {
-    int32_t col, fresh, old, unused;
+// Workspace of murmur_paged_fork and murmur_paged_compact: fork's header, the place
+// of every block's first entry, and a bit per place (zero between calls); then what a
+// call leaves to no other: fork's lists of changes (one per kForkCols columns of a
+// row) and the freed blocks by place, or compact's number of moves and the source
+// and destination blocks of at most n_blocks / 2.
+constexpr int kForkCols = 256;
+constexpr int kForkPlaces = 1 << 15;  // places of a workgroup that pushes
+struct ForkHead {
+    int32_t call;  // calls so far
+    int32_t top;   // the stack's, before the call's pushes
+    int32_t unused[62];
+};
+struct ForkChange {
+    uint32_t place;
+    int32_t fresh, old;
+};
+struct ForkWorkspace {
+    ForkHead *head;
+    uint64_t *first;      // [n_blocks]
+    ForkChange *changes;  // [lists][kForkCols]
+    int32_t *counts;      // [lists]
+    int32_t *freed;       // [B * max_blocks / kForkPlaces]: bits set
+    int32_t *block_at;    // [B * max_blocks]
+    uint32_t *bits;       // [B * max_blocks / 32]
 };
 int launch_paged_fork(const int32_t *parent, int32_t B, int32_t *bt, int32_t max_blocks, int32_t *ref,
-                      int32_t n_blocks, int32_t *stack, int32_t *top, int32_t *ws, murmur_stream_t stream);
+                      int32_t n_blocks, int32_t *stack, int32_t *top, const ForkWorkspace &ws,
+                      murmur_stream_t stream);
 int launch_paged_step_shared(const murmur_seg *seg, const murmur_policy *pol, int32_t pol_per_seq, int32_t B,
                              int32_t *bt, int32_t max_blocks, int32_t log2_bs, int32_t *ref, int32_t n_blocks,
                              int32_t *stack, int32_t *top, int32_t full_scan, int32_t *copied,

@@ -2,7 +2,8 @@
 // block tables whose rows may name the same blocks, with a reference count per
 // block.
 //
-//   fork_kernel              rows of the table become copies of other rows
+//   fork_compare_kernel, fork_apply_kernel, fork_push_kernel
+//                            rows of the table become copies of other rows
 //   step_shared_kernel       the block manager's step with reference counts and
 //                            copies on write
 //   append_shared_kernel     the copied rows and the current token's K/V
@@ -11,10 +12,9 @@
 //
 // Counts change by integer atomics, whose order does not matter.  What does
 // matter is where a block that nobody names any more lands on the free stack:
-// every entry that gave it up offers its place (row, column) with an atomic
-// minimum on the count itself, which is zero by then, so that the block is
-// pushed by its first entry whatever the timing, and the stack is the same on
-// every run.
+// every entry that gave it up has a place (row, column), and the block is pushed by
+// its first one, found with atomic minima or maxima, whatever the timing.  So the
+// stack is the same on every run.
 #pragma once
 
 namespace murmur {
@@ -30,14 +30,6 @@ static __device__ __forceinline__ void store_shared_word(int32_t *p, int32_t x) 
 static __device__ __forceinline__ void add_ref(int32_t *ref, int32_t n) {
     __hip_atomic_fetch_add(ref, n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-// Offers place `at` (below 2^30) as the one that pushes a block whose count is
-// zero; counts that are offered for are negative.
-static __device__ __forceinline__ int32_t place_key(int32_t at) { return (int32_t)(0x80000000u + (uint32_t)at); }
-static __device__ __forceinline__ void offer_place(int32_t *ref, int32_t at) {
-    if (load_shared_word(ref) <= 0)
-        __hip_atomic_fetch_min(ref, place_key(at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-
 // Exclusive scan of one int per thread over a workgroup of kThreads; `total` in
 // every thread.  s: one int per wavefront (two barriers).
 template <int kThreads>
@@ -64,200 +56,279 @@ static __device__ __forceinline__ int wg_exclusive_scan(int v, int *s, int tid, 
 }
 
 // ---------------------------------------------------------------------------
-// fork.  A workgroup per row compares it with its parent's, moves the counts of
-// the blocks that differ and lists the entries that change, in column order; no
-// table entry is written while another workgroup may read it as a parent's.  The
-// workgroup that ends last takes all rows' lists, 1024 entries at a time: it
-// pushes the blocks whose count went to zero (see above) and writes the table.
-// Beams differ from their parents in the blocks of their last tokens only, so
-// the lists are short and the comparison, which reads the table twice, is the
-// work; it is spread over the chip.
+// fork, in three launches; the first two have a wavefront per 256 columns of a row.
+//   fork_compare_kernel  Each entry that differs from the parent's moves the two
+//     counts, enters its place for the block that it gives up (`first`: a maximum of
+//     (call number, 2^30 - place), so that nothing has to be reset between calls),
+//     and goes on the wavefront's list of changes, marked if it took the count to
+//     zero.  No table entry is written while another wavefront may read it.
+//   fork_apply_kernel  The counts are final.  The changes are written, and a marked
+//     one whose block is free sets a bit at the block's first entry's place.
+//   fork_push_kernel  The blocks are pushed in the order of their bits.
+// Nothing but the comparison looks at the whole table: hypotheses differ from their
+// parents in the blocks of their last tokens only.  Bound by round trips to memory.
+// 96 rows of 215 blocks 12.5 us, 1024 rows of 311 21.0.  In one launch,
+// with the list left to the workgroup that ends last, 11.0 and 58.8: a compute unit
+// has only so many scattered loads on their way.
 // ---------------------------------------------------------------------------
-constexpr int kForkThreads = 512;
+constexpr int kForkThreads = 1024;
+constexpr int kForkWaves = kForkThreads / 64;
+constexpr uint32_t kForkEmptied = 1u << 31;  // mark of a change's place (places are below 2^30)
 
-__global__ __launch_bounds__(kForkThreads) void fork_kernel(const int32_t *__restrict__ parent, int32_t B,
-                                                            int32_t *bt, int32_t max_blocks, int32_t *ref,
-                                                            int32_t n_blocks, int32_t *stack, int32_t *top,
-                                                            int32_t *ws) {
-    __shared__ int s_scan[kForkThreads / 64];
-    __shared__ int s_first[kForkThreads + 1];
-    __shared__ int s_last;
-    const int tid = threadIdx.x, b = blockIdx.x;
-    int32_t *ticket = ws, *count = ws + kForkHeader;
-    ForkEntry *lists = reinterpret_cast<ForkEntry *>(ws + kForkHeader + ((B + 63) & ~63));
+// The wavefront's row and first column (its lane's), or none.
+struct ForkUnit {
+    int64_t at;
+    int b, col;
+};
+static __device__ __forceinline__ ForkUnit fork_unit(int32_t B, int32_t max_blocks, int wave, int lane) {
+    const int segs = (max_blocks + kForkCols - 1) / kForkCols;
+    const int64_t unit = (int64_t)blockIdx.x * kForkWaves + wave;
+    if (unit >= (int64_t)B * segs) return ForkUnit{-1, 0, 0};
+    const int b = (int)(unit / segs);
+    return ForkUnit{unit, b, (int)(unit - (int64_t)b * segs) * kForkCols + lane};
+}
+
+__global__ __launch_bounds__(kForkThreads) void fork_compare_kernel(const int32_t *__restrict__ parent, int32_t B,
+                                                                    const int32_t *__restrict__ bt,
+                                                                    int32_t max_blocks, int32_t *ref,
+                                                                    int32_t n_blocks, const ForkWorkspace ws) {
+    const int lane = threadIdx.x & 63;
+    const ForkUnit u = fork_unit(B, max_blocks, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane);
+    if (u.at < 0) return;
+    if (lane == 0 && u.at < ((int64_t)B * max_blocks - 1) / kForkPlaces + 1) ws.freed[u.at] = 0;
+    const uint32_t call = (uint32_t)ws.head->call + 1;
     int err = 0;
-    int32_t p = parent[b];
+    int32_t p = parent[u.b];
     if (p < -1 || p >= B) {
         err |= MURMUR_DEVERR_PARENT;
-        p = b;
+        p = u.b;
     }
+    int32_t old[4], fresh[4];
+    const int32_t *mine = bt + (int64_t)u.b * max_blocks, *from = bt + (int64_t)(p < 0 ? 0 : p) * max_blocks;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int c = u.col + 64 * j;
+        old[j] = c < max_blocks ? mine[c] : -1;
+        fresh[j] = c < max_blocks && p >= 0 ? from[c] : -1;
+    }
+    ForkChange *list = ws.changes + u.at * kForkCols;
     int n = 0;
-    if (p != b) {
-        const int32_t *from = bt + (int64_t)(p < 0 ? 0 : p) * max_blocks;
-        const int32_t *mine = bt + (int64_t)b * max_blocks;
-        ForkEntry *list = lists + (int64_t)b * max_blocks;
-        for (int c0 = 0; c0 < max_blocks; c0 += kForkThreads) {
-            const int c = c0 + tid;
-            const bool in = c < max_blocks;
-            const int32_t old = in ? mine[c] : -1;
-            const int32_t fresh = in && p >= 0 ? from[c] : -1;
-            const bool differs = old != fresh;
-            if (differs) {
-                if (fresh >= n_blocks || old >= n_blocks) err |= MURMUR_DEVERR_BLOCK;
-                if (fresh >= 0 && fresh < n_blocks) add_ref(ref + fresh, 1);
-                if (old >= 0 && old < n_blocks) add_ref(ref + old, -1);
-            }
-            int total;
-            const int at = n + wg_exclusive_scan<kForkThreads>(differs, s_scan, tid, total);
-            if (differs) {
-                store_shared_word(&list[at].col, c);
-                store_shared_word(&list[at].fresh, fresh);
-                store_shared_word(&list[at].old, old);
-            }
-            n += total;
+    int32_t was[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        was[j] = 0;
+        if (old[j] == fresh[j]) continue;
+        if (fresh[j] >= n_blocks || old[j] >= n_blocks) err |= MURMUR_DEVERR_BLOCK;
+        if (fresh[j] >= 0 && fresh[j] < n_blocks) add_ref(ref + fresh[j], 1);
+        if (old[j] >= 0 && old[j] < n_blocks) {
+            const uint32_t place = (uint32_t)(u.b * max_blocks + u.col + 64 * j);
+            was[j] = __hip_atomic_fetch_add(ref + old[j], -1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_fetch_max(ws.first + old[j], (uint64_t)call << 32 | ((1u << 30) - place), __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_AGENT);
         }
     }
-    if (err) raise_device_error(err);
-    if (tid == 0) store_shared_word(count + b, n);
-    wait_vmem();
-    __syncthreads();
-    if (tid == 0) {
-        const int prev = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        s_last = prev == B - 1;
-        if (s_last) store_shared_word(ticket, 0);
-    }
-    __syncthreads();
-    if (!s_last) return;
-
-    // Entry e of the rows b0 .. b0 + kForkThreads - 1, of which s_first holds each row's first.
-    const auto entry_of = [&](int e, int b0, int &row, ForkEntry &x) {
-        int lo = 0, hi = kForkThreads;  // the last row whose first entry is at or before e
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (s_first[mid] <= e) lo = mid;
-            else hi = mid;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint64_t differs = __ballot(old[j] != fresh[j]);
+        if (old[j] != fresh[j]) {
+            const uint32_t place = (uint32_t)(u.b * max_blocks + u.col + 64 * j);
+            list[n + __popcll(differs & ((1ull << lane) - 1))] =
+                ForkChange{place | (was[j] == 1 ? kForkEmptied : 0u), fresh[j], old[j]};
         }
-        row = b0 + lo;
-        const ForkEntry *l = lists + (int64_t)row * max_blocks + (e - s_first[lo]);
-        x.col = load_shared_word(&l->col);
-        x.fresh = load_shared_word(&l->fresh);
-        x.old = load_shared_word(&l->old);
-    };
-    int32_t tp = *top;
-    tp = tp < 0 ? 0 : (tp > n_blocks ? n_blocks : tp);
-    err = 0;
-    for (int pass = 0; pass < 2; ++pass) {  // every place is offered before the first block is pushed
-        for (int b0 = 0; b0 < B; b0 += kForkThreads) {
-            int total;
-            const int c = b0 + tid < B ? load_shared_word(count + b0 + tid) : 0;
-            const int first = wg_exclusive_scan<kForkThreads>(c, s_scan, tid, total);
-            s_first[tid] = first;
-            __syncthreads();
-            for (int e0 = 0; e0 < total; e0 += kForkThreads) {
-                const int e = e0 + tid;
-                int row = 0;
-                ForkEntry x{0, -1, -1, 0};
-                if (e < total) entry_of(e, b0, row, x);
-                const int32_t at = row * max_blocks + x.col;
-                const bool block = x.old >= 0 && x.old < n_blocks;
-                if (pass == 0) {
-                    if (block) offer_place(ref + x.old, at);
-                    continue;
-                }
-                const bool mine = block && load_shared_word(ref + x.old) == place_key(at);
-                int pushed;
-                const int to = tp + wg_exclusive_scan<kForkThreads>(mine, s_scan, tid, pushed);
-                if (mine) {
-                    if (to < n_blocks) stack[to] = x.old;
-                    else err |= MURMUR_DEVERR_POOL;
-                    store_shared_word(ref + x.old, 0);
-                }
-                tp = tp + pushed < n_blocks ? tp + pushed : n_blocks;
-                if (e < total) bt[at] = x.fresh;
-            }
-            __syncthreads();  // s_first is read
-        }
-        wait_vmem();
-        __syncthreads();
+        n += __popcll(differs);
     }
-    if (tid == 0) *top = tp;
+    if (lane == 0) ws.counts[u.at] = n;
     if (err) raise_device_error(err);
 }
 
+__global__ __launch_bounds__(kForkThreads) void fork_apply_kernel(int32_t B, int32_t *__restrict__ bt,
+                                                                  int32_t max_blocks, const int32_t *__restrict__ ref,
+                                                                  const int32_t *__restrict__ top,
+                                                                  const ForkWorkspace ws) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    const ForkUnit u = fork_unit(B, max_blocks, __builtin_amdgcn_readfirstlane(tid >> 6), lane);
+    if (blockIdx.x == 0 && tid == 0) ws.head->top = *top;
+    if (u.at < 0) return;
+    const ForkChange *list = ws.changes + u.at * kForkCols;
+    const int n = ws.counts[u.at];
+    ForkChange c[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c[j] = list[lane + 64 * j];  // past the end: of an earlier call, not used
+    int32_t left[4];
+    uint64_t first[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        left[j] = 1;
+        first[j] = 0;
+        if (lane + 64 * j >= n) continue;
+        bt[c[j].place & ~kForkEmptied] = c[j].fresh;
+        if (c[j].place & kForkEmptied) {
+            left[j] = ref[c[j].old];
+            first[j] = ws.first[c[j].old];
+        }
+    }
+    // One atomic per word of bits: a wavefront's places are neighbours, and the atomics of one word, or of one
+    // count, queue (one per block: 59 us for 1024 rows, not 10).
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t place = (1u << 30) - (uint32_t)first[j];
+        if (left[j] == 0) ws.block_at[place] = c[j].old;  // else not marked, or named again by another row
+        uint64_t todo = __ballot(left[j] == 0);
+        while (todo) {
+            const uint32_t word = __builtin_amdgcn_readlane(place, (int)__ffsll((unsigned long long)todo) - 1) >> 5;
+            const bool here = left[j] == 0 && place >> 5 == word;
+            uint32_t bits = here ? 1u << (place & 31) : 0u;
+#pragma unroll
+            for (int x = 32; x >= 1; x /= 2) bits |= __shfl_xor(bits, x);
+            if (lane == 0) {
+                const uint32_t had = __hip_atomic_fetch_or(ws.bits + word, bits, __ATOMIC_RELAXED,
+                                                           __HIP_MEMORY_SCOPE_AGENT);
+                add_ref(ws.freed + word / (kForkPlaces / 32), __popc(bits & ~had));  // a block may be marked twice
+            }
+            todo &= ~__ballot(here);
+        }
+    }
+}
+
+// Workgroup w: the freed blocks of places [w, w + 1) * kForkPlaces.
+__global__ __launch_bounds__(kForkThreads) void fork_push_kernel(int64_t places, int32_t n_blocks,
+                                                                 int32_t *__restrict__ stack,
+                                                                 int32_t *__restrict__ top, const ForkWorkspace ws) {
+    constexpr int kWindow = 8192;  // pushes that LDS orders at a time
+    static_assert(kForkPlaces == 32 * kForkThreads, "a word of bits per thread");
+    __shared__ int32_t s_place[kWindow];
+    __shared__ int s_scan[kForkWaves];
+    const int tid = threadIdx.x;
+    const int64_t w = (int64_t)blockIdx.x * kForkThreads + tid, words = (places + 31) / 32;
+    const uint32_t bits = w < words ? ws.bits[w] : 0u;
+    int32_t tp = ws.head->top;
+    tp = tp < 0 ? 0 : (tp > n_blocks ? n_blocks : tp);
+    int before = 0, all = 0;
+    for (int g = tid; g < (int)gridDim.x; g += kForkThreads) {
+        const int f = ws.freed[g];
+        before += g < (int)blockIdx.x ? f : 0;
+        all += f;
+    }
+    wg_exclusive_scan<kForkThreads>(before, s_scan, tid, before);
+    int total;
+    const int mine = wg_exclusive_scan<kForkThreads>(__popc(bits), s_scan, tid, total);
+    if (blockIdx.x == 0) {
+        wg_exclusive_scan<kForkThreads>(all, s_scan, tid, all);
+        if (tid == 0) {
+            *top = tp + all < n_blocks ? tp + all : n_blocks;
+            ws.head->call += 1;
+            if (tp + all > n_blocks) raise_device_error(MURMUR_DEVERR_POOL);
+        }
+    }
+    if (bits) ws.bits[w] = 0;  // zero between calls
+    const int32_t *block_at = ws.block_at + (int64_t)blockIdx.x * kForkPlaces;
+    for (int r0 = 0; r0 < total; r0 += kWindow) {
+        int rank = mine - r0;
+        for (uint32_t x = bits; x; x &= x - 1, ++rank)
+            if (rank >= 0 && rank < kWindow) s_place[rank] = 32 * tid + __ffs(x) - 1;
+        __syncthreads();
+        for (int i = tid; i < min(total - r0, kWindow); i += kForkThreads) {
+            const int64_t to = (int64_t)tp + before + r0 + i;
+            if (to < n_blocks) stack[to] = block_at[s_place[i]];
+        }
+        __syncthreads();
+    }
+}
+
 // ---------------------------------------------------------------------------
-// step_shared: paged_step's two passes with counts.  Freeing takes three rounds
-// over the sequences (the counts, the places, the pushes).  Then each sequence
-// finds whether its current token's block is missing, its own, or held by others
-// too: of R holders, the k sequences of the batch that are about to write there
-// are ranked by (position, index), and the one of rank i copies if i < R - 1, as
-// if they went one after the other: the last one keeps the block when nobody
-// else holds it.  It is the one furthest ahead, so what it writes lies behind
-// every row that the others copy.
+// step_shared: paged_step's two passes with counts, by one workgroup.  Every entry
+// given up takes one off its block's count.  Where that empties a block, each
+// entry of it offers its place with an atomic minimum on the count itself (offers
+// are negative), and the first one pushes the block; steps in which nothing empties
+// (all but one in block-size many, and those of hypotheses that share what they
+// give up) pass over that.  Then each sequence finds whether its current token's
+// block is missing, its own, or held by others too: of R holders, the k sequences
+// of the batch that are about to write there are ranked by (position, index), and
+// the one of rank i copies if i < R - 1, as if they went one after the other: the
+// last one keeps the block when nobody else holds it.  It is the one furthest
+// ahead, so what it writes lies behind every row that the others copy.
+// Round trips to memory bound it, so a sequence's layout, policy and current block
+// stay in registers where a thread has only one: 4.8 us for 4 sequences,
+// 17.7 for 96 (20.9 and 26.1 with every pass reading them again).
 // ---------------------------------------------------------------------------
+static __device__ __forceinline__ int32_t place_key(int32_t at) { return (int32_t)(0x80000000u + (uint32_t)at); }
 static __device__ __forceinline__ int64_t seq_position(const murmur_seg &s) {  // of the current token
     return (int64_t)s.prompt_pre + s.speech_len + s.prompt_mid + s.out_len - 1;
 }
 
-__global__ __launch_bounds__(256) void step_shared_kernel(const murmur_seg *__restrict__ seg,
-                                                          const murmur_policy *__restrict__ pol, int32_t pol_per_seq,
-                                                          int32_t B, int32_t *bt, int32_t max_blocks, int32_t log2_bs,
-                                                          int32_t *ref, int32_t n_blocks, int32_t *stack, int32_t *top,
-                                                          int32_t full_scan, int32_t *copied) {
-    __shared__ int s_scan[4];
-    __shared__ int2 s_writer[256];
+// What step_shared needs of a sequence: its freeable columns and where its token goes.
+struct StepSeq {
+    PagedSeq q;
+    int32_t pos;  // valid sequences: of the current token
+    int32_t x;    // the block there (-1: none, or past the table)
+};
+
+template <int kThreads>
+__global__ __launch_bounds__(kThreads) void step_shared_kernel(const murmur_seg *__restrict__ seg,
+                                                               const murmur_policy *__restrict__ pol,
+                                                               int32_t pol_per_seq, int32_t B, int32_t *bt,
+                                                               int32_t max_blocks, int32_t log2_bs, int32_t *ref,
+                                                               int32_t n_blocks, int32_t *stack, int32_t *top,
+                                                               int32_t full_scan, int32_t *copied) {
+    __shared__ int s_scan[kThreads / 64];
+    __shared__ int2 s_writer[kThreads];
     constexpr int32_t kTakeBlock = -3;
     const int tid = threadIdx.x;
+    const bool one_each = B <= kThreads;
     int32_t tp = *top;
     tp = tp < 0 ? 0 : (tp > n_blocks ? n_blocks : tp);
     int err = 0;
+    const auto load_seq = [&](int b) {
+        StepSeq s{paged_seq(seg, pol, pol_per_seq, b, B, max_blocks, log2_bs, full_scan, err), 0, -1};
+        if (s.q.valid) {
+            s.pos = (int32_t)seq_position(seg[b]);
+            if (s.q.cur < max_blocks) s.x = bt[(int64_t)b * max_blocks + s.q.cur];
+        }
+        return s;
+    };
+    const StepSeq mine = load_seq(tid);
+    const auto seq_of = [&](int b) { return one_each ? mine : load_seq(b); };
     // every entry of sequence b to give up, with its place
-    const auto each_freed = [&](int b, int &e, auto f) {
-        const PagedSeq q = paged_seq(seg, pol, pol_per_seq, b, B, max_blocks, log2_bs, full_scan, e);
-        int32_t *row = bt + (int64_t)(q.valid ? b : 0) * max_blocks;
+    const auto each_freed = [&](int b, const StepSeq &s, auto f) {
+        int32_t *row = bt + (int64_t)(s.q.valid ? b : 0) * max_blocks;
 #pragma unroll
         for (int k = 0; k < 2; ++k)
-            for (int32_t blk = q.lo[k]; blk < q.hi[k]; ++blk) {
+            for (int32_t blk = s.q.lo[k]; blk < s.q.hi[k]; ++blk) {
                 const int32_t phys = row[blk];
                 if (phys >= 0) f(row + blk, phys, b * max_blocks + blk);
             }
     };
-    // where a sequence writes its token: its position, that position's column and the block there
-    struct Writer {
-        bool valid;
-        int32_t blk, x;
-        int64_t pos;
-    };
-    const auto writer_of = [&](int b, int &e) {
-        const PagedSeq q = paged_seq(seg, pol, pol_per_seq, b, B, max_blocks, log2_bs, 1, e);
-        Writer w{q.valid, q.cur, -1, 0};
-        if (q.valid) {
-            w.pos = seq_position(seg[b]);
-            if (q.cur < max_blocks) w.x = bt[(int64_t)b * max_blocks + q.cur];
+    int emptied = 0;
+    for (int b = tid; b < B; b += kThreads)
+        each_freed(b, seq_of(b), [&](int32_t *, int32_t phys, int32_t) {
+            if (phys < n_blocks)
+                emptied |= __hip_atomic_fetch_add(ref + phys, -1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 1;
+            else
+                err |= MURMUR_DEVERR_BLOCK;
+        });
+    emptied = __syncthreads_or(emptied);
+    if (emptied) {
+        for (int b = tid; b < B; b += kThreads)
+            each_freed(b, seq_of(b), [&](int32_t *, int32_t phys, int32_t at) {
+                if (phys < n_blocks && load_shared_word(ref + phys) <= 0)
+                    __hip_atomic_fetch_min(ref + phys, place_key(at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            });
+        wait_vmem();
+        __syncthreads();
+    }
+    for (int b0 = 0; b0 < B; b0 += kThreads) {
+        const StepSeq s = seq_of(b0 + tid);
+        int to = tp;
+        if (emptied) {
+            int n = 0, pushed;
+            each_freed(b0 + tid, s, [&](int32_t *, int32_t phys, int32_t at) {
+                n += phys < n_blocks && load_shared_word(ref + phys) == place_key(at);
+            });
+            to = tp + wg_exclusive_scan<kThreads>(n, s_scan, tid, pushed);
+            tp = tp + pushed < n_blocks ? tp + pushed : n_blocks;
         }
-        return w;
-    };
-    int ignore = 0;
-    for (int b = tid; b < B; b += 256)
-        each_freed(b, err, [&](int32_t *, int32_t phys, int32_t) {
-            if (phys < n_blocks) add_ref(ref + phys, -1);
-            else err |= MURMUR_DEVERR_BLOCK;
-        });
-    wait_vmem();
-    __syncthreads();
-    for (int b = tid; b < B; b += 256)
-        each_freed(b, ignore, [&](int32_t *, int32_t phys, int32_t at) {
-            if (phys < n_blocks) offer_place(ref + phys, at);
-        });
-    wait_vmem();
-    __syncthreads();
-    for (int b0 = 0; b0 < B; b0 += 256) {
-        int n = 0, pushed;
-        each_freed(b0 + tid, ignore, [&](int32_t *, int32_t phys, int32_t at) {
-            n += phys < n_blocks && load_shared_word(ref + phys) == place_key(at);
-        });
-        int to = tp + wg_exclusive_scan<256>(n, s_scan, tid, pushed);
-        each_freed(b0 + tid, ignore, [&](int32_t *entry, int32_t phys, int32_t at) {
-            if (phys < n_blocks && load_shared_word(ref + phys) == place_key(at)) {
+        each_freed(b0 + tid, s, [&](int32_t *entry, int32_t phys, int32_t at) {
+            if (emptied && phys < n_blocks && load_shared_word(ref + phys) == place_key(at)) {
                 if (to < n_blocks) stack[to] = phys;
                 else err |= MURMUR_DEVERR_POOL;
                 ++to;
@@ -265,59 +336,67 @@ __global__ __launch_bounds__(256) void step_shared_kernel(const murmur_seg *__re
             }
             *entry = -1;
         });
-        tp = tp + pushed < n_blocks ? tp + pushed : n_blocks;
     }
-    wait_vmem();
-    __syncthreads();
+    if (emptied) {
+        wait_vmem();
+        __syncthreads();  // the stack and the counts before the pops
+    }
     // What each sequence needs, before any table entry or count changes: kTakeBlock, -1 for nothing, -2 if it is not
     // valid, else a copy of the block named.
-    for (int b0 = 0; b0 < B; b0 += 256) {
-        const Writer w = writer_of(b0 + tid, err);
-        int32_t what = w.valid ? -1 : -2;
+    const auto need_of = [&](int b0) {
+        const StepSeq s = seq_of(b0 + tid);
+        int32_t what = s.q.valid ? -1 : -2;
         int holders = 0;
-        if (w.valid && w.blk >= max_blocks) {
+        if (s.q.valid && s.q.cur >= max_blocks) {
             err |= MURMUR_DEVERR_BLOCK;
-        } else if (w.valid && w.x < 0) {
+        } else if (s.q.valid && s.x < 0) {
             what = kTakeBlock;
-        } else if (w.valid && w.x >= n_blocks) {
+        } else if (s.q.valid && s.x >= n_blocks) {
             err |= MURMUR_DEVERR_BLOCK;
-        } else if (w.valid) {
-            holders = load_shared_word(ref + w.x);
+        } else if (s.q.valid) {
+            holders = load_shared_word(ref + s.x);
         }
+        if (!__syncthreads_or(holders > 1)) return what;
         int before = 0;
-        for (int o0 = 0; o0 < B; o0 += 256) {  // all sequences that write to a block, 256 at a time
-            const Writer o = writer_of(o0 + tid, ignore);
-            s_writer[tid] = o.valid && o.blk < max_blocks ? int2{o.x, (int)o.pos} : int2{-1, 0};
+        for (int o0 = 0; o0 < B; o0 += kThreads) {  // all sequences that write to a block, kThreads at a time
+            const StepSeq o = seq_of(o0 + tid);
+            s_writer[tid] = o.q.valid && o.q.cur < max_blocks ? int2{o.x, o.pos} : int2{-1, 0};
             __syncthreads();
             if (holders > 1)
-                for (int i = 0; i < 256; ++i) {
+                for (int i = 0; i < min(kThreads, B - o0); ++i) {
                     const int2 y = s_writer[i];
-                    before += y.x == w.x && (y.y >> log2_bs) == w.blk &&
-                              (y.y < (int)w.pos || (y.y == (int)w.pos && o0 + i < b0 + tid));
+                    before += y.x == s.x && (y.y >> log2_bs) == s.q.cur &&
+                              (y.y < s.pos || (y.y == s.pos && o0 + i < b0 + tid));
                 }
             __syncthreads();
         }
-        if (holders > 1 && before < holders - 1) what = w.x;
-        if (b0 + tid < B) copied[b0 + tid] = what;
+        return holders > 1 && before < holders - 1 ? s.x : what;
+    };
+    int32_t need_mine = 0;
+    for (int b0 = 0; b0 < B; b0 += kThreads) {
+        need_mine = need_of(b0);
+        if (!one_each && b0 + tid < B) copied[b0 + tid] = need_mine;
     }
-    __syncthreads();
-    for (int b0 = 0; b0 < B; b0 += 256) {
+    __syncthreads();  // every count is read
+    for (int b0 = 0; b0 < B; b0 += kThreads) {
         const int b = b0 + tid;
-        const int32_t what = b < B ? copied[b] : -1;
+        const int32_t what = b >= B ? -2 : (one_each ? need_mine : copied[b]);
         const bool need = what >= 0 || what == kTakeBlock;
         int taken;
-        const int off = wg_exclusive_scan<256>(need, s_scan, tid, taken);
+        const int off = wg_exclusive_scan<kThreads>(need, s_scan, tid, taken);
+        int32_t from_block = what;
         if (need) {
-            const int64_t blk = seq_position(seg[b]) >> log2_bs;
+            const int32_t cur = one_each ? mine.q.cur : (int32_t)(seq_position(seg[b]) >> log2_bs);
             const int from = tp - 1 - off;
             const int32_t got = from >= 0 ? stack[from] : -1;
             const bool good = got >= 0 && got < n_blocks;
             if (good) store_shared_word(ref + got, 1);
             else err |= MURMUR_DEVERR_POOL;
             if (what >= 0) add_ref(ref + what, -1);
-            bt[(int64_t)b * max_blocks + blk] = good ? got : -1;
-            copied[b] = good ? (what >= 0 ? what : -1) : -2;
+            bt[(int64_t)b * max_blocks + cur] = good ? got : -1;
+            from_block = good ? (what >= 0 ? what : -1) : -2;
         }
+        if (b < B) copied[b] = from_block;
         tp = tp - taken > 0 ? tp - taken : 0;
     }
     if (tid == 0) *top = tp;
@@ -364,35 +443,57 @@ __global__ __launch_bounds__(256) void append_shared_kernel(const murmur_seg *__
 // written.  One workgroup ranks them with scans over the counts; then the chip copies the blocks and renames the table's entries.
 // ---------------------------------------------------------------------------
 constexpr int kCompactThreads = 1024;
+constexpr int kCompactEach = 4;  // consecutive blocks of a thread
 
 __global__ __launch_bounds__(kCompactThreads) void compact_plan_kernel(int32_t *__restrict__ ref, int32_t n_blocks,
                                                                        int32_t *__restrict__ stack,
                                                                        int32_t *__restrict__ top, int32_t *map,
                                                                        int32_t *ws) {
     __shared__ int s_scan[kCompactThreads / 64];
+    constexpr int kRound = kCompactThreads * kCompactEach;
     const int tid = threadIdx.x;
-    int32_t *src = ws + kForkHeader, *dst = src + n_blocks / 2;
+    int32_t *src = ws + 1, *dst = src + n_blocks / 2;
+    const auto load = [&](int i0, int32_t (&r)[kCompactEach]) {
+#pragma unroll
+        for (int j = 0; j < kCompactEach; ++j) r[j] = i0 + j < n_blocks ? ref[i0 + j] : 0;
+    };
+    int32_t r[kCompactEach];
     int used = 0;
-    for (int i0 = 0; i0 < n_blocks; i0 += kCompactThreads) {
-        const int i = i0 + tid;
-        int total;
-        wg_exclusive_scan<kCompactThreads>(i < n_blocks && ref[i] > 0, s_scan, tid, total);
+    for (int i0 = 0; i0 < n_blocks; i0 += kRound) {
+        load(i0 + tid * kCompactEach, r);
+        int n = 0, total;
+#pragma unroll
+        for (int j = 0; j < kCompactEach; ++j) n += r[j] > 0;
+        wg_exclusive_scan<kCompactThreads>(n, s_scan, tid, total);
         used += total;
     }
     int moves = 0, holes = 0;
-    for (int i0 = 0; i0 < n_blocks; i0 += kCompactThreads) {
-        const int i = i0 + tid;
-        const bool in = i < n_blocks, live = in && ref[i] > 0;
-        const bool mover = live && i >= used, hole = in && !live && i < used;
-        int nm, nh;
-        const int am = moves + wg_exclusive_scan<kCompactThreads>(mover, s_scan, tid, nm);
-        const int ah = holes + wg_exclusive_scan<kCompactThreads>(hole, s_scan, tid, nh);
-        if (mover) src[am] = i;
-        if (hole) dst[ah] = i;
-        if (in) map[i] = live && !mover ? i : -1;
-        moves += nm;
-        holes += nh;
-        if (in && i < n_blocks - used) stack[i] = n_blocks - 1 - i;
+    for (int i0 = 0; i0 < n_blocks; i0 += kRound) {
+        const int first = i0 + tid * kCompactEach;
+        if (n_blocks > kRound) load(first, r);  // one round: still in registers
+        // movers and holes in one scan: at most kRound each, 16 bits apart
+        static_assert(kRound < 1 << 16, "two counts in one word");
+        int n = 0, total;
+#pragma unroll
+        for (int j = 0; j < kCompactEach; ++j) {
+            const int i = first + j;
+            n += i < n_blocks && i >= used && r[j] > 0 ? 1 : 0;
+            n += i < used && r[j] <= 0 ? 1 << 16 : 0;
+        }
+        const int at = wg_exclusive_scan<kCompactThreads>(n, s_scan, tid, total);
+        int am = moves + (at & 0xffff), ah = holes + (at >> 16);
+#pragma unroll
+        for (int j = 0; j < kCompactEach; ++j) {
+            const int i = first + j;
+            if (i >= n_blocks) break;
+            const bool live = r[j] > 0;
+            if (live && i >= used) src[am++] = i;
+            if (!live && i < used) dst[ah++] = i;
+            map[i] = live && i < used ? i : -1;
+            if (i < n_blocks - used) stack[i] = n_blocks - 1 - i;
+        }
+        moves += total & 0xffff;
+        holes += total >> 16;
     }
     __syncthreads();
     for (int j = tid; j < moves; j += kCompactThreads) {
@@ -402,7 +503,7 @@ __global__ __launch_bounds__(kCompactThreads) void compact_plan_kernel(int32_t *
         ref[s] = 0;
     }
     if (tid == 0) {
-        ws[1] = moves;  // ws[0] is the ticket of a fork
+        ws[0] = moves;
         *top = n_blocks - used;
     }
 }
@@ -430,8 +531,8 @@ __global__ __launch_bounds__(256) void compact_move_kernel(int32_t *__restrict__
         if (err) raise_device_error(err);
         return;
     }
-    const int32_t *src = ws + kForkHeader, *dst = src + n_blocks / 2;
-    const int64_t items = (int64_t)ws[1] * NL * 2;
+    const int32_t *src = ws + 1, *dst = src + n_blocks / 2;
+    const int64_t items = (int64_t)ws[0] * NL * 2;
     const int units = (Hkv * 16) << log2_bs;
     for (int64_t it = (int64_t)(blockIdx.y - 1) * gridDim.x + blockIdx.x; it < items;
          it += (int64_t)(gridDim.y - 1) * gridDim.x) {
@@ -449,9 +550,20 @@ __global__ __launch_bounds__(256) void compact_move_kernel(int32_t *__restrict__
 // ---- launchers ----
 
 int launch_paged_fork(const int32_t *parent, int32_t B, int32_t *bt, int32_t max_blocks, int32_t *ref,
-                      int32_t n_blocks, int32_t *stack, int32_t *top, int32_t *ws, murmur_stream_t stream) {
-    hipLaunchKernelGGL(fork_kernel, dim3((unsigned)B), dim3(kForkThreads), 0, (hipStream_t)stream, parent, B, bt,
-                       max_blocks, ref, n_blocks, stack, top, ws);
+                      int32_t n_blocks, int32_t *stack, int32_t *top, const ForkWorkspace &ws,
+                      murmur_stream_t stream) {
+    const int64_t units = (int64_t)B * ((max_blocks + kForkCols - 1) / kForkCols);
+    const dim3 grid((unsigned)((units + kForkWaves - 1) / kForkWaves)), threads(kForkThreads);
+    hipLaunchKernelGGL(fork_compare_kernel, grid, threads, 0, (hipStream_t)stream, parent, B, bt, max_blocks, ref,
+                       n_blocks, ws);
+    int e = (int)hipGetLastError();
+    if (e != 0) return e;
+    hipLaunchKernelGGL(fork_apply_kernel, grid, threads, 0, (hipStream_t)stream, B, bt, max_blocks, ref, top, ws);
+    e = (int)hipGetLastError();
+    if (e != 0) return e;
+    const int64_t places = (int64_t)B * max_blocks;
+    hipLaunchKernelGGL(fork_push_kernel, dim3((unsigned)((places - 1) / kForkPlaces + 1)), threads, 0,
+                       (hipStream_t)stream, places, n_blocks, stack, top, ws);
     return (int)hipGetLastError();
 }
 
@@ -459,8 +571,13 @@ int launch_paged_step_shared(const murmur_seg *seg, const murmur_policy *pol, in
                              int32_t *bt, int32_t max_blocks, int32_t log2_bs, int32_t *ref, int32_t n_blocks,
                              int32_t *stack, int32_t *top, int32_t full_scan, int32_t *copied,
                              murmur_stream_t stream) {
-    hipLaunchKernelGGL(step_shared_kernel, dim3(1), dim3(256), 0, (hipStream_t)stream, seg, pol, pol_per_seq, B, bt,
-                       max_blocks, log2_bs, ref, n_blocks, stack, top, full_scan, copied);
+    // a thread per sequence up to 1024; a small batch takes fewer wavefronts through the barriers
+    if (B <= 256)
+        hipLaunchKernelGGL(step_shared_kernel<256>, dim3(1), dim3(256), 0, (hipStream_t)stream, seg, pol, pol_per_seq,
+                           B, bt, max_blocks, log2_bs, ref, n_blocks, stack, top, full_scan, copied);
+    else
+        hipLaunchKernelGGL(step_shared_kernel<1024>, dim3(1), dim3(1024), 0, (hipStream_t)stream, seg, pol,
+                           pol_per_seq, B, bt, max_blocks, log2_bs, ref, n_blocks, stack, top, full_scan, copied);
     return (int)hipGetLastError();
 }
 

@@ -57,16 +57,40 @@ int check_pool(const murmur_kv *pool, int32_t Hkv, int32_t n_blocks, int32_t blo
     return MURMUR_OK;
 }
 
-size_t fork_words(int32_t B, int32_t max_blocks) {
-    return kForkHeader + round_up((size_t)B, 64) + sizeof(ForkEntry) / 4 * (size_t)B * (size_t)max_blocks;
+// The parts of a workspace at `ws`, and the bytes they take.
+struct PagesWorkspace {
+    ForkWorkspace fork;
+    int32_t *moves;
+    size_t bytes;
+};
+PagesWorkspace pages_workspace(void *ws, int32_t B, int32_t max_blocks, int32_t n_blocks) {
+    PagesWorkspace p{};
+    const size_t entries = (size_t)B * (size_t)max_blocks;
+    const size_t lists = (size_t)B * (((size_t)max_blocks + kForkCols - 1) / kForkCols);
+    size_t at = 0;
+    const auto take = [&](size_t bytes) {
+        void *q = (void *)((uintptr_t)ws + at);
+        at += round_up(bytes, 256);
+        return q;
+    };
+    p.fork.head = (ForkHead *)take(sizeof(ForkHead));
+    p.fork.first = (uint64_t *)take(sizeof(uint64_t) * (size_t)n_blocks);
+    p.fork.bits = (uint32_t *)take((entries + 31) / 32 * 4);
+    p.moves = (int32_t *)take(0);
+    const size_t kept = at;
+    p.fork.changes = (ForkChange *)take(sizeof(ForkChange) * lists * kForkCols);
+    p.fork.counts = (int32_t *)take(sizeof(int32_t) * lists);
+    p.fork.freed = (int32_t *)take(sizeof(int32_t) * ((entries - 1) / kForkPlaces + 1));
+    p.fork.block_at = (int32_t *)take(sizeof(int32_t) * entries);
+    p.bytes = std::max(at, kept + round_up(sizeof(int32_t) * (1 + 2 * (size_t)(n_blocks / 2)), 256));
+    return p;
 }
-size_t compact_words(int32_t n_blocks) { return kForkHeader + 2 * (size_t)(n_blocks / 2); }
 
-int check_workspace(const void *ws, size_t ws_bytes, size_t words) {
+int check_workspace(const void *ws, size_t ws_bytes, size_t needed) {
     if (!ws) return fail(MURMUR_EINVAL, "ws_dev must not be NULL");
     if (!aligned(ws, 256)) return fail(MURMUR_EINVAL, "ws_dev must be 256-byte aligned");
-    if (ws_bytes < 4 * words)
-        return fail(MURMUR_ENOSPACE, "workspace of %zu bytes is too small (%zu needed)", ws_bytes, 4 * words);
+    if (ws_bytes < needed)
+        return fail(MURMUR_ENOSPACE, "workspace of %zu bytes is too small (%zu needed)", ws_bytes, needed);
     return MURMUR_OK;
 }
 
@@ -126,7 +150,7 @@ MURMUR_EXPORT int murmur_paged_workspace(int32_t B, int32_t max_blocks, int32_t 
         (int64_t)B * max_blocks > (1 << 30))
         return fail(MURMUR_EINVAL, "B must be in [1, %d], max_blocks >= 1, B * max_blocks and n_blocks at most 2^30",
                     kMaxRows);
-    *bytes = round_up(4 * std::max(fork_words(B, max_blocks), compact_words(n_blocks)), 256);
+    *bytes = pages_workspace(nullptr, B, max_blocks, n_blocks).bytes;
     return ok();
 }
 
@@ -137,10 +161,11 @@ MURMUR_EXPORT int murmur_paged_fork(const int32_t *parent_dev, int32_t B, int32_
     if (!parent_dev) return fail(MURMUR_EINVAL, "parent_dev must not be NULL");
     if (!aligned(parent_dev, 4)) return fail(MURMUR_EINVAL, "device pointers must be 4-byte aligned");
     int rc = check_pages(B, block_table_dev, max_blocks, ref_dev, n_blocks, free_stack_dev, free_top_dev, capacity);
-    if (rc == MURMUR_OK) rc = check_workspace(ws_dev, ws_bytes, fork_words(B, max_blocks));
+    if (rc == MURMUR_OK) rc = check_workspace(ws_dev, ws_bytes, pages_workspace(nullptr, B, max_blocks, n_blocks).bytes);
     if (rc != MURMUR_OK) return rc;
+    const ForkWorkspace ws = pages_workspace(ws_dev, B, max_blocks, n_blocks).fork;
     const int e = launch_paged_fork(parent_dev, B, block_table_dev, max_blocks, ref_dev, n_blocks, free_stack_dev,
-                                    free_top_dev, (int32_t *)ws_dev, stream);
+                                    free_top_dev, ws, stream);
     if (e != 0) return fail(MURMUR_EHIP, "paged_fork launch failed: %s", hip_error_text(e));
     return ok();
 }
@@ -194,10 +219,11 @@ MURMUR_EXPORT int murmur_paged_compact(int32_t B, int32_t *block_table_dev, int3
     int rc = check_pages(B, block_table_dev, max_blocks, ref_dev, n_blocks, free_stack_dev, free_top_dev, capacity);
     if (rc == MURMUR_OK) rc = check_block_size(block_size, log2_bs);
     if (rc == MURMUR_OK && pool) rc = check_pool(pool, Hkv, n_blocks, block_size);
-    if (rc == MURMUR_OK) rc = check_workspace(ws_dev, ws_bytes, compact_words(n_blocks));
+    if (rc == MURMUR_OK) rc = check_workspace(ws_dev, ws_bytes, pages_workspace(nullptr, B, max_blocks, n_blocks).bytes);
     if (rc != MURMUR_OK) return rc;
     const int e = launch_paged_compact(B, block_table_dev, max_blocks, log2_bs, ref_dev, n_blocks, free_stack_dev,
-                                       free_top_dev, map_dev, pool, Hkv, (int32_t *)ws_dev, stream);
+                                       free_top_dev, map_dev, pool, Hkv,
+                                       pages_workspace(ws_dev, B, max_blocks, n_blocks).moves, stream);
     if (e != 0) return fail(MURMUR_EHIP, "paged_compact launch failed: %s", hip_error_text(e));
     return ok();
 }

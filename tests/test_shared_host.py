@@ -100,13 +100,13 @@ SIZE_FAULTS = [("max_keep", 0, E, ">= 1"), ("B", 0, E, ">= 1"), ("n_groups", 0, 
                ("idx_dev", None, E, "idx_dev and ranges_dev"), ("idx_dev", FAKE + 2, E, "aligned")]
 FAULTS = {
     "murmur_paged_fork": PAGE_FAULTS + WS_FAULTS + [("parent_dev", None, E, "NULL"), ("parent_dev", FAKE + 2, E, "aligned"),
-                                                    ("ws_bytes", 4 * (64 + 64 + 4 * 12 * 64) - 1, S, "too small")],
+                                                    ("ws_bytes", M.murmur_paged_workspace(12, 64, 256) - 1, S, "too small")],
     "murmur_paged_step_shared": PAGE_FAULTS + POOL_FAULTS + [
         ("seg_dev", None, E, "NULL"), ("pol_dev", None, E, "NULL"), ("copied_dev", None, E, "NULL"),
         ("copied_dev", FAKE + 2, E, "aligned"), ("pol_per_seq", 2, E, "pol_per_seq"), ("k_new_dev", None, E, "k_new_dev"),
         ("v_new_dev", FAKE + 8, E, "16-byte")],
     "murmur_paged_compact": PAGE_FAULTS + POOL_FAULTS + WS_FAULTS + [
-        ("map_dev", None, E, "NULL"), ("map_dev", FAKE + 2, E, "aligned"), ("ws_bytes", 4 * (64 + 256) - 1, S, "too small")],
+        ("map_dev", None, E, "NULL"), ("map_dev", FAKE + 2, E, "aligned"), ("ws_bytes", M.murmur_paged_workspace(12, 64, 256) - 1, S, "too small")],
     "murmur_shared_plan": SIZE_FAULTS + [
         ("count_dev", None, E, "count_dev"), ("ranges_dev", FAKE, E, "find_shared"), ("group_dev", None, E, "NULL"),
         ("shared_dev", None, E, "NULL"), ("group_dev", FAKE + 2, E, "aligned"), ("shared_dev", FAKE + 2, E, "aligned"),
@@ -135,8 +135,8 @@ def test_optional_arguments():
 
 
 def test_sizes():
-    assert M.murmur_paged_workspace(12, 64, 256) >= 4 * (64 + 64 + 4 * 12 * 64)
-    assert M.murmur_paged_workspace(1, 1, 1 << 20) >= 4 * (64 + (1 << 20))
+    assert M.murmur_paged_workspace(12, 64, 256) >= 8 * 256 + 16 * 12 * 64
+    assert M.murmur_paged_workspace(1, 1, 1 << 20) >= 12 * (1 << 20)
     for bad in ((0, 1, 1), (65536, 1, 1), (1, 0, 1), (1, 1, 0), (1024, 1 << 21, 1)):
         with pytest.raises(M.MurmurError):
             M.murmur_paged_workspace(*bad)
