@@ -112,6 +112,7 @@ int murmur_paged_compact(int32_t B, int32_t *block_table_dev, int32_t max_blocks
  * call of these sizes needs: a plan (16-byte aligned), which murmur_shared_plan
  * writes and murmur_decode_attn_shared reads, and a workspace (256-byte aligned)
  * for the partial sums.  Neither needs to be initialised; a larger buffer is fine.
+ * At most 4096 sequences (MURMUR_EUNSUPPORTED beyond) and as many groups.
  * Calls that run at the same time need workspaces of their own, and may share a
  * plan. */
 int murmur_decode_attn_shared_workspace(int32_t n_layers, int32_t B, int32_t Hq, int32_t Hkv, int32_t max_keep,

@@ -222,38 +222,41 @@ int launch_paged_compact(int32_t B, int32_t *bt, int32_t max_blocks, int32_t log
                          murmur_stream_t stream);
 
 // The schedule of an attention over shared prefixes, written by
-// murmur_shared_plan into the caller's plan buffer (int32 words, in this order):
+// murmur_shared_plan into the caller's plan buffer (in this order):
 //   PlanHeader;
 //   PlanSeq [B]: where a sequence's partials lie;
-//   PlanItem [n_wg]: prefix work, one workgroup each;
-//   PlanChunk [kSharedWaves * n_wg]: remainders, one wavefront each, the
-//     kSharedWaves of a workgroup side by side;
+//   PlanItem [n_wg]: what a workgroup does;
+//   PlanChunk [n_wg][kSharedWaves]: the wavefronts' parts where it does remainders;
 //   first differing rank [B][n_scan] of each sequence's list against its group's
 //     first one, per kScanLen entries.
-// Workgroups 0 .. n_items-1 of a (layer, KV head) take the items and the next
-// n_rest the chunks.  n_wg bounds their number whatever the lists hold (see
+// n_wg bounds the workgroups of a (layer, KV head) whatever the lists hold (see
 // shared_caps).
 constexpr int kSharedWaves = 8;
-constexpr int kSharedRows = 64;     // query rows of one prefix item: four MFMA row tiles
-constexpr int kSharedMaxPasses = 16;  // passes of kWaveTile positions per wavefront, at most
+constexpr int kSharedRows = 64;       // query rows of one prefix item: four MFMA row tiles
+constexpr int kSharedMaxSeqs = 4096;  // sequences of a batch (the planner's LDS)
+// A cut of the work at level j = 1 .. kSharedLevels gives a wavefront of a prefix
+// item up to j passes of kWaveTile positions and one of a rest up to j + j / 2 (it
+// holds half the row tiles or fewer).
+constexpr int kSharedLevels = 16;
 constexpr int kScanLen = 4096;
 constexpr int32_t kPlanMagic = 0x6d75726d;
 struct PlanHeader {
-    int32_t magic, n_items, n_rest, bad;  // bad: the groups are not in order; every output is NaN
+    int32_t magic, n_work, bad, unused0;  // bad: the groups are not in order; every output is NaN
     int32_t B, max_keep, n_layers, Hq, Hkv, n_groups;  // what the plan was made for
-    int32_t rows, passes, unused[4];  // partial rows per (layer, KV head); passes per wavefront
+    int32_t rows, level, unused[4];       // partial rows per (layer, KV head)
 };
 struct PlanSeq {
     int32_t state;  // 0: not in any group (outputs untouched), 1: computed, 2: invalid count (NaN outputs)
     int32_t pre_row, pre_stride, n_pre;  // partials over the prefix: rows pre_row + i * pre_stride + head
     int32_t rest_row, n_rest;            // over the rest: rows rest_row + i * G + head
-    int32_t first_chunk, common;         // common: positions that the group shares
+    int32_t unused[2];
 };
 struct PlanItem {
-    int32_t seq0, n_seq, list, r0, r1, row, unused[2];  // list: the sequence whose list is read; row: partial row
+    int32_t seq0, n_seq, list, r0, r1, row, unused[2];  // n_seq 0: remainders; list: the sequence whose list is read;
+                                                        // row: partial row
 };
 struct PlanChunk {
-    int32_t seq, r0, r1, row;
+    int32_t seq, r0, r1, row;  // seq -1: none
 };
 struct SharedCaps {
     int32_t per_round;  // workgroups per (layer, KV head) of one dispatch round
@@ -284,6 +287,7 @@ struct SharedAttnLaunch {
     float *part_ml;  // [layers * KV heads][rows][2]  (running max in log2 units, sum)
     int64_t rows_cap;
     int32_t max_len, max_keep, B, Hq, Hkv, G, NL, n_groups, n_wg, out_f32;
+    uint32_t magic_g;  // magic16(G): row / G for rows below 2^16
     float scale_log2;
 };
 int launch_decode_attn_shared(const SharedAttnLaunch &a, murmur_stream_t stream);

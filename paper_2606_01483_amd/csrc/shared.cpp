@@ -11,7 +11,7 @@
 namespace murmur {
 namespace {
 
-constexpr int kMaxRows = 65535;  // sequences of a call
+constexpr int kMaxRows = 65535;  // rows of a block table
 
 // The bookkeeping arguments that every call on shared pages takes.
 int check_pages(int32_t B, const int32_t *bt, int32_t max_blocks, const int32_t *ref, int32_t n_blocks,
@@ -97,13 +97,15 @@ int check_workspace(const void *ws, size_t ws_bytes, size_t needed) {
 int check_shared_sizes(int32_t n_layers, int32_t B, int32_t Hq, int32_t Hkv, int32_t max_keep, int32_t n_groups) {
     if (n_layers < 1 || B < 1 || Hq < 1 || Hkv < 1 || max_keep < 1)
         return fail(MURMUR_EINVAL, "n_layers, B, Hq, Hkv and max_keep must be >= 1");
-    if (n_groups < 1 || n_groups > kMaxRows)
-        return fail(MURMUR_EINVAL, "n_groups must be in [1, %d] (got %d)", kMaxRows, n_groups);
+    if (B > kSharedMaxSeqs)
+        return fail(MURMUR_EUNSUPPORTED, "%d sequences exceed %d", B, kSharedMaxSeqs);
+    if (n_groups < 1 || n_groups > kSharedMaxSeqs)
+        return fail(MURMUR_EINVAL, "n_groups must be in [1, %d] (got %d)", kSharedMaxSeqs, n_groups);
     if (Hq % Hkv != 0) return fail(MURMUR_EINVAL, "Hq (%d) must be a multiple of Hkv (%d)", Hq, Hkv);
     if (Hq / Hkv > kMaxGroup)
         return fail(MURMUR_EUNSUPPORTED, "query heads per KV head %d exceeds %d", Hq / Hkv, kMaxGroup);
     if (max_keep > kMaxKeep) return fail(MURMUR_EUNSUPPORTED, "max_keep %d exceeds %d", max_keep, kMaxKeep);
-    if (B > kMaxRows || (int64_t)n_layers * Hkv > 65535 || (int64_t)n_layers * B * Hq > 0x7fffffffLL)
+    if ((int64_t)n_layers * Hkv > 65535 || (int64_t)n_layers * B * Hq > 0x7fffffffLL)
         return fail(MURMUR_EINVAL, "problem too large for one launch (n_layers * Hkv = %lld, B = %d)",
                     (long long)n_layers * Hkv, B);
     const SharedCaps c = shared_caps(n_layers, B, Hq, Hkv, max_keep, n_groups);
@@ -116,19 +118,20 @@ int check_shared_sizes(int32_t n_layers, int32_t B, int32_t Hq, int32_t Hkv, int
 
 // Bounds of any plan for these sizes.  A plan that fits one dispatch round has at
 // most per_round workgroups per (layer, KV head), each with at most kSharedRows
-// partial rows of a prefix.  Any other cuts at kSharedMaxPasses passes per
-// wavefront: a group of n sequences has at most n / (sequences per item) + 1 row
-// tiles, each list at most max_keep entries.  Each sequence's rest has a partial
-// per workgroup that it touches: one, and one more for every workgroup boundary.
+// partial rows of a prefix.  Any other is cut at the highest level: a group of n
+// sequences has at most n / (sequences per item) + 1 sets of rows, each list at most
+// max_keep entries.  Each sequence's rest has a partial per workgroup that it
+// touches: one, and one more for every workgroup boundary.
 SharedCaps shared_caps(int32_t n_layers, int32_t B, int32_t Hq, int32_t Hkv, int32_t max_keep, int32_t n_groups) {
     SharedCaps c{};
     const int64_t G = Hq / Hkv, heads = (int64_t)n_layers * Hkv;
-    const int64_t passes = ((int64_t)max_keep + kWaveTile - 1) / kWaveTile;
-    const int64_t cuts = (passes + kSharedWaves * kSharedMaxPasses - 1) / (kSharedWaves * kSharedMaxPasses);
-    const int64_t chunks = (passes + kSharedMaxPasses - 1) / kSharedMaxPasses;
-    const int64_t tiles = n_groups + B / (kSharedRows / G);
+    const auto div_up = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
+    const int64_t passes = div_up(max_keep, kWaveTile);
+    const int64_t cuts = div_up(passes, kSharedWaves / 2 * kSharedLevels);
+    const int64_t chunks = div_up(passes, kSharedLevels + kSharedLevels / 2);
+    const int64_t sets = n_groups + B / (kSharedRows / G);
     c.per_round = (int32_t)std::max<int64_t>(1, kRoundWorkgroups / heads);
-    const int64_t longest = tiles * cuts + (B * chunks + kSharedWaves - 1) / kSharedWaves;
+    const int64_t longest = sets * cuts + div_up(B * chunks, kSharedWaves);
     c.n_wg = (int32_t)std::min<int64_t>(std::max<int64_t>(c.per_round, longest), 0x7fffffff);
     c.rows = std::max<int64_t>((int64_t)c.per_round * kSharedRows, B * G * cuts) + G * (B + (int64_t)c.n_wg);
     c.n_scan = (max_keep - 1) / kScanLen + 1;
@@ -344,6 +347,7 @@ MURMUR_EXPORT int murmur_decode_attn_shared(const void *q_dev, const murmur_kv *
     a.n_groups = n_groups;
     a.n_wg = c.n_wg;
     a.out_f32 = out_dtype == MURMUR_DTYPE_F32;
+    a.magic_g = (uint32_t)((((uint64_t)1 << 32) + a.G - 1) / a.G - 1);
     a.scale_log2 = scale * 1.4426950408889634f;
     const int e = launch_decode_attn_shared(a, stream);
     if (e != 0) return fail(MURMUR_EHIP, "decode_attn_shared launch failed: %s", hip_error_text(e));

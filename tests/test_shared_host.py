@@ -94,8 +94,8 @@ POOL_FAULTS = [("block_size", 0, E, "power of two"), ("block_size", 12, E, "powe
                ("pool", kv(v=FAKE + 8), E, "aligned"), ("Hkv", 0, E, ">= 1"), ("Hkv", 1 << 27, E, "2^26")]
 WS_FAULTS = [("ws_dev", None, E, "NULL"), ("ws_dev", FAKE + 64, E, "256-byte")]
 SIZE_FAULTS = [("max_keep", 0, E, ">= 1"), ("B", 0, E, ">= 1"), ("n_groups", 0, E, "n_groups"),
-               ("n_groups", 65536, E, "n_groups"), ("Hq", 27, E, "multiple"), ("Hq", 68, U, "exceeds 16"),
-               ("max_keep", (1 << 28) + 1, U, "max_keep"), ("B", 65536, E, "too large"), ("plan_dev", None, E, "NULL"),
+               ("n_groups", 4097, E, "n_groups"), ("Hq", 27, E, "multiple"), ("Hq", 68, U, "exceeds 16"),
+               ("max_keep", (1 << 28) + 1, U, "max_keep"), ("B", 4097, U, "4097 sequences"), ("plan_dev", None, E, "NULL"),
                ("plan_dev", FAKE + 8, E, "16-byte"), ("plan_bytes", 1000, S, "plan of 1000"),
                ("idx_dev", None, E, "idx_dev and ranges_dev"), ("idx_dev", FAKE + 2, E, "aligned")]
 FAULTS = {
