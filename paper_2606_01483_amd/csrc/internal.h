@@ -231,29 +231,29 @@ int launch_paged_compact(int32_t B, int32_t *bt, int32_t max_blocks, int32_t log
 //     first one, per kScanLen entries.
 // n_wg bounds the workgroups of a (layer, KV head) whatever the lists hold (see
 // shared_caps).
-constexpr int kSharedWaves = 8;
-constexpr int kSharedRows = 64;       // query rows of one prefix item: four MFMA row tiles
+constexpr int kSharedWaves = 4;       // of a workgroup, two of which share a compute unit
+constexpr int kSharedRows = 48;       // query rows of one prefix item: three MFMA row tiles
 constexpr int kSharedMaxSeqs = 4096;  // sequences of a batch (the planner's LDS)
 // A cut of the work at level j = 1 .. kSharedLevels gives a wavefront of a prefix
 // item up to j passes of kWaveTile positions and one of a rest up to j + j / 2 (it
-// holds half the row tiles or fewer).
+// has one row tile).
 constexpr int kSharedLevels = 16;
 constexpr int kScanLen = 4096;
 constexpr int32_t kPlanMagic = 0x6d75726d;
 struct PlanHeader {
     int32_t magic, n_work, bad, unused0;  // bad: the groups are not in order; every output is NaN
     int32_t B, max_keep, n_layers, Hq, Hkv, n_groups;  // what the plan was made for
-    int32_t rows, level, unused[4];       // partial rows per (layer, KV head)
+    int32_t rows, level, unused[4];       // partial rows per (layer, KV head); the cut (below 0: no list is cut)
 };
 struct PlanSeq {
     int32_t state;  // 0: not in any group (outputs untouched), 1: computed, 2: invalid count (NaN outputs)
     int32_t pre_row, pre_stride, n_pre;  // partials over the prefix: rows pre_row + i * pre_stride + head
     int32_t rest_row, n_rest;            // over the rest: rows rest_row + i * G + head
-    int32_t unused[2];
+    int32_t rest, unused;                // length of the rest (plans without cuts)
 };
 struct PlanItem {
-    int32_t seq0, n_seq, list, r0, r1, row, unused[2];  // n_seq 0: remainders; list: the sequence whose list is read;
-                                                        // row: partial row
+    int32_t seq0, n_seq, list, r0, r1, row;  // n_seq 0: remainders; list: the sequence whose list is read; row: partial row
+    int32_t stream, unused;                  // stream: the rows are read once, in a large launch
 };
 struct PlanChunk {
     int32_t seq, r0, r1, row;  // seq -1: none
@@ -261,6 +261,8 @@ struct PlanChunk {
 struct SharedCaps {
     int32_t per_round;  // workgroups per (layer, KV head) of one dispatch round
     int32_t n_wg, n_scan;
+    bool whole;         // no list is cut (see shared_caps)
+    int32_t waves;      // of a workgroup then
     int64_t rows;       // partial rows per (layer, KV head)
     size_t plan_bytes, ws_bytes, scan_offset, chunk_offset, item_offset;
 };
@@ -287,6 +289,7 @@ struct SharedAttnLaunch {
     float *part_ml;  // [layers * KV heads][rows][2]  (running max in log2 units, sum)
     int64_t rows_cap;
     int32_t max_len, max_keep, B, Hq, Hkv, G, NL, n_groups, n_wg, out_f32;
+    int32_t waves;     // SharedCaps::waves, 0 where lists are cut
     uint32_t magic_g;  // magic16(G): row / G for rows below 2^16
     float scale_log2;
 };

@@ -117,8 +117,8 @@ int check_shared_sizes(int32_t n_layers, int32_t B, int32_t Hq, int32_t Hkv, int
 }  // namespace
 
 // Bounds of any plan for these sizes.  A plan that fits one dispatch round has at
-// most per_round workgroups per (layer, KV head), each with at most kSharedRows
-// partial rows of a prefix.  Any other is cut at the highest level: a group of n
+// most per_round workgroups per (layer, KV head) (two share a compute unit), each
+// with at most kSharedRows partial rows of a prefix.  Any other is cut at the highest level: a group of n
 // sequences has at most n / (sequences per item) + 1 sets of rows, each list at most
 // max_keep entries.  Each sequence's rest has a partial per workgroup that it
 // touches: one, and one more for every workgroup boundary.
@@ -127,19 +127,32 @@ SharedCaps shared_caps(int32_t n_layers, int32_t B, int32_t Hq, int32_t Hkv, int
     const int64_t G = Hq / Hkv, heads = (int64_t)n_layers * Hkv;
     const auto div_up = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
     const int64_t passes = div_up(max_keep, kWaveTile);
-    const int64_t cuts = div_up(passes, kSharedWaves / 2 * kSharedLevels);
+    const int64_t cuts = div_up(passes, kSharedWaves * kSharedLevels);
     const int64_t chunks = div_up(passes, kSharedLevels + kSharedLevels / 2);
     const int64_t sets = n_groups + B / (kSharedRows / G);
-    c.per_round = (int32_t)std::max<int64_t>(1, kRoundWorkgroups / heads);
+    c.per_round = (int32_t)std::max<int64_t>(1, 2 * kRoundWorkgroups / heads);
     const int64_t longest = sets * cuts + div_up(B * chunks, kSharedWaves);
     c.n_wg = (int32_t)std::min<int64_t>(std::max<int64_t>(c.per_round, longest), 0x7fffffff);
     c.rows = std::max<int64_t>((int64_t)c.per_round * kSharedRows, B * G * cuts) + G * (B + (int64_t)c.n_wg);
+    // Whether lists are left whole (shared_whole_kernel) or cut (shared_attn_kernel and the merge), from what the host
+    // knows, in us: whole, each workgroup of eight wavefronts takes a list's passes at 1 us a round of them (as many
+    // compute units read at once, from the L2s too), and a dispatch round after the other; cut, every group's list
+    // comes at the memory's rate, and the partials cost about 12 more.
+    const int64_t whole_wg = heads * std::min<int64_t>(B, n_groups + B / (kMaxGroup / G));
+    const double whole_us = (double)div_up(whole_wg, kRoundWorkgroups) * (double)div_up(passes, 8) + 5.0;
+    const double cut_us = (double)heads * std::min(n_groups, B) * max_keep * 512.0 / 5e6 + 17.0;
+    c.whole = whole_us <= cut_us;
+    c.waves = heads * std::min(n_groups, B) > kRoundWorkgroups ? 4 : 8;
+    if (c.whole) {
+        c.n_wg = (int32_t)std::min<int64_t>(B, n_groups + B / (kMaxGroup / G));
+        c.rows = 0;
+    }
     c.n_scan = (max_keep - 1) / kScanLen + 1;
     c.item_offset = sizeof(PlanHeader) + sizeof(PlanSeq) * (size_t)B;
     c.chunk_offset = c.item_offset + sizeof(PlanItem) * (size_t)c.n_wg;
     c.scan_offset = c.chunk_offset + sizeof(PlanChunk) * (size_t)c.n_wg * kSharedWaves;
     c.plan_bytes = round_up(c.scan_offset + 4 * (size_t)B * c.n_scan, 256);
-    c.ws_bytes = round_up((size_t)heads * (size_t)c.rows * (kHeadDim + 2) * sizeof(float), 256);
+    c.ws_bytes = round_up((size_t)heads * (size_t)c.rows * (kHeadDim + 2) * sizeof(float) + 1, 256);
     return c;
 }
 
@@ -346,6 +359,7 @@ MURMUR_EXPORT int murmur_decode_attn_shared(const void *q_dev, const murmur_kv *
     a.NL = kv->n_layers;
     a.n_groups = n_groups;
     a.n_wg = c.n_wg;
+    a.waves = c.whole ? c.waves : 0;
     a.out_f32 = out_dtype == MURMUR_DTYPE_F32;
     a.magic_g = (uint32_t)((((uint64_t)1 << 32) + a.G - 1) / a.G - 1);
     a.scale_log2 = scale * 1.4426950408889634f;

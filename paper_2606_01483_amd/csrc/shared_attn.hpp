@@ -9,7 +9,7 @@
 // (e^(mP-m) OP + e^(mT-m) OT) / (e^(mP-m) lP + e^(mT-m) lT), m = max(mP, mT), for
 // the (max, sum, unscaled sum) of each part, so the part P that the sequences of
 // a group have in common is read once for all of their query rows: a workgroup
-// multiplies each pass of 32 positions with up to 64 rows (four MFMA row tiles).  Bound: the K/V bytes, each distinct row once.
+// multiplies each pass of 32 positions with up to 48 rows (three MFMA row tiles).  Bound: the K/V bytes, each distinct row once.
 #pragma once
 
 namespace murmur {
@@ -75,28 +75,97 @@ __global__ __launch_bounds__(kScanThreads) void shared_scan_kernel(const int32_t
 
 static __device__ __forceinline__ int div_up(int x, int y) { return (x + y - 1) / y; }
 
-// Of a cut at level j: positions that one workgroup takes of a prefix with so many
-// query rows, and passes that one wavefront takes of a rest.
-static __device__ __forceinline__ int item_groups(int rows) { return rows > 32 ? kSharedWaves / 2 : kSharedWaves; }
-static __device__ __forceinline__ int item_passes(int rows, int level) { return item_groups(rows) * level; }
+// Of a cut at some level: passes that one workgroup takes of a prefix, and one
+// wavefront of a rest.
+static __device__ __forceinline__ int item_passes(int level) { return kSharedWaves * level; }
 static __device__ __forceinline__ int chunk_passes(int level) { return level + level / 2; }
 
 // One workgroup; what it needs of every sequence and group is in LDS, so that the
 // global round trips are the counts with the groups, and the stores.  The lowest
-// level of cut whose workgroups fit one dispatch round is taken (each of the sixteen
-// wavefronts adds up one), or the highest.
-constexpr int kPlanThreads = 1024;
+// level of cut whose workgroups fit one dispatch round is taken (the wavefronts add
+// them up side by side), or the highest.
 struct PlanLds {
     int rest[kSharedMaxSeqs];           // by sequence: length of the rest, -1 if the sequence is left out
     uint16_t of[kSharedMaxSeqs];        // its group
     int lo[kSharedMaxSeqs + 1];         // by group: first sequence
     int common[kSharedMaxSeqs];         // what it shares
     int row[kSharedMaxSeqs], item[kSharedMaxSeqs];  // its first partial row and item
-    int scan[kPlanThreads / 64], work[kSharedLevels + 1], bad;
+    int scan[16], work[kSharedLevels + 1], bad;
+    unsigned positions;
 };
+// The plan where no list is cut: a workgroup per (layer, KV head) and some sequences
+// of a group, with one, two or three row tiles, whichever is estimated fastest (in
+// tenths of a pass with one tile; measured: a pass takes half as long again with
+// each further tile, and a workgroup about six passes besides).
+template <int kPlanThreads>
+static __device__ __forceinline__ void plan_whole(const SharedPlanLaunch &p, PlanLds &l, PlanHeader *h, PlanSeq *seqs,
+                                                  PlanItem *items, int end, int stream, int tid) {
+    const int n_groups = p.n_groups, G = p.Hq / p.Hkv, lane = tid & 63, wave = tid >> 6;
+    const int heads = p.n_layers * p.Hkv, waves = p.caps.waves, slots = waves == 8 ? kRoundWorkgroups : 2 * kRoundWorkgroups;
+    for (int g = tid; g < n_groups; g += kPlanThreads) l.row[g] = 0;
+    __syncthreads();
+    for (int b = tid; b < p.B; b += kPlanThreads) {
+        const int rest = b < end ? max(l.rest[b], 0) : 0;
+        if (b < end) {
+            PlanSeq s = {};
+            s.state = l.rest[b] >= 0 ? 1 : 2;
+            s.rest = rest;
+            seqs[b] = s;
+            atomicAdd(&l.row[l.of[b]], div_up(rest, kWaveTile));
+        }
+    }
+    __syncthreads();
+    if (wave < 3) {
+        const int per = 16 * (wave + 1) / G;
+        int wg = 0, sum = 0, most = 0;
+        for (int g = lane; per > 0 && g < n_groups; g += 64) {
+            const int n = l.lo[g + 1] - l.lo[g], parts = div_up(n, per);
+            if (n == 0) continue;
+            const int cost = 60 + (10 + 5 * wave) * div_up(div_up(max(l.common[g], 0), kWaveTile) + div_up(l.row[g], parts), waves);
+            wg += parts;
+            sum += parts * min(cost, 1 << 18);
+            most = max(most, cost);
+        }
+#pragma unroll
+        for (int x = 32; x >= 1; x /= 2) {
+            wg += __shfl_xor(wg, x);
+            sum += __shfl_xor(sum, x);
+            most = max(most, __shfl_xor(most, x));
+        }
+        if (lane == 0)
+            l.work[wave] = per == 0 ? 0x7fffffff
+                                    : (int)min<int64_t>(0x7ffffffe, (int64_t)most + ((int64_t)wg * heads > slots ? (int64_t)sum * heads / slots : 0));
+    }
+    __syncthreads();
+    int tiles = 0;
+    for (int i = 1; i < 3; ++i) tiles = l.work[i] < l.work[tiles] ? i : tiles;
+    const int per = 16 * (tiles + 1) / G;
+    int work = 0;
+    for (int g0 = 0; g0 < n_groups; g0 += kPlanThreads) {
+        const int g = g0 + tid, n = g < n_groups ? l.lo[g + 1] - l.lo[g] : 0;
+        int total;
+        const int at = work + wg_exclusive_scan<kPlanThreads>(div_up(n, per), l.scan, tid, total);
+        work += total;
+        if (g < n_groups) l.item[g] = at;
+    }
+    __syncthreads();
+    for (int g = wave; g < n_groups; g += kPlanThreads / 64) {
+        const int lo = l.lo[g], n = l.lo[g + 1] - lo, parts = div_up(n, per);
+        for (int i = lane; i < parts; i += 64) {
+            const int s0 = n * i / parts, s1 = n * (i + 1) / parts;
+            items[l.item[g] + i] = PlanItem{lo + s0, s1 - s0, lo, 0, max(l.common[g], 0), 0, stream && parts <= 2, 0};
+        }
+    }
+    if (tid == 0) {
+        h->n_work = work;
+        h->rows = 0;
+        h->level = -(tiles + 1);
+    }
+}
+
+template <int kPlanThreads>
 __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedPlanLaunch p) {
     __shared__ PlanLds l;
-    static_assert(kSharedLevels == kPlanThreads / 64, "a wavefront per level");
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int B = p.B, n_groups = p.n_groups, max_keep = p.max_keep;
     const int G = p.Hq / p.Hkv, per_item = kSharedRows / G;
@@ -108,7 +177,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     const int n_scan = p.caps.n_scan;
 
     // the groups, and every sequence's count (in `rest` for now)
-    if (tid == 0) l.bad = 0;
+    if (tid == 0) l.bad = l.positions = 0;
     for (int b = tid; b < B; b += kPlanThreads) l.rest[b] = list_count(p.ranges, p.count, b);
     for (int g = tid; g <= n_groups; g += kPlanThreads) l.lo[g] = p.group[g];
     for (int g = tid; g < n_groups; g += kPlanThreads) l.common[g] = p.find ? max_keep : p.shared[g];
@@ -174,12 +243,27 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     if (err) raise_device_error(err);
     __syncthreads();
 
-    {
-        const int level = wave + 1;
+    int stream;
+    {  // positions that a layer reads
+        int n = 0;
+        for (int g = tid; g < n_groups; g += kPlanThreads) n += max(l.common[g], 0);
+        for (int b = tid; b < end; b += kPlanThreads) n += max(l.rest[b], 0);
+#pragma unroll
+        for (int x = 32; x >= 1; x /= 2) n += __shfl_xor(n, x);
+        if (lane == 0) atomicAdd(&l.positions, (unsigned)min(n, 1 << 24));
+        __syncthreads();
+        stream = (int64_t)l.positions * p.Hkv * 2 * kTileRowBytes >= kStreamBytes;
+    }
+    if (p.caps.whole) {
+        plan_whole<kPlanThreads>(p, l, h, seqs, items, end, stream, tid);
+        return;
+    }
+
+    for (int level = wave + 1; level <= kSharedLevels; level += kPlanThreads / 64) {
         int wg = 0, waves = 0;
         for (int g = lane; g < n_groups; g += 64) {
             const int n = l.lo[g + 1] - l.lo[g], pre = div_up(max(l.common[g], 0), kWaveTile);
-            wg += div_up(n, per_item) * div_up(pre, item_passes(min(n, per_item) * G, level));
+            wg += div_up(n, per_item) * div_up(pre, item_passes(level));
         }
         for (int b = lane; b < end; b += 64)
             waves += div_up(div_up(max(l.rest[b], 0), kWaveTile), chunk_passes(level));
@@ -199,7 +283,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     for (int g0 = 0; g0 < n_groups; g0 += kPlanThreads) {
         const int g = g0 + tid;
         const int n = g < n_groups ? l.lo[g + 1] - l.lo[g] : 0, pre = n > 0 ? div_up(max(l.common[g], 0), kWaveTile) : 0;
-        const int cuts = div_up(pre, item_passes(min(n, per_item) * G, level));
+        const int cuts = div_up(pre, item_passes(level));
         int total;
         const int at = work + wg_exclusive_scan<kPlanThreads>(div_up(n, per_item) * cuts, l.scan, tid, total);
         work += total;
@@ -211,14 +295,20 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
         }
     }
     __syncthreads();
+    const int heads = p.n_layers * p.Hkv;
+    const int apart = heads % 8 == 0 ? 1 : (heads % 4 == 0 ? 2 : (heads % 2 == 0 ? 4 : 8));
     for (int g = wave; g < n_groups; g += kPlanThreads / 64) {
         const int lo = l.lo[g], n = l.lo[g + 1] - lo, common = max(l.common[g], 0), pre = n > 0 ? div_up(common, kWaveTile) : 0;
-        const int cuts = div_up(pre, item_passes(min(n, per_item) * G, level)), parts = div_up(n, per_item);
+        const int cuts = div_up(pre, item_passes(level)), parts = div_up(n, per_item);
         for (int i = lane; i < cuts * parts; i += 64) {
-            const int cut = i / parts, s0 = (i - cut * parts) * per_item;
+            const int cut = i / parts, part = i - cut * parts, s0 = n * part / parts, s1 = n * (part + 1) / parts;
             const int r0 = (int)((int64_t)pre * cut / cuts) * kWaveTile;
             const int r1 = min((int)((int64_t)pre * (cut + 1) / cuts) * kWaveTile, common);
-            items[l.item[g] + i] = PlanItem{lo + s0, min(per_item, n - s0), lo, r0, r1, l.row[g] + (cut * n + s0) * G, {0, 0}};
+            // The parts of one stretch read the same rows: they lie `apart` items apart, which puts them on one XCD
+            // (workgroup w of the launch runs on XCD w mod 8), one after the other.
+            const int block = cut / apart, wide = min(apart, cuts - block * apart);
+            items[l.item[g] + block * apart * parts + part * wide + cut % apart] = PlanItem{lo + s0, s1 - s0, lo, r0, r1, l.row[g] + (cut * n + s0) * G,
+                         stream && parts <= 2, 0};
         }
     }
     // The rests: a wavefront's chunk each, the sequences one after the other; a
@@ -246,14 +336,14 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
         s.state = l.rest[b] >= 0 ? 1 : 2;
         s.pre_row = l.row[g] + (b - lo) * G;
         s.pre_stride = n_seq * G;
-        s.n_pre = div_up(div_up(common, kWaveTile), item_passes(min(n_seq, per_item) * G, level));
+        s.n_pre = div_up(div_up(common, kWaveTile), item_passes(level));
         s.rest_row = row;
         s.n_rest = parts;
         seqs[b] = s;
     }
     const int rest_wg = div_up(done, kSharedWaves);
     for (int c = done + tid; c < rest_wg * kSharedWaves; c += kPlanThreads) chunks[chunk0 + c] = PlanChunk{-1, 0, 0, 0};
-    for (int w = tid; w < rest_wg; w += kPlanThreads) items[work + w] = PlanItem{0, 0, 0, 0, 0, 0, {0, 0}};
+    for (int w = tid; w < rest_wg; w += kPlanThreads) items[work + w] = PlanItem{0, 0, 0, 0, 0, 0, stream, 0};
     if (tid == 0) {
         h->n_work = work + rest_wg;
         h->rows = rows;
@@ -332,10 +422,11 @@ struct RowSource<true> {
         row_bytes = (uint32_t)s_pos * 2u;
         base = raw_buffer(p, (uint32_t)(max_len - 1) * row_bytes + kTileRowBytes);
     }
+    template <int kAux>
     __device__ __forceinline__ void load(uint8_t *tile, const uint32_t (&at)[8]) const {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(base, (lds_void_t *)(tile + j * 1024), 16, at[j], 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(base, (lds_void_t *)(tile + j * 1024), 16, at[j], 0, 0, kAux);
     }
 };
 template <>
@@ -346,65 +437,152 @@ struct RowSource<false> {
         base = p;
         s_pos = s;
     }
+    template <int kAux>
     __device__ __forceinline__ void load(uint8_t *tile, const int32_t (&pos)[8], int lane) const {
         const int q = lane >> 4, sl = lane & 15;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             __builtin_amdgcn_global_load_lds(base + (int64_t)pos[j] * s_pos + 8 * (sl ^ ((4 * j + q) & 15)),
-                                             (lds_void_t *)(tile + j * 1024), 16, 0, 0);
+                                             (lds_void_t *)(tile + j * 1024), 16, 0, kAux);
     }
 };
 
-// What a wavefront reads from: the list or range table of one sequence, and the
-// K/V of one (layer, KV head) of it.
+// What a pass reads from: the list or range table of one sequence, and the K/V of
+// one (layer, KV head) of it.
 template <bool kNear>
 struct Rows {
     RangeTab tab;
     __amdgpu_buffer_rsrc_t list;
     RowSource<kNear> k, v;
-    int max_len;
+};
+template <int kSrc, bool kNear>
+static __device__ __forceinline__ Rows<kNear> rows_of(const SharedAttnLaunch &a, int list, int layer, int g) {
+    Rows<kNear> in;
+    if (kSrc == kSrcIndex) {
+        in.list = raw_buffer(a.idx + (int64_t)list * a.max_keep, (uint32_t)a.max_keep * 4u);
+    } else {
+        int32_t rg[2 * kPieces];
+#pragma unroll
+        for (int k = 0; k < 2 * kPieces; ++k) rg[k] = a.ranges[(int64_t)list * 2 * kPieces + k];
+        in.tab = make_tab(rg);
+    }
+    const int64_t off = layer * a.s_layer + list * a.s_b + g * a.s_h;
+    in.k.init(a.k + off, a.s_pos, a.max_len);
+    in.v.init(a.v + off, a.s_pos, a.max_len);
+    return in;
+}
+
+// A pass: ranks r .. min(r + 32, r_end) - 1 of a sequence's list, for the rows of
+// every sequence of the item, or (only >= 0) of one.
+struct Pass {
+    int list, r, r_end, only;
 };
 
-// Ranks r, r + step, ... below r_end, 32 at a time, against kTiles row tiles whose
-// queries are in registers.
-template <int kSrc, bool kNear, int kTiles>
-static __device__ __forceinline__ void run_passes(const Rows<kNear> &in, int r, int r_end, int step, uint8_t *stage,
-                                                  uint8_t (*slots)[kIdxSlotBytes], const u32x4 (&qf)[kTiles][4],
-                                                  float scale, WaveAcc (&w)[kTiles], int lane) {
-    if (r >= r_end) return;
+// Where a wavefront's passes come from; next() is false behind the last one.
+struct OneList {  // ranks r, r + step, ... below r_end of one list
+    static constexpr bool kOne = true;
+    int list, r, r_end, step;
+    __device__ __forceinline__ bool next(Pass &p) {
+        p = Pass{list, r, r_end, -1};
+        r += step;
+        return p.r < r_end;
+    }
+};
+struct WholeLists {  // every step-th pass of an item: those of the prefix, then its sequences' rests
+    static constexpr bool kOne = false;
+    int list, seq0, n_seq, common, pre, total;  // passes of the prefix, of everything
+    int at, step;
+    int rest, first;  // of the lane's sequence: length, first pass of the rests
+    __device__ __forceinline__ bool next(Pass &p) {
+        const int i = at;
+        at += step;
+        p = Pass{list, i * kWaveTile, common, -1};
+        if (i < pre) return true;
+        const int q = i - pre;
+        // the last sequence that starts at or before pass q (sequences without a rest start where the next one does)
+        const uint64_t begun = __ballot((int)(threadIdx.x & 63) < n_seq && first <= q);
+        const int s = max(__popcll(begun) - 1, 0);
+        const int r = common + (q - __builtin_amdgcn_readlane(first, s)) * kWaveTile;
+        p = Pass{seq0 + s, r, common + __builtin_amdgcn_readlane(rest, s), s};
+        return i < total;
+    }
+};
+
+// A running max that is below every logit and finite, so that a row which a pass
+// leaves out entirely (every logit -inf) stays as it is: exp2 of -inf, not of NaN.
+constexpr float kNoRows = -3.0e38f;
+
+// The passes of `feed` against kTiles row tiles.  load_queries starts the loads of
+// the queries (4 kTiles of them) into qf.  row_seq: which of the item's sequences
+// the lane's row of a tile belongs to (several lists only).  on_bad(pass) is called
+// for a pass with a position outside the cache.  Returns the positive scale
+// (signed_scale).
+template <int kSrc, bool kNear, int kTiles, typename Feed, typename LoadQ, typename OnBad>
+static __device__ __forceinline__ float run_passes(const SharedAttnLaunch &a, int layer, int g, bool stream, Feed &feed,
+                                                   uint8_t *stage, uint8_t (*slots)[kIdxSlotBytes],
+                                                   u32x4 (&qf)[kTiles][4], LoadQ load_queries,
+                                                   const int (&row_seq)[kTiles], WaveAcc (&w)[kTiles], int lane,
+                                                   OnBad on_bad) {
+    Pass cur, nxt;
+    if (!feed.next(cur)) return 1.f;
+    bool more = feed.next(nxt);
     const int n16 = lane & 15, c4 = lane >> 4;
     const uint32_t kt = lds_addr(stage), vt = kt + kTileBytes;
     int32_t pos[8];
     uint32_t at[8];
     int bad = 0;
-    const auto positions = [&](int r0, int slot) {
-        if (kSrc == kSrcIndex) dma_pos_index(slots[slot], r0, r_end, in.max_len, c4, pos, bad);
-        else dma_pos_ranges(in.tab, r0, r_end, in.max_len, c4, pos, bad);
+    const auto positions = [&](const Rows<kNear> &in, const Pass &p, int slot) {
+        if (kSrc == kSrcIndex) dma_pos_index(slots[slot], p.r, p.r_end, a.max_len, c4, pos, bad);
+        else dma_pos_ranges(in.tab, p.r, p.r_end, a.max_len, c4, pos, bad);
+        if (__ballot(bad)) {
+            on_bad(p);
+            bad = 0;
+        }
         if constexpr (kNear) {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 at[j] = (uint32_t)pos[j] * in.k.row_bytes + 16u * (uint32_t)(n16 ^ ((4 * j + c4) & 15));
         }
     };
-    const auto load = [&](const RowSource<kNear> &from, uint8_t *tile) {
-        if constexpr (kNear) from.load(tile, at);
-        else from.load(tile, pos, lane);
+    const auto load_as = [&](const RowSource<kNear> &from, uint8_t *tile, auto aux) {
+        if constexpr (kNear) from.template load<decltype(aux)::value>(tile, at);
+        else from.template load<decltype(aux)::value>(tile, pos, lane);
     };
-    if (kSrc == kSrcIndex) wait_vm<1>();  // the first slot (the caller has loaded two)
-    positions(r, 0);
+    const auto load = [&](const RowSource<kNear> &from, uint8_t *tile) {  // uniform
+        if (stream) load_as(from, tile, std::integral_constant<int, kAuxStream>{});
+        else load_as(from, tile, std::integral_constant<int, 0>{});
+    };
+    Rows<kNear> in = rows_of<kSrc, kNear>(a, cur.list, layer, g), in_next = in;
+    if (!Feed::kOne && more && nxt.list != cur.list) in_next = rows_of<kSrc, kNear>(a, nxt.list, layer, g);
+    if (kSrc == kSrcIndex) {
+        dma_idx(slots[0], in.list, cur.r, lane);
+        dma_idx(slots[1], in_next.list, more ? nxt.r : cur.r, lane);
+    }
+    asm volatile("" ::: "memory");  // the queries' loads stay behind the entries'
+    load_queries();
+    // the first slot: the second slot's load and then the queries' came after it
+    if (kSrc == kSrcIndex) wait_vm<1 + 4 * kTiles>();
+    positions(in, cur, 0);
     load(in.k, stage);
     load(in.v, stage + kTileBytes);
-    for (int it = 0;; r += step, ++it) {
-        const bool more = r + step < r_end;
-        const int valid = min(kWaveTile, r_end - r);
+    float scale = 1.f;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) scale = signed_scale(qf[t], a.scale_log2);
+    for (int it = 0;; ++it) {
         u32x4 kf[8];
         wait_vm<8>();  // this pass's K rows; its V rows came after them
         read_k_operands(kf, kt, n16, c4);
+        Pass after;
+        bool more_after = false;
+        in = in_next;
         if (more) {
-            positions(r + step, (it + 1) & 1);  // entries that were loaded before this pass's K rows
-            if (kSrc == kSrcIndex) dma_idx(slots[it & 1], in.list, r + 2 * step, lane);
+            positions(in, nxt, (it + 1) & 1);  // entries that were loaded before this pass's K rows
+            more_after = feed.next(after);
+            if (!Feed::kOne && more_after && after.list != nxt.list) in_next = rows_of<kSrc, kNear>(a, after.list, layer, g);
+            if (kSrc == kSrcIndex) dma_idx(slots[it & 1], in_next.list, more_after ? after.r : nxt.r, lane);
             load(in.k, stage);
         }
+        const int valid = min(kWaveTile, cur.r_end - cur.r);
         u32x4 p_hi[kTiles], p_lo[kTiles];
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
@@ -414,6 +592,13 @@ static __device__ __forceinline__ void run_passes(const Rows<kNear> &in, int r, 
                 s[blk] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int kc = 0; kc < 4; ++kc) s[blk] = mfma16x16x32(kf[4 * blk + kc], qf[t][kc], s[blk]);
+            }
+            if (!Feed::kOne && cur.only >= 0) {  // uniform
+                const bool mine = row_seq[t] == cur.only;
+#pragma unroll
+                for (int blk = 0; blk < 2; ++blk)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[blk][i] = mine ? s[blk][i] : kNegInf;
             }
             softmax_step<true>(s, valid, scale, w[t], c4, p_hi[t], p_lo[t]);
         }
@@ -432,69 +617,72 @@ static __device__ __forceinline__ void run_passes(const Rows<kNear> &in, int r, 
             }
         }
         if (!more) break;
+        cur = nxt;
+        nxt = after;
+        more = more_after;
     }
-    w[0].bad_pos |= bad;
+    return scale;
+}
+
+// The queries of an item's rows as B operands of its row tiles, past the last row
+// its copies (their results are not stored); row_seq: each lane's sequence.
+template <int kTiles>
+static __device__ __forceinline__ void load_item_queries(const SharedAttnLaunch &a, const PlanItem &it, int layer, int g,
+                                                         int n16, int c4, u32x4 (&qf)[kTiles][4], int (&row_seq)[kTiles]) {
+    const int rows = it.n_seq * a.G;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        const uint32_t rr = (uint32_t)min(16 * t + n16, rows - 1);
+        const uint32_t s = div16(rr, a.magic_g);
+        row_seq[t] = (int)s;
+        const int64_t row = ((int64_t)layer * a.B + it.seq0 + (int)s) * a.Hq + g * a.G + (int)(rr - s * (uint32_t)a.G);
+#pragma unroll
+        for (int kc = 0; kc < 4; ++kc) qf[t][kc] = load16(a.q + row * kHeadDim + 8 * c4 + 32 * kc);
+    }
 }
 
 // ---------------------------------------------------------------------------
-// Workgroup (layer and KV head, i) does item i of the plan.
-// A prefix item: up to 32 query rows are two row tiles, which every wavefront holds,
-// the eight taking the passes in turn; with more, four wavefronts take the passes
-// for the first two row tiles and the other four the same passes for the rest (each
-// loads its own K and V: the second load of a row comes from the L2; a wavefront
-// with all four tiles leaves no registers and needs four rounds to publish them).
-// Remainders: a wavefront works on a chunk of a sequence of its own.
+// Workgroup (layer and KV head, i) does item i of the plan: a stretch of a prefix,
+// whose passes its wavefronts take in turn, each for all of the item's query rows;
+// or remainders, each wavefront a chunk of some sequence's.  Four wavefronts and
+// less than 80 KiB of LDS, so that two workgroups share a compute unit and one's
+// prologue and epilogue overlap the other's loads.
 // ---------------------------------------------------------------------------
 constexpr int kSharedThreads = kSharedWaves * 64;
+template <int kWaves>
 struct SharedLds {
-    uint8_t stages[kSharedWaves][kStageBytes];
-    uint8_t slots[kSharedWaves][2][kIdxSlotBytes];
-    float ml[kSharedWaves][32][2];  // per wavefront and row: max (log2 units), sum
-    int flag[kSharedWaves];
-    int seq[kSharedWaves + 1], row[kSharedWaves];
+    uint8_t stages[kWaves][kStageBytes];
+    uint8_t slots[kWaves][2][kIdxSlotBytes];
+    float ml[kWaves][32][2];  // per wavefront and row of a round: max (log2 units), sum
+    int flag[kWaves];
+    int seq[kWaves + 1], row[kWaves];
+    unsigned long long bad;   // sequences of the item with a position outside the cache
 };
 
-template <int kSrc, bool kNear>
-static __device__ __forceinline__ Rows<kNear> rows_of(const SharedAttnLaunch &a, int list, int layer, int g) {
-    Rows<kNear> in;
-    if (kSrc == kSrcIndex) {
-        in.list = raw_buffer(a.idx + (int64_t)list * a.max_keep, (uint32_t)a.max_keep * 4u);
-    } else {
-        int32_t rg[2 * kPieces];
-#pragma unroll
-        for (int k = 0; k < 2 * kPieces; ++k) rg[k] = a.ranges[(int64_t)list * 2 * kPieces + k];
-        in.tab = make_tab(rg);
-    }
-    const int64_t off = layer * a.s_layer + list * a.s_b + g * a.s_h;
-    in.k.init(a.k + off, a.s_pos, a.max_len);
-    in.v.init(a.v + off, a.s_pos, a.max_len);
-    in.max_len = a.max_len;
-    return in;
-}
-
-// A wavefront's tiles into its own stage and the pairs, for the sums over the
-// wavefronts: row r of the wavefront, 16-byte chunk c at slot c ^ (r & 7) (the
-// lanes of a store hold 16 rows of one chunk).
-template <int kTiles>
-static __device__ __forceinline__ void publish_tiles(SharedLds &l, WaveAcc (&w)[kTiles], float scale, int wave, int n16,
+// Up to two of a wavefront's tiles into its own stage and the pairs, for the sums
+// over the wavefronts: row r, 16-byte chunk c at slot c ^ (r & 7) (the lanes of a
+// store hold 16 rows of one chunk).
+template <int kFirst, int kTiles, int kWaves, int kAll>
+static __device__ __forceinline__ void publish_tiles(SharedLds<kWaves> &l, WaveAcc (&w)[kAll], float scale, int wave, int n16,
                                                      int c4) {
+    static_assert(kTiles <= 2, "two tiles fit a stage");
     float *o = reinterpret_cast<float *>(&l.stages[wave][0]);
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-        const float sum = sum_over_c4(w[t].l_run);
+        const float sum = sum_over_c4(w[kFirst + t].l_run);
         const int r = 16 * t + n16;
-        if (c4 == 0) *reinterpret_cast<float2 *>(&l.ml[wave][r][0]) = float2{w[t].m_run * scale, sum};
+        if (c4 == 0) *reinterpret_cast<float2 *>(&l.ml[wave][r][0]) = float2{w[kFirst + t].m_run * scale, sum};
 #pragma unroll
         for (int db = 0; db < 8; ++db)
-            *reinterpret_cast<f32x4 *>(&o[r * kHeadDim + 4 * ((4 * db + c4) ^ (r & 7))]) = w[t].acc[db];
+            *reinterpret_cast<f32x4 *>(&o[r * kHeadDim + 4 * ((4 * db + c4) ^ (r & 7))]) = w[kFirst + t].acc[db];
     }
 }
 
-// The state of row r, head dims 4 c .. 4 c + 3, over the wavefronts w0, w0 + 1 ... of
-// the workgroup into partial row `row` of this (layer, KV head).
-template <int kMost>
-static __device__ __forceinline__ void store_partial(const SharedLds &l, float *part_o, float *part_ml, int w0, int n,
-                                                     int r, int c, int64_t row, bool bad) {
+// The state of row r, head dims 4 c .. 4 c + 3, over n wavefronts (at most kMost)
+// from w0 on.
+template <int kMost, int kWaves>
+static __device__ __forceinline__ void gather_row(const SharedLds<kWaves> &l, int w0, int n, int r, int c, float &M, float &L,
+                                                  f32x4 &O) {
     float2 ml[kMost];
     f32x4 o[kMost];
 #pragma unroll
@@ -503,88 +691,96 @@ static __device__ __forceinline__ void store_partial(const SharedLds &l, float *
         ml[w] = *reinterpret_cast<const float2 *>(&l.ml[wv][r][0]);
         o[w] = *reinterpret_cast<const f32x4 *>(&l.stages[wv][(r * kHeadDim + 4 * (c ^ (r & 7))) * 4]);
     }
-    float M = ml[0].x, L = 0.f;
+    M = ml[0].x;
+    L = 0.f;
 #pragma unroll
     for (int w = 1; w < kMost; ++w) M = fmaxf(M, ml[w].x);
-    f32x4 O = {0.f, 0.f, 0.f, 0.f};
+    O = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < kMost; ++w) {
         const float f = w >= n || ml[w].x == kNegInf ? 0.f : __builtin_amdgcn_exp2f(ml[w].x - M);
         L += ml[w].y * f;
         O += f * o[w];
     }
+}
+
+// The same into partial row `row` of this (layer, KV head).
+template <int kMost>
+static __device__ __forceinline__ void store_partial(const SharedLds<kSharedWaves> &l, float *part_o, float *part_ml, int w0,
+                                                     int n, int r, int c, int64_t row, bool bad) {
+    float M, L;
+    f32x4 O;
+    gather_row<kMost>(l, w0, n, r, c, M, L, O);
     if (bad) L = __builtin_nanf("");
     *reinterpret_cast<f32x4 *>(part_o + row * kHeadDim + 4 * c) = O;
     if (c == 0) *reinterpret_cast<float2 *>(part_ml + 2 * row) = float2{M, L};
 }
 
-// kTiles row tiles per wavefront; kHalves 2: the upper four wavefronts hold the
-// second two of three or four.
-template <int kSrc, bool kNear, int kTiles, int kHalves>
-static __device__ __forceinline__ void item_work(const SharedAttnLaunch &a, const PlanItem &it, SharedLds &l, int layer,
-                                                 int g, float *part_o, float *part_ml, int tid, int wave) {
-    constexpr int kGroups = kSharedWaves / kHalves, kWaveRows = 16 * kTiles;
+// Normalised output of four head dims of query row `row`, and the lse (c == 0).
+static __device__ __forceinline__ void store_row(const SharedAttnLaunch &a, int64_t row, int c, f32x4 O, float M, float L) {
+    const float inv = 1.f / L;
+    if (a.out_f32)
+        *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.out) + row * kHeadDim + 4 * c) = O * inv;
+    else
+        *reinterpret_cast<u32x2 *>(reinterpret_cast<uint16_t *>(a.out) + row * kHeadDim + 4 * c) =
+            u32x2{pack_bf16(O[0] * inv, O[1] * inv), pack_bf16(O[2] * inv, O[3] * inv)};
+    if (c == 0 && a.lse) a.lse[row] = (M + __builtin_log2f(L)) * 0.69314718055994530942f;
+}
+
+template <int kSrc, bool kNear, int kTiles>
+static __device__ __forceinline__ void item_work(const SharedAttnLaunch &a, const PlanItem &it, SharedLds<kSharedWaves> &l,
+                                                 int layer, int g, float *part_o, float *part_ml, int tid, int wave) {
     const int lane = tid & 63, n16 = lane & 15, c4 = lane >> 4;
-    const int rows = it.n_seq * a.G, half = wave / kGroups, who = wave - half * kGroups;
-    const Rows<kNear> in = rows_of<kSrc, kNear>(a, it.list, layer, g);
-    const int r = it.r0 + who * kWaveTile, step = kGroups * kWaveTile;
-    if (kSrc == kSrcIndex && r < it.r1) {
-        dma_idx(l.slots[wave][0], in.list, r, lane);
-        dma_idx(l.slots[wave][1], in.list, r + step, lane);
-    }
-    // the queries, past the last row its copies (their results are not stored)
+    const int rows = it.n_seq * a.G;
     u32x4 qf[kTiles][4];
-    float scale = 1.f;
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-        const uint32_t rr = (uint32_t)min(half * kWaveRows + 16 * t + n16, rows - 1);
-        const uint32_t s = div16(rr, a.magic_g);
-        const int64_t row = ((int64_t)layer * a.B + it.seq0 + (int)s) * a.Hq + g * a.G + (int)(rr - s * (uint32_t)a.G);
-#pragma unroll
-        for (int kc = 0; kc < 4; ++kc) qf[t][kc] = load16(a.q + row * kHeadDim + 8 * c4 + 32 * kc);
-    }
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t) scale = signed_scale(qf[t], a.scale_log2);
+    int row_seq[kTiles];
     WaveAcc w[kTiles];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) wave_acc_reset(w[t]);
-    run_passes<kSrc, kNear, kTiles>(in, r, it.r1, step, l.stages[wave], l.slots[wave], qf, scale, w, lane);
-    publish_tiles(l, w, scale, wave, n16, c4);
-    const int bad = barrier_or<kSharedWaves>(w[0].bad_pos, l.flag, wave, lane);
-#pragma unroll
-    for (int j = 0; j < kTiles * kHalves; ++j) {
-        const int row = 16 * j + (tid >> 5), c = tid & 31;  // 16 rows of 32 chunks
-        if (row < rows)
-            store_partial<kGroups>(l, part_o, part_ml, row / kWaveRows * kGroups, kGroups, row % kWaveRows, c, it.row + row,
-                                   bad);
+    OneList feed{it.list, it.r0 + wave * kWaveTile, it.r1, kSharedWaves * kWaveTile};
+    int wave_bad = 0;
+    const float scale = run_passes<kSrc, kNear, kTiles>(
+        a, layer, g, it.stream, feed, l.stages[wave], l.slots[wave], qf,
+        [&] { load_item_queries<kTiles>(a, it, layer, g, n16, c4, qf, row_seq); }, row_seq, w, lane,
+        [&](const Pass &) { wave_bad = 1; });
+    const auto store = [&](int t0, int n_tiles, bool bad) {
+#pragma unroll 1
+        for (int j = tid >> 5; j < min(16 * n_tiles, rows - 16 * t0); j += kSharedThreads / 32)
+            store_partial<kSharedWaves>(l, part_o, part_ml, 0, kSharedWaves, j, tid & 31, it.row + 16 * t0 + j, bad);
+    };
+    constexpr int kFirstTiles = kTiles < 2 ? 1 : 2;
+    publish_tiles<0, kFirstTiles>(l, w, scale, wave, n16, c4);
+    const int bad = barrier_or<kSharedWaves>(wave_bad, l.flag, wave, lane);
+    store(0, kFirstTiles, bad);
+    if constexpr (kTiles > 2) {
+        __syncthreads();  // the rows of the tiles before are read
+        publish_tiles<2, 1>(l, w, scale, wave, n16, c4);
+        __syncthreads();
+        store(2, 1, bad);
     }
     if (bad && tid == 0) raise_device_error(MURMUR_DEVERR_POSITION);
 }
 
 template <int kSrc, bool kNear>
-static __device__ __forceinline__ void chunk_work(const SharedAttnLaunch &a, const PlanChunk &c, SharedLds &l, int layer,
-                                                  int g, float *part_o, float *part_ml, int tid, int wave) {
+static __device__ __forceinline__ void chunk_work(const SharedAttnLaunch &a, const PlanChunk &c, bool stream,
+                                                  SharedLds<kSharedWaves> &l, int layer, int g, float *part_o, float *part_ml,
+                                                  int tid, int wave) {
     const int lane = tid & 63, n16 = lane & 15, c4 = lane >> 4;
     WaveAcc w[1];
     wave_acc_reset(w[0]);
-    float scale = 1.f;
-    if (c.seq >= 0) {
-        const Rows<kNear> in = rows_of<kSrc, kNear>(a, c.seq, layer, g);
-        if (kSrc == kSrcIndex) {
-            dma_idx(l.slots[wave][0], in.list, c.r0, lane);
-            dma_idx(l.slots[wave][1], in.list, c.r0 + kWaveTile, lane);
-        }
-        u32x4 qf[1][4];
-        load_q(qf[0], a.q, ((int64_t)layer * a.B + c.seq) * a.Hq + g * a.G, a.G, n16, c4);
-        scale = signed_scale(qf[0], a.scale_log2);
-        run_passes<kSrc, kNear, 1>(in, c.r0, c.r1, kWaveTile, l.stages[wave], l.slots[wave], qf, scale, w, lane);
-    }
-    publish_tiles(l, w, scale, wave, n16, c4);
-    const int any_bad = __ballot(w[0].bad_pos != 0) != 0;
+    u32x4 qf[1][4];
+    int row_seq[1], wave_bad = 0;
+    OneList feed{c.seq, c.r0, c.r1, kWaveTile};  // none: r0 == r1
+    const PlanItem one{c.seq, 1, c.seq, 0, 0, 0, 0, 0};
+    const float scale = run_passes<kSrc, kNear, 1>(
+        a, layer, g, stream, feed, l.stages[wave], l.slots[wave], qf,
+        [&] { load_item_queries<1>(a, one, layer, g, n16, c4, qf, row_seq); }, row_seq, w, lane,
+        [&](const Pass &) { wave_bad = 1; });
+    publish_tiles<0, 1>(l, w, scale, wave, n16, c4);
     if (lane == 0) {
         l.seq[wave] = c.seq;
         l.row[wave] = c.row;
-        l.flag[wave] = any_bad;
+        l.flag[wave] = wave_bad;
     }
     if (tid == 0) l.seq[kSharedWaves] = -2;
     __syncthreads();
@@ -607,31 +803,134 @@ static __device__ __forceinline__ void chunk_work(const SharedAttnLaunch &a, con
 // Whether a plan was made for a call of these sizes.
 static __device__ __forceinline__ bool plan_fits(const SharedAttnLaunch &a, const PlanHeader &h) {
     return h.magic == kPlanMagic && !h.bad && h.B == a.B && h.max_keep == a.max_keep && h.n_layers == a.NL &&
-           h.Hq == a.Hq && h.Hkv == a.Hkv && h.n_groups == a.n_groups && h.rows <= a.rows_cap && h.n_work <= a.n_wg;
+           h.Hq == a.Hq && h.Hkv == a.Hkv && h.n_groups == a.n_groups && h.rows <= a.rows_cap && h.n_work <= a.n_wg && (h.level < 0) == (a.waves > 0);
 }
 
 template <int kSrc, bool kNear>
 __global__ __launch_bounds__(kSharedThreads, 2) void shared_attn_kernel(const SharedAttnLaunch a) {
-    __shared__ __attribute__((aligned(16))) SharedLds l;
+    __shared__ __attribute__((aligned(16))) SharedLds<kSharedWaves> l;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = blockIdx.y;
     // the header, the item and the wavefront's chunk in one round trip, whichever of the two it will be
     const PlanHeader h = *reinterpret_cast<const PlanHeader *>(a.plan);
     const PlanItem it = reinterpret_cast<const PlanItem *>(a.plan + a.item_offset)[i];
     const PlanChunk c = reinterpret_cast<const PlanChunk *>(a.plan + a.chunk_offset)[i * kSharedWaves + wave];
-    materialize(h.magic, h.n_work, h.rows, it.seq0, it.n_seq, it.list, it.r0, it.r1, it.row, c.seq, c.r0, c.r1, c.row);
+    materialize(h.magic, h.n_work, h.rows, it.seq0, it.n_seq, it.list, it.r0, it.r1, it.row, it.stream, c.seq, c.r0, c.r1, c.row);
     if (!plan_fits(a, h) || i >= h.n_work) return;
     const int layer = (int)blockIdx.x / a.Hkv, g = (int)blockIdx.x - layer * a.Hkv;
     float *part_o = a.part_o + (int64_t)blockIdx.x * h.rows * kHeadDim;
     float *part_ml = a.part_ml + (int64_t)blockIdx.x * h.rows * 2;
     const int rows = it.n_seq * a.G;
     if (rows == 0)
-        chunk_work<kSrc, kNear>(a, c, l, layer, g, part_o, part_ml, tid, wave);
+        chunk_work<kSrc, kNear>(a, c, it.stream, l, layer, g, part_o, part_ml, tid, wave);
     else if (rows <= 16)
-        item_work<kSrc, kNear, 1, 1>(a, it, l, layer, g, part_o, part_ml, tid, wave);
+        item_work<kSrc, kNear, 1>(a, it, l, layer, g, part_o, part_ml, tid, wave);
     else if (rows <= 32)
-        item_work<kSrc, kNear, 2, 1>(a, it, l, layer, g, part_o, part_ml, tid, wave);
+        item_work<kSrc, kNear, 2>(a, it, l, layer, g, part_o, part_ml, tid, wave);
     else
-        item_work<kSrc, kNear, 2, 2>(a, it, l, layer, g, part_o, part_ml, tid, wave);
+        item_work<kSrc, kNear, 3>(a, it, l, layer, g, part_o, part_ml, tid, wave);
+}
+
+// ---------------------------------------------------------------------------
+// The attention without cuts (SharedCaps::whole): a workgroup takes the whole lists
+// of some sequences of one group, up to 48 query rows, the prefix once for all of
+// them and each rest with the other sequences' rows masked, and writes the outputs.
+// No partials, no second launch.  Workgroups of one group read the same prefix
+// (from the L2s, mostly).  Eight wavefronts and a compute unit each where there are
+// about as many workgroups as compute units, else four, two workgroups on one.
+// ---------------------------------------------------------------------------
+template <int kSrc, bool kNear, int kTiles, int kWaves>
+static __device__ __forceinline__ void whole_work(const SharedAttnLaunch &a, const PlanItem &it, SharedLds<kWaves> &l,
+                                                  int layer, int g, int tid, int wave) {
+    const int lane = tid & 63, n16 = lane & 15, c4 = lane >> 4;
+    const int rows = it.n_seq * a.G;
+    const PlanSeq *seqs = reinterpret_cast<const PlanSeq *>(a.plan + sizeof(PlanHeader)) + it.seq0;
+    int rest = 0, state = 1;
+    if (lane < it.n_seq) {
+        rest = seqs[lane].rest;
+        state = seqs[lane].state;
+    }
+    if (tid == 0) l.bad = 0;
+    __syncthreads();
+    if (wave == 0) {
+        const uint64_t invalid = __ballot(state != 1);
+        if (lane == 0 && invalid) atomicOr(&l.bad, invalid);
+    }
+    const int passes = (rest + kWaveTile - 1) / kWaveTile;
+    int upto = passes;
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) {
+        const int y = __shfl_up(upto, x);
+        upto += lane >= x ? y : 0;
+    }
+    const int pre = (it.r1 + kWaveTile - 1) / kWaveTile;
+    WholeLists feed{it.list, it.seq0, it.n_seq, it.r1, pre, pre + __builtin_amdgcn_readlane(upto, 63), wave, kWaves, rest,
+                    upto - passes};
+    u32x4 qf[kTiles][4];
+    int row_seq[kTiles];
+    WaveAcc w[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        wave_acc_reset(w[t]);
+        w[t].m_run = kNoRows;
+    }
+    const float scale = run_passes<kSrc, kNear, kTiles>(
+        a, layer, g, it.stream, feed, l.stages[wave], l.slots[wave], qf,
+        [&] { load_item_queries<kTiles>(a, it, layer, g, n16, c4, qf, row_seq); }, row_seq, w, lane,
+        [&](const Pass &p) {
+            if (lane == 0) {
+                atomicOr(&l.bad, p.only < 0 ? ~0ull : 1ull << p.only);
+                raise_device_error(MURMUR_DEVERR_POSITION);
+            }
+        });
+    const auto store = [&](int t0, int n_tiles) {
+        const uint64_t bad = l.bad;
+#pragma unroll 1
+        for (int j = tid >> 5; j < min(16 * n_tiles, rows - 16 * t0); j += kWaves * 2) {
+            const uint32_t rr = (uint32_t)(16 * t0 + j), s = div16(rr, a.magic_g);
+            float M, L;
+            f32x4 O;
+            gather_row<kWaves>(l, 0, kWaves, j, tid & 31, M, L, O);
+            if (bad >> s & 1) L = __builtin_nanf("");
+            store_row(a, ((int64_t)layer * a.B + it.seq0 + (int)s) * a.Hq + g * a.G + (int)(rr - s * (uint32_t)a.G), tid & 31,
+                      O, M, L);
+        }
+    };
+    constexpr int kFirstTiles = kTiles < 2 ? 1 : 2;
+    publish_tiles<0, kFirstTiles>(l, w, scale, wave, n16, c4);
+    __syncthreads();
+    store(0, kFirstTiles);
+    if constexpr (kTiles > 2) {
+        __syncthreads();  // the rows of the tiles before are read
+        publish_tiles<2, 1>(l, w, scale, wave, n16, c4);
+        __syncthreads();
+        store(2, 1);
+    }
+}
+
+template <int kSrc, bool kNear, int kWaves>
+__global__ __launch_bounds__(kWaves * 64, 2) void shared_whole_kernel(const SharedAttnLaunch a) {
+    __shared__ __attribute__((aligned(16))) SharedLds<kWaves> l;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = blockIdx.y;
+    const PlanHeader h = *reinterpret_cast<const PlanHeader *>(a.plan);
+    const PlanItem it = reinterpret_cast<const PlanItem *>(a.plan + a.item_offset)[i];
+    materialize(h.magic, h.n_work, it.seq0, it.n_seq, it.list, it.r1, it.stream);
+    if (!plan_fits(a, h)) {  // every output is NaN
+        const int64_t rows = (int64_t)a.NL * a.B * a.Hq, step = (int64_t)gridDim.x * gridDim.y * (kWaves * 2);
+        const float nan = __builtin_nanf("");
+        for (int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (kWaves * 2) + (tid >> 5); row < rows; row += step)
+            store_row(a, row, tid & 31, f32x4{nan, nan, nan, nan}, nan, nan);
+        if (blockIdx.x == 0 && i == 0 && tid == 0) raise_device_error(MURMUR_DEVERR_GROUP);
+        return;
+    }
+    if (i >= h.n_work) return;
+    const int layer = (int)blockIdx.x / a.Hkv, g = (int)blockIdx.x - layer * a.Hkv;
+    const int rows = it.n_seq * a.G;
+    if (rows <= 16)
+        whole_work<kSrc, kNear, 1, kWaves>(a, it, l, layer, g, tid, wave);
+    else if (rows <= 32)
+        whole_work<kSrc, kNear, 2, kWaves>(a, it, l, layer, g, tid, wave);
+    else
+        whole_work<kSrc, kNear, 3, kWaves>(a, it, l, layer, g, tid, wave);
 }
 
 // kPer half wavefronts per query row, each folding every kPer-th partial: the pairs
@@ -659,9 +958,19 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(const SharedAttnLaunc
     const auto row_of = [&](int i) {
         return base + (i < s.n_pre ? s.pre_row + i * s.pre_stride : s.rest_row + (i - s.n_pre) * a.G);
     };
+    f32x4 o[kMergeBatch];
+    const auto load_rows = [&](int i0, int i, int here) {
+#pragma unroll
+        for (int j = 0; j < kMergeBatch; ++j) {
+            const int x = i + j * kPer;
+            o[j] = *reinterpret_cast<const f32x4 *>(a.part_o + row_of(i0 + (x < here ? x : 0)) * kHeadDim + 4 * lane);
+        }
+    };
     for (int i0 = 0; i0 < n; i0 += 32) {
+        const int here = min(32, n - i0);
         float2 ml = {kNegInf, 0.f};
-        if (i0 + lane < n) ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * row_of(i0 + lane));
+        if (lane < here) ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * row_of(i0 + lane));
+        load_rows(i0, who, here);
         float top = ml.x;
 #pragma unroll
         for (int x = 16; x >= 1; x /= 2) top = fmaxf(top, __shfl_xor(top, x, 32));
@@ -674,14 +983,8 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(const SharedAttnLaunc
         L = L * before + total;
         O *= before;
         M = top;
-        const int here = min(32, n - i0);
         for (int i = who; i < here; i += kPer * kMergeBatch) {
-            f32x4 o[kMergeBatch];
-#pragma unroll
-            for (int j = 0; j < kMergeBatch; ++j) {
-                const int x = i + j * kPer;
-                o[j] = *reinterpret_cast<const f32x4 *>(a.part_o + row_of(i0 + (x < here ? x : i)) * kHeadDim + 4 * lane);
-            }
+            if (i != who) load_rows(i0, i, here);
 #pragma unroll
             for (int j = 0; j < kMergeBatch; ++j) {
                 const int x = i + j * kPer;
@@ -699,13 +1002,7 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(const SharedAttnLaunc
         for (int x = 1; x < kPer; ++x) O += s_o[first + x][lane];
     }
     if (s.state == 0 || (int64_t)blockIdx.x * (8 / kPer) + (threadIdx.x >> 5) / kPer >= n_rows) return;
-    const float inv = 1.f / L;
-    if (a.out_f32)
-        *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.out) + row * kHeadDim + 4 * lane) = O * inv;
-    else
-        *reinterpret_cast<u32x2 *>(reinterpret_cast<uint16_t *>(a.out) + row * kHeadDim + 4 * lane) =
-            u32x2{pack_bf16(O[0] * inv, O[1] * inv), pack_bf16(O[2] * inv, O[3] * inv)};
-    if (lane == 0 && a.lse) a.lse[row] = (M + __builtin_log2f(L)) * 0.69314718055994530942f;
+    store_row(a, row, lane, O, M, L);
 }
 
 // ---- launchers ----
@@ -718,23 +1015,37 @@ int launch_shared_plan(const SharedPlanLaunch &p, murmur_stream_t stream) {
         const int e = (int)hipGetLastError();
         if (e != 0) return e;
     }
-    hipLaunchKernelGGL(shared_plan_kernel, dim3(1), dim3(kPlanThreads), 0, (hipStream_t)stream, p);
+    // small batches take fewer wavefronts through the barriers
+    if (p.B <= 256 && p.n_groups <= 256)
+        hipLaunchKernelGGL(shared_plan_kernel<256>, dim3(1), dim3(256), 0, (hipStream_t)stream, p);
+    else
+        hipLaunchKernelGGL(shared_plan_kernel<1024>, dim3(1), dim3(1024), 0, (hipStream_t)stream, p);
     return (int)hipGetLastError();
+}
+
+template <int kSrc, bool kNear>
+static void launch_shared_attn_near(const SharedAttnLaunch &a, hipStream_t stream) {
+    const dim3 grid((unsigned)(a.NL * a.Hkv), (unsigned)a.n_wg);
+    if (a.waves == 8)
+        hipLaunchKernelGGL((shared_whole_kernel<kSrc, kNear, 8>), grid, dim3(8 * 64), 0, stream, a);
+    else if (a.waves == 4)
+        hipLaunchKernelGGL((shared_whole_kernel<kSrc, kNear, 4>), grid, dim3(4 * 64), 0, stream, a);
+    else
+        hipLaunchKernelGGL((shared_attn_kernel<kSrc, kNear>), grid, dim3(kSharedThreads), 0, stream, a);
 }
 
 template <int kSrc>
 static void launch_shared_attn(const SharedAttnLaunch &a, hipStream_t stream) {
-    const dim3 grid((unsigned)(a.NL * a.Hkv), (unsigned)a.n_wg), threads(kSharedThreads);
     const bool near = (__int128)(a.max_len - 1) * a.s_pos * 2 + kTileRowBytes < ((__int128)1 << 32);
-    if (near) hipLaunchKernelGGL((shared_attn_kernel<kSrc, true>), grid, threads, 0, stream, a);
-    else hipLaunchKernelGGL((shared_attn_kernel<kSrc, false>), grid, threads, 0, stream, a);
+    if (near) launch_shared_attn_near<kSrc, true>(a, stream);
+    else launch_shared_attn_near<kSrc, false>(a, stream);
 }
 
 int launch_decode_attn_shared(const SharedAttnLaunch &a, murmur_stream_t stream) {
     if (a.ranges) launch_shared_attn<kSrcRanges>(a, (hipStream_t)stream);
     else launch_shared_attn<kSrcIndex>(a, (hipStream_t)stream);
     const int e = (int)hipGetLastError();
-    if (e != 0) return e;
+    if (e != 0 || a.waves > 0) return e;
     // Half wavefronts per row: as many as keep the rows' workgroups below two per compute unit; few rows have many
     // partials (a dispatch round's workgroups are shared out among them).
     const int64_t rows = (int64_t)a.NL * a.B * a.Hq;

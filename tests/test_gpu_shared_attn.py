@@ -130,11 +130,15 @@ GROUPS = {
 }
 
 
+CUT = 8000  # a max_keep this far above the lists makes the schedule that cuts them
+
+
+@pytest.mark.parametrize("extra_keep", [0, CUT])
 @pytest.mark.parametrize("hq,hkv", [(28, 4), (16, 1), (3, 3)])
 @pytest.mark.parametrize("name", sorted(GROUPS))
-def test_index_lists(name, hq, hkv):
-    announce(f"shared attention, {name}, {hq}/{hkv}")
-    c = Case(len(name) + hq, GROUPS[name], hq=hq, hkv=hkv)
+def test_index_lists(name, hq, hkv, extra_keep):
+    announce(f"shared attention, {name}, {hq}/{hkv}, +{extra_keep}")
+    c = Case(len(name) + hq, GROUPS[name], hq=hq, hkv=hkv, extra_keep=extra_keep)
     c.make_plan()
     c.attend()
     c.check()
@@ -142,41 +146,46 @@ def test_index_lists(name, hq, hkv):
     assert M.murmur_device_error() == 0
 
 
+@pytest.mark.parametrize("extra_keep", [0, CUT])
 @pytest.mark.parametrize("hq,hkv,width", [(28, 4, 9), (28, 4, 10), (28, 4, 19), (16, 1, 4), (16, 1, 5), (1, 1, 64),
                                           (1, 1, 65), (2, 2, 130), (15, 1, 9), (12, 4, 21)])
-def test_row_tiles(hq, hkv, width):
+def test_row_tiles(hq, hkv, width, extra_keep):
     """Groups at and beyond the query rows of one item, several layers, bf16 outputs."""
     announce(f"row tiles {hq}/{hkv} x {width}")
-    c = Case(width, [(300, [x % 5 for x in range(width)]), (45, [3])], NL=3, hq=hq, hkv=hkv, f32=False)
+    c = Case(width, [(300, [x % 5 for x in range(width)]), (45, [3])], NL=3, hq=hq, hkv=hkv, f32=False,
+             extra_keep=extra_keep)
     c.make_plan()
     c.attend()
     c.check()
 
 
+@pytest.mark.parametrize("extra_keep", [0, CUT])
 @pytest.mark.parametrize("layout", ["head", "padded"])
-def test_layouts(layout):
+def test_layouts(layout, extra_keep):
     announce(f"pool layout {layout}")
-    c = Case(5, [(90, [10, 0, 33]), (0, [50])], NL=2, layout=layout)
+    c = Case(5, [(90, [10, 0, 33]), (0, [50])], NL=2, layout=layout, extra_keep=extra_keep)
     c.make_plan()
     c.attend()
     c.check()
 
 
+@pytest.mark.parametrize("extra_keep", [0, CUT])
 @pytest.mark.parametrize("scale,lift", [(0.0, 1.0), (-0.7, 1.0), (1.0, 4.0), (1e-30, 1.0), (40.0, 30.0)])
-def test_scales(scale, lift):
+def test_scales(scale, lift, extra_keep):
     """Negative and zero scales, and logits of thousands (a one-hot softmax)."""
     announce(f"scale {scale}")
-    c = Case(6, [(200, [30, 1, 0]), (0, [3])], scale=scale, lift=lift)
+    c = Case(6, [(200, [30, 1, 0]), (0, [3])], scale=scale, lift=lift, extra_keep=extra_keep)
     c.make_plan()
     c.attend()
     c.check()
 
 
-def test_shares_given_by_the_caller():
+@pytest.mark.parametrize("extra_keep", [0, CUT])
+def test_shares_given_by_the_caller(extra_keep):
     """Any number up to what the lists share gives the same result; too many is an error of the sequences it is too
     many for, or of the whole group where the first one's list is too short."""
     announce("given shares")
-    c = Case(7, [(70, [10, 0, 5]), (40, [0, 2])], extra_keep=40)
+    c = Case(7, [(70, [10, 0, 5]), (40, [0, 2])], extra_keep=40 + extra_keep)
     for given in ([70, 40], [0, 0], [33, 1], [69, 39]):
         c.shared.copy_(i32(given))
         c.make_plan(find=False)
@@ -198,10 +207,11 @@ def test_shares_given_by_the_caller():
             c.check([b for b in range(5) if b not in bad])
 
 
-def test_bad_counts():
+@pytest.mark.parametrize("extra_keep", [0, CUT])
+def test_bad_counts(extra_keep):
     """A count of zero or above max_keep is the sequence's own error; the others share as if it were not there."""
     announce("bad counts")
-    c = Case(8, [(50, [10, 0, 5, 9]), (40, [3, 2])])
+    c = Case(8, [(50, [10, 0, 5, 9]), (40, [3, 2])], extra_keep=extra_keep)
     count = c.count.clone()
     for bad, value in ((1, 0), (2, c.keep + 1), (3, -4)):
         c.count[bad] = value
@@ -223,9 +233,10 @@ def test_bad_counts():
     assert int(c.shared[1]) == 0
 
 
-def test_positions_outside_the_pool():
+@pytest.mark.parametrize("extra_keep", [0, CUT])
+def test_positions_outside_the_pool(extra_keep):
     announce("positions outside the pool")
-    c = Case(9, [(50, [10, 0, 5]), (40, [3, 2])])
+    c = Case(9, [(50, [10, 0, 5]), (40, [3, 2])], extra_keep=extra_keep)
     c.idx[2, 53] = c.rows  # in the rest of sequence 2
     c.make_plan()
     c.attend()
@@ -242,10 +253,11 @@ def test_positions_outside_the_pool():
     c.check([3, 4])
 
 
+@pytest.mark.parametrize("extra_keep", [0, CUT])
 @pytest.mark.parametrize("group", [[1, 3, 5], [0, 4, 3], [0, 3, 9], [0, -1, 5]])
-def test_groups_out_of_order(group):
+def test_groups_out_of_order(group, extra_keep):
     announce(f"groups {group}")
-    c = Case(10, [(50, [10, 0, 5]), (40, [3, 2])])
+    c = Case(10, [(50, [10, 0, 5]), (40, [3, 2])], extra_keep=extra_keep)
     c.group.copy_(i32(group))
     c.make_plan()
     c.attend()
@@ -254,9 +266,10 @@ def test_groups_out_of_order(group):
     assert torch.isnan(c.out).all() and torch.isnan(c.lse).all()
 
 
-def test_a_plan_of_another_call():
+@pytest.mark.parametrize("extra_keep", [0, CUT])
+def test_a_plan_of_another_call(extra_keep):
     announce("plan of another call")
-    c = Case(11, [(50, [10, 0, 5])], NL=2)
+    c = Case(11, [(50, [10, 0, 5])], NL=2, extra_keep=extra_keep)
     for fill in (0, -1):
         c.plan.fill_(fill)
         c.attend()
@@ -275,9 +288,10 @@ def test_a_plan_of_another_call():
     c.check()
 
 
-def test_sequences_behind_the_last_group_and_empty_groups():
+@pytest.mark.parametrize("extra_keep", [0, CUT])
+def test_sequences_behind_the_last_group_and_empty_groups(extra_keep):
     announce("sequences behind the last group, empty groups")
-    c = Case(12, [(0, []), (50, [10, 0, 5]), (0, []), (20, [3, 2]), (0, [])], spare=3)
+    c = Case(12, [(0, []), (50, [10, 0, 5]), (0, []), (20, [3, 2]), (0, [])], spare=3, extra_keep=extra_keep)
     c.make_plan()
     c.attend(lse=False)
     torch.cuda.synchronize()
@@ -288,7 +302,8 @@ def test_sequences_behind_the_last_group_and_empty_groups():
     assert M.murmur_device_error() == 0
 
 
-def test_ranges_of_sequence_ordered_caches():
+@pytest.mark.parametrize("extra_keep", [0, CUT])
+def test_ranges_of_sequence_ordered_caches(extra_keep):
     """Chunks with caches of their own behind one prompt, from range tables; what is shared is read from the first
     one's cache only (the others' copies are NaN)."""
     announce("range tables")
@@ -299,7 +314,7 @@ def test_ranges_of_sequence_ordered_caches():
                     np.array([20, -1, 8, 5, -1, 30, 11]), rng.integers(0, 3, B)], 1).astype(np.int32)
     L = (int(seg.sum(1).max()) + 7) // 8 * 8
     idx, cnt = oracle.retained(seg, pol)
-    keep = idx.shape[1]
+    keep = idx.shape[1] + extra_keep
     q, k, v = bf16(rng, NL, B, hq, D), bf16(rng, NL, B, hkv, L, D), bf16(rng, NL, B, hkv, L, D)
     group, shared = i32([0, 4, 7]), i32([prompt, prompt - 5])
     for x in (k, v):
@@ -331,11 +346,12 @@ def test_ranges_of_sequence_ordered_caches():
                 assert (np.abs(lse[layer, b].cpu().numpy() - want_lse) <= far_lse).all(), (b, layer)
 
 
-def test_same_bits_every_run_and_replay():
+@pytest.mark.parametrize("extra_keep", [0, CUT])
+def test_same_bits_every_run_and_replay(extra_keep):
     """Eager runs, runs on another stream and graph replays (plan and attention captured) give the same bits, and a
     graph replayed after the lists have changed follows them."""
     announce("replays")
-    c = Case(14, [(600, [30, 1, 0, 90]), (80, [3] * 6)], NL=2)
+    c = Case(14, [(600, [30, 1, 0, 90]), (80, [3] * 6)], NL=2, extra_keep=extra_keep)
     c.make_plan()
     c.attend()
     c.check()
@@ -367,10 +383,11 @@ def test_same_bits_every_run_and_replay():
     assert c.shared.cpu().tolist() == [100, 80]
 
 
-def test_two_calls_at_once():
+@pytest.mark.parametrize("extra_keep", [0, CUT])
+def test_two_calls_at_once(extra_keep):
     """Two streams, one plan, a workspace each."""
     announce("two calls at once")
-    c = Case(15, [(900, [30, 1, 0, 90])], NL=2)
+    c = Case(15, [(900, [30, 1, 0, 90])], NL=2, extra_keep=extra_keep)
     c.make_plan()
     c.attend()
     c.check()
@@ -388,11 +405,12 @@ def test_two_calls_at_once():
     assert all(torch.equal(o, want) for o in outs)
 
 
-def test_a_pool_past_2_gib():
+@pytest.mark.parametrize("extra_keep", [0, CUT])
+def test_a_pool_past_2_gib(extra_keep):
     """Rows whose offsets pass 32 bits, in bytes and in elements."""
     announce("offsets past 32 bits")
     rows, hkv = (1 << 32) // (4 * D) + 4096, 4
-    c = Case(16, [(40, [10, 3])])
+    c = Case(16, [(40, [10, 3])], extra_keep=extra_keep)
     k, v = (torch.empty((1, rows, hkv, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
     far = np.random.default_rng(1).permutation(rows - c.rows)[:c.rows]
     far[:c.rows // 2] = rows - 1 - np.arange(c.rows // 2)  # half of them at the end
