@@ -93,6 +93,19 @@ struct PlanLds {
     int scan[16], work[kSharedLevels + 1], bad;
     unsigned positions;
 };
+// Workgroups that read the same rows should share an L2.  Workgroup w of a launch runs
+// on XCD w mod 8, and the (layer, KV head) is the fastest index of the grid, so with
+// `heads` of them item i of a head runs on one of 8 / gcd(8, heads) XCDs in turn.  Item
+// number q of n, in an order with neighbours that share rows, goes to the place that
+// gives every such XCD a run of neighbours (a bijection of [0, n)).
+static __device__ __forceinline__ int item_place(int q, int n, int heads) {
+    const int xcds = heads % 8 == 0 ? 1 : (heads % 4 == 0 ? 2 : (heads % 2 == 0 ? 4 : 8));
+    const int per = div_up(n, xcds), tall = n - xcds * (per - 1);  // the first `tall` runs have `per`, the others one less
+    const int x = q < tall * per ? q / per : tall + (q - tall * per) / max(per - 1, 1);
+    const int first = x * (per - 1) + min(x, tall);
+    return (q - first) * xcds + x;
+}
+
 // The plan where no list is cut: a workgroup per (layer, KV head) and some sequences
 // of a group, with one, two or three row tiles, whichever is estimated fastest (in
 // tenths of a pass with one tile; measured: a pass takes half as long again with
@@ -153,7 +166,8 @@ static __device__ __forceinline__ void plan_whole(const SharedPlanLaunch &p, Pla
         const int lo = l.lo[g], n = l.lo[g + 1] - lo, parts = div_up(n, per);
         for (int i = lane; i < parts; i += 64) {
             const int s0 = n * i / parts, s1 = n * (i + 1) / parts;
-            items[l.item[g] + i] = PlanItem{lo + s0, s1 - s0, lo, 0, max(l.common[g], 0), 0, stream && parts <= 2, 0};
+            items[item_place(l.item[g] + i, work, heads)] =
+                PlanItem{lo + s0, s1 - s0, lo, 0, max(l.common[g], 0), 0, stream && parts <= 2, 0};
         }
     }
     if (tid == 0) {
@@ -296,7 +310,6 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     }
     __syncthreads();
     const int heads = p.n_layers * p.Hkv;
-    const int apart = heads % 8 == 0 ? 1 : (heads % 4 == 0 ? 2 : (heads % 2 == 0 ? 4 : 8));
     for (int g = wave; g < n_groups; g += kPlanThreads / 64) {
         const int lo = l.lo[g], n = l.lo[g + 1] - lo, common = max(l.common[g], 0), pre = n > 0 ? div_up(common, kWaveTile) : 0;
         const int cuts = div_up(pre, item_passes(level)), parts = div_up(n, per_item);
@@ -304,10 +317,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
             const int cut = i / parts, part = i - cut * parts, s0 = n * part / parts, s1 = n * (part + 1) / parts;
             const int r0 = (int)((int64_t)pre * cut / cuts) * kWaveTile;
             const int r1 = min((int)((int64_t)pre * (cut + 1) / cuts) * kWaveTile, common);
-            // The parts of one stretch read the same rows: they lie `apart` items apart, which puts them on one XCD
-            // (workgroup w of the launch runs on XCD w mod 8), one after the other.
-            const int block = cut / apart, wide = min(apart, cuts - block * apart);
-            items[l.item[g] + block * apart * parts + part * wide + cut % apart] = PlanItem{lo + s0, s1 - s0, lo, r0, r1, l.row[g] + (cut * n + s0) * G,
+            items[item_place(l.item[g] + i, work, heads)] = PlanItem{lo + s0, s1 - s0, lo, r0, r1, l.row[g] + (cut * n + s0) * G,
                          stream && parts <= 2, 0};
         }
     }
@@ -417,10 +427,8 @@ struct RowSource;
 template <>
 struct RowSource<true> {
     __amdgpu_buffer_rsrc_t base;
-    uint32_t row_bytes;
     __device__ __forceinline__ void init(const uint16_t *p, int64_t s_pos, int max_len) {
-        row_bytes = (uint32_t)s_pos * 2u;
-        base = raw_buffer(p, (uint32_t)(max_len - 1) * row_bytes + kTileRowBytes);
+        base = raw_buffer(p, (uint32_t)(max_len - 1) * ((uint32_t)s_pos * 2u) + kTileRowBytes);
     }
     template <int kAux>
     __device__ __forceinline__ void load(uint8_t *tile, const uint32_t (&at)[8]) const {
@@ -447,29 +455,50 @@ struct RowSource<false> {
     }
 };
 
-// What a pass reads from: the list or range table of one sequence, and the K/V of
-// one (layer, KV head) of it.
+// The K/V of one (layer, KV head) of a sequence, and its list or range table.
 template <bool kNear>
 struct Rows {
-    RangeTab tab;
-    __amdgpu_buffer_rsrc_t list;
     RowSource<kNear> k, v;
 };
-template <int kSrc, bool kNear>
+template <bool kNear>
 static __device__ __forceinline__ Rows<kNear> rows_of(const SharedAttnLaunch &a, int list, int layer, int g) {
     Rows<kNear> in;
-    if (kSrc == kSrcIndex) {
-        in.list = raw_buffer(a.idx + (int64_t)list * a.max_keep, (uint32_t)a.max_keep * 4u);
-    } else {
-        int32_t rg[2 * kPieces];
-#pragma unroll
-        for (int k = 0; k < 2 * kPieces; ++k) rg[k] = a.ranges[(int64_t)list * 2 * kPieces + k];
-        in.tab = make_tab(rg);
-    }
     const int64_t off = layer * a.s_layer + list * a.s_b + g * a.s_h;
     in.k.init(a.k + off, a.s_pos, a.max_len);
     in.v.init(a.v + off, a.s_pos, a.max_len);
     return in;
+}
+static __device__ __forceinline__ __amdgpu_buffer_rsrc_t list_of(const SharedAttnLaunch &a, int list) {
+    return raw_buffer(a.idx + (int64_t)list * a.max_keep, (uint32_t)a.max_keep * 4u);
+}
+static __device__ __forceinline__ RangeTab table_of(const SharedAttnLaunch &a, int list) {
+    int32_t rg[2 * kPieces];
+#pragma unroll
+    for (int k = 0; k < 2 * kPieces; ++k) rg[k] = a.ranges[(int64_t)list * 2 * kPieces + k];
+    return make_tab(rg);
+}
+
+// Positions of a pass from its index slot (dma_idx), as dma_pos_index, which a pass
+// that is not full or names a position outside the cache goes to: a full one needs
+// no clamping once all of its positions are known to be inside (5 instructions for
+// the eight of a lane, not 80, in a loop that instruction issue bounds).
+static __device__ __forceinline__ void slot_positions(const uint8_t *slot, int r, int r_end, int max_len, int q,
+                                                      int32_t (&pos)[8], int &bad) {
+    if (r_end - r >= kWaveTile) {
+        u32x4 e0, e1;
+        asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %2 offset:16\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(e0), "=&v"(e1)
+                     : "v"(lds_addr(slot) + 32u * q)
+                     : "memory");
+        uint32_t most = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            pos[j] = (int32_t)(j < 4 ? e0[j] : e1[j - 4]);
+            most = max(most, (uint32_t)pos[j]);
+        }
+        if (__builtin_expect(__ballot(most >= (uint32_t)max_len) == 0, 1)) return;
+    }
+    dma_pos_index(slot, r, r_end, max_len, q, pos, bad);
 }
 
 // A pass: ranks r .. min(r + 32, r_end) - 1 of a sequence's list, for the rows of
@@ -531,17 +560,19 @@ static __device__ __forceinline__ float run_passes(const SharedAttnLaunch &a, in
     int32_t pos[8];
     uint32_t at[8];
     int bad = 0;
-    const auto positions = [&](const Rows<kNear> &in, const Pass &p, int slot) {
-        if (kSrc == kSrcIndex) dma_pos_index(slots[slot], p.r, p.r_end, a.max_len, c4, pos, bad);
-        else dma_pos_ranges(in.tab, p.r, p.r_end, a.max_len, c4, pos, bad);
-        if (__ballot(bad)) {
+    const uint32_t row_bytes = (uint32_t)a.s_pos * 2u;
+    RangeTab tab;
+    const auto positions = [&](const Pass &p, int slot) {
+        if (kSrc == kSrcIndex) slot_positions(slots[slot], p.r, p.r_end, a.max_len, c4, pos, bad);
+        else dma_pos_ranges(tab, p.r, p.r_end, a.max_len, c4, pos, bad);
+        if (__builtin_expect(__ballot(bad) != 0, 0)) {
             on_bad(p);
             bad = 0;
         }
-        if constexpr (kNear) {
+        if constexpr (kNear) {  // positions and row bytes are below 2^24 (see launch_shared_attn)
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                at[j] = (uint32_t)pos[j] * in.k.row_bytes + 16u * (uint32_t)(n16 ^ ((4 * j + c4) & 15));
+                at[j] = __umul24((uint32_t)pos[j], row_bytes) + 16u * (uint32_t)(n16 ^ ((4 * j + c4) & 15));
         }
     };
     const auto load_as = [&](const RowSource<kNear> &from, uint8_t *tile, auto aux) {
@@ -552,17 +583,18 @@ static __device__ __forceinline__ float run_passes(const SharedAttnLaunch &a, in
         if (stream) load_as(from, tile, std::integral_constant<int, kAuxStream>{});
         else load_as(from, tile, std::integral_constant<int, 0>{});
     };
-    Rows<kNear> in = rows_of<kSrc, kNear>(a, cur.list, layer, g), in_next = in;
-    if (!Feed::kOne && more && nxt.list != cur.list) in_next = rows_of<kSrc, kNear>(a, nxt.list, layer, g);
     if (kSrc == kSrcIndex) {
-        dma_idx(slots[0], in.list, cur.r, lane);
-        dma_idx(slots[1], in_next.list, more ? nxt.r : cur.r, lane);
+        dma_idx(slots[0], list_of(a, cur.list), cur.r, lane);
+        dma_idx(slots[1], list_of(a, more ? nxt.list : cur.list), more ? nxt.r : cur.r, lane);
+    } else {
+        tab = table_of(a, cur.list);
     }
+    Rows<kNear> in = rows_of<kNear>(a, cur.list, layer, g);
     asm volatile("" ::: "memory");  // the queries' loads stay behind the entries'
     load_queries();
     // the first slot: the second slot's load and then the queries' came after it
     if (kSrc == kSrcIndex) wait_vm<1 + 4 * kTiles>();
-    positions(in, cur, 0);
+    positions(cur, 0);
     load(in.k, stage);
     load(in.v, stage + kTileBytes);
     float scale = 1.f;
@@ -574,12 +606,17 @@ static __device__ __forceinline__ float run_passes(const SharedAttnLaunch &a, in
         read_k_operands(kf, kt, n16, c4);
         Pass after;
         bool more_after = false;
-        in = in_next;
         if (more) {
-            positions(in, nxt, (it + 1) & 1);  // entries that were loaded before this pass's K rows
+            if (!Feed::kOne) {  // uniform
+                if (kSrc != kSrcIndex && nxt.list != cur.list) tab = table_of(a, nxt.list);
+                in = rows_of<kNear>(a, nxt.list, layer, g);
+            }
+            positions(nxt, (it + 1) & 1);  // entries that were loaded before this pass's K rows
             more_after = feed.next(after);
-            if (!Feed::kOne && more_after && after.list != nxt.list) in_next = rows_of<kSrc, kNear>(a, after.list, layer, g);
-            if (kSrc == kSrcIndex) dma_idx(slots[it & 1], in_next.list, more_after ? after.r : nxt.r, lane);
+            if (kSrc == kSrcIndex) {
+                const Pass &x = more_after ? after : nxt;
+                dma_idx(slots[it & 1], list_of(a, x.list), x.r, lane);
+            }
             load(in.k, stage);
         }
         const int valid = min(kWaveTile, cur.r_end - cur.r);
@@ -593,7 +630,8 @@ static __device__ __forceinline__ float run_passes(const SharedAttnLaunch &a, in
 #pragma unroll
                 for (int kc = 0; kc < 4; ++kc) s[blk] = mfma16x16x32(kf[4 * blk + kc], qf[t][kc], s[blk]);
             }
-            if (!Feed::kOne && cur.only >= 0) {  // uniform
+            if (!Feed::kOne && cur.only >= 0) {
+                asm volatile("");  // a branch, which few passes take, rather than selects in every pass
                 const bool mine = row_seq[t] == cur.only;
 #pragma unroll
                 for (int blk = 0; blk < 2; ++blk)
@@ -1036,7 +1074,9 @@ static void launch_shared_attn_near(const SharedAttnLaunch &a, hipStream_t strea
 
 template <int kSrc>
 static void launch_shared_attn(const SharedAttnLaunch &a, hipStream_t stream) {
-    const bool near = (__int128)(a.max_len - 1) * a.s_pos * 2 + kTileRowBytes < ((__int128)1 << 32);
+    // rows of at least 256 bytes (one if the cache has one row) within 2^32: positions below 2^24
+    const bool near = a.s_pos < kRunRowLimit && (a.s_pos >= kHeadDim || a.max_len == 1) &&
+                      (__int128)(a.max_len - 1) * a.s_pos * 2 + kTileRowBytes < ((__int128)1 << 32);
     if (near) launch_shared_attn_near<kSrc, true>(a, stream);
     else launch_shared_attn_near<kSrc, false>(a, stream);
 }
