@@ -541,6 +541,52 @@ struct WholeLists {  // every step-th pass of an item: those of the prefix, then
 // leaves out entirely (every logit -inf) stays as it is: exp2 of -inf, not of NaN.
 constexpr float kNoRows = -3.0e38f;
 
+// A pass of one sequence's rest is multiplied with the rows of other sequences too,
+// whose weights are zero, but zero times an infinity or a NaN is NaN.  Where the
+// values hold one (the product with zeros tells), they are taken out of the tile
+// and added to the sums of the sequence itself, whose result is not finite there
+// whatever its weights.
+template <int kTiles>
+static __device__ __forceinline__ void keep_apart(u32x2 (&vf)[16], uint8_t *tile, int valid, int only,
+                                                  const int (&row_seq)[kTiles], WaveAcc (&w)[kTiles], int lane) {
+    const int c4 = lane >> 4;
+    f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int db = 0; db < 8; ++db)
+        zero = mfma16x16x32(u32x4{vf[2 * db][0], vf[2 * db][1], vf[2 * db + 1][0], vf[2 * db + 1][1]}, u32x4{0u, 0u, 0u, 0u}, zero);
+    if (__builtin_expect(__ballot(zero[0] + zero[1] + zero[2] + zero[3] != 0.f) == 0, 1)) return;
+    // 0xffff in the halves of x whose exponent is all ones
+    const auto not_finite = [](uint32_t x) { return ((((x & 0x7f807f80u) + 0x00800080u) >> 15) & 0x00010001u) * 0xffffu; };
+#pragma unroll
+    for (int db = 0; db < 8; ++db) {
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+        for (int r = 0; r < valid; ++r) {
+            u32x2 e = *reinterpret_cast<const u32x2 *>(tile + r * kTileRowBytes + (((2 * db + (c4 >> 1)) ^ (r & 15)) << 4) +
+                                                       8 * (c4 & 1));
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                e[i] &= not_finite(e[i]);
+                sum[2 * i] += __builtin_bit_cast(float, e[i] << 16);
+                sum[2 * i + 1] += __builtin_bit_cast(float, e[i] & 0xffff0000u);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[t].acc[db][i] += row_seq[t] == only ? sum[i] : 0.f;
+    }
+#pragma unroll 1
+    for (int i = lane; i < kTileBytes / 16; i += 64) {
+        u32x4 e = *reinterpret_cast<const u32x4 *>(tile + 16 * i);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) e[x] &= ~not_finite(e[x]);
+        *reinterpret_cast<u32x4 *>(tile + 16 * i) = e;
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    read_v_operands(vf, lds_addr(tile), lane & 15, c4);
+}
+
 // The passes of `feed` against kTiles row tiles.  load_queries starts the loads of
 // the queries (4 kTiles of them) into qf.  row_seq: which of the item's sequences
 // the lane's row of a tile belongs to (several lists only).  on_bad(pass) is called
@@ -644,6 +690,7 @@ static __device__ __forceinline__ float run_passes(const SharedAttnLaunch &a, in
         if (more) wait_vm<8>();  // this pass's V rows; the next pass's K rows came after them
         else wait_vm<0>();
         read_v_operands(vf, vt, n16, c4);
+        if (!Feed::kOne && cur.only >= 0) keep_apart<kTiles>(vf, stage + kTileBytes, valid, cur.only, row_seq, w, lane);
         if (more) load(in.v, stage + kTileBytes);
 #pragma unroll
         for (int db = 0; db < 8; ++db) {

@@ -208,6 +208,35 @@ def test_shares_given_by_the_caller(extra_keep):
 
 
 @pytest.mark.parametrize("extra_keep", [0, CUT])
+@pytest.mark.parametrize("hq,hkv", [(28, 4), (16, 1), (3, 3)])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+def test_values_that_are_not_finite_stay_with_their_sequence(value, hq, hkv, extra_keep):
+    announce(f"infinities and NaN in one sequence's own rows: {value} Hq {hq} Hkv {hkv} keep + {extra_keep}")
+    c = Case(8, [(70, [40, 33, 5, 1]), (20, [64, 1, 90, 33])], hq=hq, hkv=hkv, extra_keep=extra_keep)
+    c.make_plan()
+    c.attend()
+    c.check()
+    clean, lse = c.out.clone(), c.lse.clone()
+    dims, hit = [3, 64, 127], [1, 6]
+    for b in hit:
+        for at in (c.lists[b][-1], c.lists[b][-20]):
+            c.v[0, at][:, dims] = value
+    c.attend()
+    torch.cuda.synchronize()
+    others = [b for b in range(c.B) if b not in hit]
+    assert torch.equal(c.out[:, others], clean[:, others]) and torch.equal(c.lse, lse)
+    kept = [d for d in range(D) if d not in dims]
+    assert torch.equal(c.out[:, hit][..., kept], clean[:, hit][..., kept])
+    assert not torch.isfinite(c.out[:, hit][..., dims]).any()
+    for b in hit:
+        c.k[0, c.lists[b][-1]] = float("nan")
+    c.attend()
+    torch.cuda.synchronize()
+    assert torch.equal(c.out[:, others], clean[:, others]) and torch.equal(c.lse[:, others], lse[:, others])
+    assert torch.isnan(c.out[:, hit]).all()
+
+
+@pytest.mark.parametrize("extra_keep", [0, CUT])
 def test_bad_counts(extra_keep):
     """A count of zero or above max_keep is the sequence's own error; the others share as if it were not there."""
     announce("bad counts")
