@@ -231,7 +231,7 @@ int launch_paged_compact(int32_t B, int32_t *bt, int32_t max_blocks, int32_t log
 //     first one, per kScanLen entries.
 // n_wg bounds the workgroups of a (layer, KV head) whatever the lists hold (see
 // shared_caps).
-constexpr int kSharedWaves = 4;       // of a workgroup, two of which share a compute unit
+constexpr int kSharedWaves = 8;       // of a workgroup, which has a compute unit to itself
 constexpr int kSharedRows = 48;       // query rows of one prefix item: three MFMA row tiles
 constexpr int kSharedMaxSeqs = 4096;  // sequences of a batch (the planner's LDS)
 // A cut of the work at level j = 1 .. kSharedLevels gives a wavefront of a prefix

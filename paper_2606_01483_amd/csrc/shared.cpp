@@ -117,7 +117,7 @@ int check_shared_sizes(int32_t n_layers, int32_t B, int32_t Hq, int32_t Hkv, int
 }  // namespace
 
 // Bounds of any plan for these sizes.  A plan that fits one dispatch round has at
-// most per_round workgroups per (layer, KV head) (two share a compute unit), each
+// most per_round workgroups per (layer, KV head) (one on a compute unit), each
 // with at most kSharedRows partial rows of a prefix.  Any other is cut at the highest level: a group of n
 // sequences has at most n / (sequences per item) + 1 sets of rows, each list at most
 // max_keep entries.  Each sequence's rest has a partial per workgroup that it
@@ -130,7 +130,7 @@ SharedCaps shared_caps(int32_t n_layers, int32_t B, int32_t Hq, int32_t Hkv, int
     const int64_t cuts = div_up(passes, kSharedWaves * kSharedLevels);
     const int64_t chunks = div_up(passes, kSharedLevels + kSharedLevels / 2);
     const int64_t sets = n_groups + B / (kSharedRows / G);
-    c.per_round = (int32_t)std::max<int64_t>(1, 2 * kRoundWorkgroups / heads);
+    c.per_round = (int32_t)std::max<int64_t>(1, kRoundWorkgroups / heads);
     const int64_t longest = sets * cuts + div_up(B * chunks, kSharedWaves);
     c.n_wg = (int32_t)std::min<int64_t>(std::max<int64_t>(c.per_round, longest), 0x7fffffff);
     c.rows = std::max<int64_t>((int64_t)c.per_round * kSharedRows, B * G * cuts) + G * (B + (int64_t)c.n_wg);
