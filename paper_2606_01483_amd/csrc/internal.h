@@ -234,10 +234,12 @@ int launch_paged_compact(int32_t B, int32_t *bt, int32_t max_blocks, int32_t log
 constexpr int kSharedWaves = 8;       // of a workgroup, which has a compute unit to itself
 constexpr int kSharedRows = 48;       // query rows of one prefix item: three MFMA row tiles
 constexpr int kSharedMaxSeqs = 4096;  // sequences of a batch (the planner's LDS)
-// A cut of the work at level j = 1 .. kSharedLevels gives a wavefront of a prefix
-// item up to j passes of kWaveTile positions and one of a rest up to j + j / 2 (it
-// has one row tile).
-constexpr int kSharedLevels = 16;
+// A cut of the work at level j = 4 .. kSharedLevels gives the wavefronts of a prefix
+// item j / 4 passes of kWaveTile positions on average and one of a rest up to 3 j / 8
+// (it has one row tile).
+constexpr int kSharedLevels = 64;
+constexpr int item_passes(int level) { return kSharedWaves * level / 4; }
+constexpr int chunk_passes(int level) { return level * 3 / 8; }
 constexpr int kScanLen = 4096;
 constexpr int32_t kPlanMagic = 0x6d75726d;
 struct PlanHeader {

@@ -127,8 +127,8 @@ SharedCaps shared_caps(int32_t n_layers, int32_t B, int32_t Hq, int32_t Hkv, int
     const int64_t G = Hq / Hkv, heads = (int64_t)n_layers * Hkv;
     const auto div_up = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
     const int64_t passes = div_up(max_keep, kWaveTile);
-    const int64_t cuts = div_up(passes, kSharedWaves * kSharedLevels);
-    const int64_t chunks = div_up(passes, kSharedLevels + kSharedLevels / 2);
+    const int64_t cuts = div_up(passes, item_passes(kSharedLevels));
+    const int64_t chunks = div_up(passes, chunk_passes(kSharedLevels));
     const int64_t sets = n_groups + B / (kSharedRows / G);
     c.per_round = (int32_t)std::max<int64_t>(1, kRoundWorkgroups / heads);
     const int64_t longest = sets * cuts + div_up(B * chunks, kSharedWaves);

@@ -75,22 +75,36 @@ __global__ __launch_bounds__(kScanThreads) void shared_scan_kernel(const int32_t
 
 static __device__ __forceinline__ int div_up(int x, int y) { return (x + y - 1) / y; }
 
-// Of a cut at some level: passes that one workgroup takes of a prefix, and one
-// wavefront of a rest.
-static __device__ __forceinline__ int item_passes(int level) { return kSharedWaves * level; }
-static __device__ __forceinline__ int chunk_passes(int level) { return level + level / 2; }
+// x / y for 0 <= x < 2^22 and y >= 1: the estimate is off by one at most.
+static __device__ __forceinline__ int small_div(int x, int y) {
+    int q = (int)((float)x * __builtin_amdgcn_rcpf((float)y));
+    const int r = x - q * y;
+    q += r >= y ? 1 : 0;
+    return r < 0 ? q - 1 : q;
+}
+static __device__ __forceinline__ int small_div_up(int x, int y) { return small_div(x + y - 1, y); }
+// n things dealt to `parts` parts in runs: the first of part i.
+struct Dealt {
+    int per, more;
+    __device__ __forceinline__ Dealt(int n, int parts) : per((int)((unsigned)n / (unsigned)parts)), more(n - per * parts) {}
+    __device__ __forceinline__ int start(int i) const { return per * i + min(i, more); }
+};
 
 // One workgroup; what it needs of every sequence and group is in LDS, so that the
-// global round trips are the counts with the groups, and the stores.  The lowest
-// level of cut whose workgroups fit one dispatch round is taken (the wavefronts add
-// them up side by side), or the highest.
+// global round trips are the counts with the groups, the scans, and the stores.  It
+// runs each line once, on code that no cache holds yet, so what bounds it is the
+// size of the code (loops are not unrolled, divisions are by reciprocal): 17 KB
+// took 9.1 us for 96 sequences.  The lowest level of cut whose workgroups fit one
+// dispatch round is taken, or the highest; the wavefronts add up eight levels side
+// by side, then the eight between two of them.
 struct PlanLds {
     int rest[kSharedMaxSeqs];           // by sequence: length of the rest, -1 if the sequence is left out
     uint16_t of[kSharedMaxSeqs];        // its group
     int lo[kSharedMaxSeqs + 1];         // by group: first sequence
     int common[kSharedMaxSeqs];         // what it shares
     int row[kSharedMaxSeqs], item[kSharedMaxSeqs];  // its first partial row and item
-    int scan[16], work[kSharedLevels + 1], bad;
+    int cuts[kSharedMaxSeqs];
+    int scan[16], work[2][8], bad;
     unsigned positions;
 };
 // Workgroups that read the same rows should share an L2.  Workgroup w of a launch runs
@@ -99,9 +113,9 @@ struct PlanLds {
 // number q of n, in an order with neighbours that share rows, goes to the place that
 // gives every such XCD a run of neighbours (a bijection of [0, n)).
 static __device__ __forceinline__ int item_place(int q, int n, int heads) {
-    const int xcds = heads % 8 == 0 ? 1 : (heads % 4 == 0 ? 2 : (heads % 2 == 0 ? 4 : 8));
-    const int per = div_up(n, xcds), tall = n - xcds * (per - 1);  // the first `tall` runs have `per`, the others one less
-    const int x = q < tall * per ? q / per : tall + (q - tall * per) / max(per - 1, 1);
+    const int log2 = 3 - min(3, __ffs(heads) - 1), xcds = 1 << log2;
+    const int per = (n + xcds - 1) >> log2, tall = n - xcds * (per - 1);  // the first `tall` runs have `per`, the others one less
+    const int x = q < tall * per ? small_div(q, per) : tall + small_div(q - tall * per, max(per - 1, 1));
     const int first = x * (per - 1) + min(x, tall);
     return (q - first) * xcds + x;
 }
@@ -113,10 +127,12 @@ static __device__ __forceinline__ int item_place(int q, int n, int heads) {
 template <int kPlanThreads>
 static __device__ __forceinline__ void plan_whole(const SharedPlanLaunch &p, PlanLds &l, PlanHeader *h, PlanSeq *seqs,
                                                   PlanItem *items, int end, int stream, int tid) {
-    const int n_groups = p.n_groups, G = p.Hq / p.Hkv, lane = tid & 63, wave = tid >> 6;
+    const int n_groups = p.n_groups, G = small_div(p.Hq, p.Hkv), lane = tid & 63, wave = tid >> 6;
     const int heads = p.n_layers * p.Hkv, waves = p.caps.waves, slots = waves == 8 ? kRoundWorkgroups : 2 * kRoundWorkgroups;
+#pragma unroll 1
     for (int g = tid; g < n_groups; g += kPlanThreads) l.row[g] = 0;
     __syncthreads();
+#pragma unroll 1
     for (int b = tid; b < p.B; b += kPlanThreads) {
         const int rest = b < end ? max(l.rest[b], 0) : 0;
         if (b < end) {
@@ -129,43 +145,50 @@ static __device__ __forceinline__ void plan_whole(const SharedPlanLaunch &p, Pla
     }
     __syncthreads();
     if (wave < 3) {
-        const int per = 16 * (wave + 1) / G;
+        const int per = small_div(16 * (wave + 1), G);
         int wg = 0, sum = 0, most = 0;
+#pragma unroll 1
         for (int g = lane; per > 0 && g < n_groups; g += 64) {
-            const int n = l.lo[g + 1] - l.lo[g], parts = div_up(n, per);
+            const int n = l.lo[g + 1] - l.lo[g], parts = small_div_up(n, per);
             if (n == 0) continue;
-            const int cost = 60 + (10 + 5 * wave) * div_up(div_up(max(l.common[g], 0), kWaveTile) + div_up(l.row[g], parts), waves);
+            const int rounds = (div_up(max(l.common[g], 0), kWaveTile) + (int)((unsigned)l.row[g] / (unsigned)parts)) / (waves == 8 ? 8 : 4) + 1;
+            const int cost = 60 + (10 + 5 * wave) * rounds;
             wg += parts;
             sum += parts * min(cost, 1 << 18);
             most = max(most, cost);
         }
-#pragma unroll
+#pragma unroll 1
         for (int x = 32; x >= 1; x /= 2) {
             wg += __shfl_xor(wg, x);
             sum += __shfl_xor(sum, x);
             most = max(most, __shfl_xor(most, x));
         }
         if (lane == 0)
-            l.work[wave] = per == 0 ? 0x7fffffff
-                                    : (int)min<int64_t>(0x7ffffffe, (int64_t)most + ((int64_t)wg * heads > slots ? (int64_t)sum * heads / slots : 0));
+            l.work[0][wave] = per == 0 ? 0x7fffffff
+                                    : (int)min<int64_t>(0x7ffffffe, (int64_t)most + ((int64_t)wg * heads > slots ? (int64_t)((uint64_t)((int64_t)sum * heads) / kRoundWorkgroups / (waves == 8 ? 1 : 2)) : 0));
     }
     __syncthreads();
     int tiles = 0;
-    for (int i = 1; i < 3; ++i) tiles = l.work[i] < l.work[tiles] ? i : tiles;
-    const int per = 16 * (tiles + 1) / G;
+#pragma unroll 1
+    for (int i = 1; i < 3; ++i) tiles = l.work[0][i] < l.work[0][tiles] ? i : tiles;
+    const int per = small_div(16 * (tiles + 1), G);
     int work = 0;
+#pragma unroll 1
     for (int g0 = 0; g0 < n_groups; g0 += kPlanThreads) {
         const int g = g0 + tid, n = g < n_groups ? l.lo[g + 1] - l.lo[g] : 0;
         int total;
-        const int at = work + wg_exclusive_scan<kPlanThreads>(div_up(n, per), l.scan, tid, total);
+        const int at = work + wg_exclusive_scan<kPlanThreads>(small_div_up(n, per), l.scan, tid, total);
         work += total;
         if (g < n_groups) l.item[g] = at;
     }
     __syncthreads();
+#pragma unroll 1
     for (int g = wave; g < n_groups; g += kPlanThreads / 64) {
-        const int lo = l.lo[g], n = l.lo[g + 1] - lo, parts = div_up(n, per);
+        const int lo = l.lo[g], n = l.lo[g + 1] - lo, parts = small_div_up(n, per);
+        const Dealt dealt(n, max(parts, 1));
+#pragma unroll 1
         for (int i = lane; i < parts; i += 64) {
-            const int s0 = n * i / parts, s1 = n * (i + 1) / parts;
+            const int s0 = dealt.start(i), s1 = dealt.start(i + 1);
             items[item_place(l.item[g] + i, work, heads)] =
                 PlanItem{lo + s0, s1 - s0, lo, 0, max(l.common[g], 0), 0, stream && parts <= 2, 0};
         }
@@ -182,7 +205,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     __shared__ PlanLds l;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int B = p.B, n_groups = p.n_groups, max_keep = p.max_keep;
-    const int G = p.Hq / p.Hkv, per_item = kSharedRows / G;
+    const int G = small_div(p.Hq, p.Hkv), per_item = small_div(kSharedRows, G);
     PlanHeader *h = reinterpret_cast<PlanHeader *>(p.plan);
     PlanSeq *seqs = reinterpret_cast<PlanSeq *>(p.plan + sizeof(PlanHeader));
     PlanItem *items = reinterpret_cast<PlanItem *>(p.plan + p.caps.item_offset);
@@ -192,10 +215,14 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
 
     // the groups, and every sequence's count (in `rest` for now)
     if (tid == 0) l.bad = l.positions = 0;
+#pragma unroll 1
     for (int b = tid; b < B; b += kPlanThreads) l.rest[b] = list_count(p.ranges, p.count, b);
+#pragma unroll 1
     for (int g = tid; g <= n_groups; g += kPlanThreads) l.lo[g] = p.group[g];
+#pragma unroll 1
     for (int g = tid; g < n_groups; g += kPlanThreads) l.common[g] = p.find ? max_keep : p.shared[g];
     __syncthreads();
+#pragma unroll 1
     for (int g = tid; g < n_groups; g += kPlanThreads)
         if (l.lo[g] < 0 || l.lo[g] > l.lo[g + 1] || l.lo[g + 1] > B || (g == 0 && l.lo[0] != 0)) l.bad = 1;
     __syncthreads();
@@ -217,27 +244,30 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     if (bad) return;
 
     // a sequence's group: the last one that starts at or before it and is not empty
+#pragma unroll 1
     for (int b = tid; b < end; b += kPlanThreads) {
         int lo = 0, hi = n_groups;  // l.lo[lo] <= b < l.lo[hi]
+#pragma unroll 1
         while (hi - lo > 1) {
             const int mid = (lo + hi) / 2;
             if (l.lo[mid] <= b) lo = mid;
             else hi = mid;
         }
         l.of[b] = (uint16_t)lo;
-        if (p.find) {
-            const int c = l.rest[b];
-            if (c >= 1 && c <= max_keep) {
-                int least = c;
-                for (int x = 0; x < n_scan; ++x) least = min(least, scan[(int64_t)b * n_scan + x]);
-                atomicMin(&l.common[lo], least);
-            } else if (b == l.lo[lo]) {
-                atomicMin(&l.common[lo], 0);
-            }
-        }
+        const int c = l.rest[b];
+        if (p.find && ((c >= 1 && c <= max_keep) || b == l.lo[lo])) atomicMin(&l.common[lo], max(c, 0));
     }
     __syncthreads();
+    if (p.find) {
+#pragma unroll 1
+        for (int t = tid; t < end * n_scan; t += kPlanThreads) {  // below 2^29
+            const int b = (int)((unsigned)t / (unsigned)n_scan), c = l.rest[b];
+            if (c >= 1 && c <= max_keep) atomicMin(&l.common[l.of[b]], scan[t]);
+        }
+        __syncthreads();
+    }
     // what is shared has to be in the group's first list, which is the one that is read (-1: it is not)
+#pragma unroll 1
     for (int g = tid; g < n_groups; g += kPlanThreads) {
         const int lo = l.lo[g];
         int common = lo < l.lo[g + 1] ? l.common[g] : 0;
@@ -247,6 +277,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     }
     __syncthreads();
     int err = 0;
+#pragma unroll 1
     for (int b = tid; b < B; b += kPlanThreads) {
         const int c = l.rest[b], common = b < end ? l.common[l.of[b]] : 0;
         const bool good = c >= 1 && c <= max_keep && common >= 0 && c >= common;
@@ -260,9 +291,11 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     int stream;
     {  // positions that a layer reads
         int n = 0;
+#pragma unroll 1
         for (int g = tid; g < n_groups; g += kPlanThreads) n += max(l.common[g], 0);
+#pragma unroll 1
         for (int b = tid; b < end; b += kPlanThreads) n += max(l.rest[b], 0);
-#pragma unroll
+#pragma unroll 1
         for (int x = 32; x >= 1; x /= 2) n += __shfl_xor(n, x);
         if (lane == 0) atomicAdd(&l.positions, (unsigned)min(n, 1 << 24));
         __syncthreads();
@@ -273,50 +306,65 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
         return;
     }
 
-    for (int level = wave + 1; level <= kSharedLevels; level += kPlanThreads / 64) {
-        int wg = 0, waves = 0;
-        for (int g = lane; g < n_groups; g += 64) {
-            const int n = l.lo[g + 1] - l.lo[g], pre = div_up(max(l.common[g], 0), kWaveTile);
-            wg += div_up(n, per_item) * div_up(pre, item_passes(level));
+    int level = 0;
+#pragma unroll 1
+    for (int round = 0; round < 2; ++round) {
+        const auto candidate = [&](int k) { return min(round == 0 ? 4 + 8 * k : max(level - 7 + k, 4), kSharedLevels); };
+#pragma unroll 1
+        for (int k = wave; k < 8; k += kPlanThreads / 64) {
+            const unsigned item = item_passes(candidate(k)), chunk = chunk_passes(candidate(k));
+            int wg = 0, waves = 0;
+#pragma unroll 1
+            for (int g = lane; g < n_groups; g += 64) {
+                const int n = l.lo[g + 1] - l.lo[g], pre = div_up(max(l.common[g], 0), kWaveTile);
+                wg += small_div_up(n, per_item) * (int)((pre + item - 1) / item);
+            }
+#pragma unroll 1
+            for (int b = lane; b < end; b += 64) waves += (int)((div_up(max(l.rest[b], 0), kWaveTile) + chunk - 1) / chunk);
+#pragma unroll 1
+            for (int x = 32; x >= 1; x /= 2) {
+                wg += __shfl_xor(wg, x);
+                waves += __shfl_xor(waves, x);
+            }
+            if (lane == 0) l.work[round][k] = wg + div_up(waves, kSharedWaves);
         }
-        for (int b = lane; b < end; b += 64)
-            waves += div_up(div_up(max(l.rest[b], 0), kWaveTile), chunk_passes(level));
-#pragma unroll
-        for (int x = 32; x >= 1; x /= 2) {
-            wg += __shfl_xor(wg, x);
-            waves += __shfl_xor(waves, x);
-        }
-        if (lane == 0) l.work[level] = wg + div_up(waves, kSharedWaves);
+        __syncthreads();
+        int k = 0;
+#pragma unroll 1
+        while (k < 8 && l.work[round][k] > p.caps.per_round) ++k;
+        level = round == 0 ? 4 + 8 * k : candidate(min(k, 7));
     }
-    __syncthreads();
-    int level = 1;
-    while (level < kSharedLevels && l.work[level] > p.caps.per_round) ++level;
 
     // Prefix work: the groups' items one after the other, the row tiles of one stretch side by side.
     int work = 0, rows = 0;
+#pragma unroll 1
     for (int g0 = 0; g0 < n_groups; g0 += kPlanThreads) {
         const int g = g0 + tid;
         const int n = g < n_groups ? l.lo[g + 1] - l.lo[g] : 0, pre = n > 0 ? div_up(max(l.common[g], 0), kWaveTile) : 0;
-        const int cuts = div_up(pre, item_passes(level));
+        const int cuts = (int)((unsigned)(pre + item_passes(level) - 1) / (unsigned)item_passes(level));
         int total;
-        const int at = work + wg_exclusive_scan<kPlanThreads>(div_up(n, per_item) * cuts, l.scan, tid, total);
+        const int at = work + wg_exclusive_scan<kPlanThreads>(small_div_up(n, per_item) * cuts, l.scan, tid, total);
         work += total;
         const int row = rows + wg_exclusive_scan<kPlanThreads>(cuts * n * G, l.scan, tid, total);
         rows += total;
         if (g < n_groups) {
             l.item[g] = at;
             l.row[g] = row;
+            l.cuts[g] = cuts;
         }
     }
     __syncthreads();
     const int heads = p.n_layers * p.Hkv;
+#pragma unroll 1
     for (int g = wave; g < n_groups; g += kPlanThreads / 64) {
         const int lo = l.lo[g], n = l.lo[g + 1] - lo, common = max(l.common[g], 0), pre = n > 0 ? div_up(common, kWaveTile) : 0;
-        const int cuts = div_up(pre, item_passes(level)), parts = div_up(n, per_item);
+        const int cuts = l.cuts[g], parts = small_div_up(n, per_item);
+        const Dealt to_parts(n, max(parts, 1)), to_cuts(pre, max(cuts, 1));
+#pragma unroll 1
         for (int i = lane; i < cuts * parts; i += 64) {
-            const int cut = i / parts, part = i - cut * parts, s0 = n * part / parts, s1 = n * (part + 1) / parts;
-            const int r0 = (int)((int64_t)pre * cut / cuts) * kWaveTile;
-            const int r1 = min((int)((int64_t)pre * (cut + 1) / cuts) * kWaveTile, common);
+            const int cut = small_div(i, parts), part = i - cut * parts;
+            const int s0 = to_parts.start(part), s1 = to_parts.start(part + 1);
+            const int r0 = to_cuts.start(cut) * kWaveTile, r1 = min(to_cuts.start(cut + 1) * kWaveTile, common);
             items[item_place(l.item[g] + i, work, heads)] = PlanItem{lo + s0, s1 - s0, lo, r0, r1, l.row[g] + (cut * n + s0) * G,
                          stream && parts <= 2, 0};
         }
@@ -325,9 +373,11 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     // workgroup's chunks of one sequence end in one partial.
     const int chunk0 = work * kSharedWaves, each = chunk_passes(level);
     int done = 0;
+#pragma unroll 1
     for (int b0 = 0; b0 < B; b0 += kPlanThreads) {
         const int b = b0 + tid;
-        const int rest = b < end ? max(l.rest[b], 0) : 0, pre = div_up(rest, kWaveTile), n = div_up(pre, each);
+        const int rest = b < end ? max(l.rest[b], 0) : 0, pre = div_up(rest, kWaveTile);
+        const int n = (int)((unsigned)(pre + each - 1) / (unsigned)each);
         int total;
         const int at = done + wg_exclusive_scan<kPlanThreads>(n, l.scan, tid, total);
         done += total;
@@ -336,9 +386,10 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
         rows += total;
         if (b >= end) continue;
         const int g = l.of[b], lo = l.lo[g], n_seq = l.lo[g + 1] - lo, common = max(l.common[g], 0);
+        const Dealt dealt(pre, max(n, 1));
+#pragma unroll 1
         for (int i = 0; i < n; ++i) {
-            const int r0 = (int)((int64_t)pre * i / n) * kWaveTile;
-            const int r1 = min((int)((int64_t)pre * (i + 1) / n) * kWaveTile, rest);
+            const int r0 = dealt.start(i) * kWaveTile, r1 = min(dealt.start(i + 1) * kWaveTile, rest);
             chunks[chunk0 + at + i] = PlanChunk{b, common + r0, common + r1,
                                                 row + ((at + i) / kSharedWaves - at / kSharedWaves) * G};
         }
@@ -346,13 +397,15 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
         s.state = l.rest[b] >= 0 ? 1 : 2;
         s.pre_row = l.row[g] + (b - lo) * G;
         s.pre_stride = n_seq * G;
-        s.n_pre = div_up(div_up(common, kWaveTile), item_passes(level));
+        s.n_pre = l.cuts[g];
         s.rest_row = row;
         s.n_rest = parts;
         seqs[b] = s;
     }
     const int rest_wg = div_up(done, kSharedWaves);
+#pragma unroll 1
     for (int c = done + tid; c < rest_wg * kSharedWaves; c += kPlanThreads) chunks[chunk0 + c] = PlanChunk{-1, 0, 0, 0};
+#pragma unroll 1
     for (int w = tid; w < rest_wg; w += kPlanThreads) items[work + w] = PlanItem{0, 0, 0, 0, 0, 0, stream, 0};
     if (tid == 0) {
         h->n_work = work + rest_wg;
