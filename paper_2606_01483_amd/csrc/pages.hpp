@@ -19,6 +19,30 @@
 
 namespace murmur {
 
+// Sums over the wavefront's lanes up to each one, all lanes active: shifts within the
+// rows of 16 lanes, then the sums of the row and of the two rows before (DPP operands
+// of the adds, where a shuffle is a round trip to LDS).
+static __device__ __forceinline__ int wave_inclusive_scan(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr:1
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31
+    return x;
+}
+static __device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_inclusive_scan(x), 63); }
+// The maximum of values that are not negative.
+static __device__ __forceinline__ int wave_max(int x) {
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
+    return __builtin_amdgcn_readlane(x, 63);
+}
+
 // Loads and stores of words that other workgroups of the launch, or atomics of
 // this one, write: past the caches that are not coherent between XCDs.
 static __device__ __forceinline__ int32_t load_shared_word(const int32_t *p) {
@@ -35,12 +59,7 @@ static __device__ __forceinline__ void add_ref(int32_t *ref, int32_t n) {
 template <int kThreads>
 static __device__ __forceinline__ int wg_exclusive_scan(int v, int *s, int tid, int &total) {
     const int lane = tid & 63, wave = tid >> 6;
-    int x = v;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const int y = __shfl_up(x, off);
-        x += lane >= off ? y : 0;
-    }
+    const int x = wave_inclusive_scan(v);
     if (lane == 63) s[wave] = x;
     __syncthreads();
     int before = 0;

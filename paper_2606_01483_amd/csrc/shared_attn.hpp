@@ -90,6 +90,11 @@ struct Dealt {
     __device__ __forceinline__ int start(int i) const { return per * i + min(i, more); }
 };
 
+// SharedPlanLaunch::find where the planner compares the lists itself: few entries, a
+// load or two of a thread, are cheaper than another launch (4 lists of 266: 2.7 us).
+constexpr int kFindHere = 2;
+constexpr int kFindHereEntries = 4096;
+
 // One workgroup; what it needs of every sequence and group is in LDS, so that the
 // global round trips are the counts with the groups, the scans, and the stores.  It
 // runs each line once, on code that no cache holds yet, so what bounds it is the
@@ -157,12 +162,9 @@ static __device__ __forceinline__ void plan_whole(const SharedPlanLaunch &p, Pla
             sum += parts * min(cost, 1 << 18);
             most = max(most, cost);
         }
-#pragma unroll 1
-        for (int x = 32; x >= 1; x /= 2) {
-            wg += __shfl_xor(wg, x);
-            sum += __shfl_xor(sum, x);
-            most = max(most, __shfl_xor(most, x));
-        }
+        wg = wave_sum(wg);
+        sum = wave_sum(sum);
+        most = wave_max(most);
         if (lane == 0)
             l.work[0][wave] = per == 0 ? 0x7fffffff
                                     : (int)min<int64_t>(0x7ffffffe, (int64_t)most + ((int64_t)wg * heads > slots ? (int64_t)((uint64_t)((int64_t)sum * heads) / kRoundWorkgroups / (waves == 8 ? 1 : 2)) : 0));
@@ -258,7 +260,28 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
         if (p.find && ((c >= 1 && c <= max_keep) || b == l.lo[lo])) atomicMin(&l.common[lo], max(c, 0));
     }
     __syncthreads();
-    if (p.find) {
+    if (p.find == kFindHere) {
+        // entries side by side, four of a thread in flight
+        const int n = end * max_keep;
+#pragma unroll 1
+        for (int t0 = tid; t0 < n; t0 += 4 * kPlanThreads) {
+            int b[4], r[4], x[4], y[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int t = min(t0 + j * kPlanThreads, n - 1);
+                b[j] = small_div(t, max_keep);
+                r[j] = t - b[j] * max_keep;
+                x[j] = p.idx[t];
+                y[j] = p.idx[l.lo[l.of[b[j]]] * max_keep + r[j]];
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int c = l.rest[b[j]];
+                if (r[j] < c && c <= max_keep && x[j] != y[j]) atomicMin(&l.common[l.of[b[j]]], r[j]);
+            }
+        }
+        __syncthreads();
+    } else if (p.find) {
 #pragma unroll 1
         for (int t = tid; t < end * n_scan; t += kPlanThreads) {  // below 2^29
             const int b = (int)((unsigned)t / (unsigned)n_scan), c = l.rest[b];
@@ -295,8 +318,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
         for (int g = tid; g < n_groups; g += kPlanThreads) n += max(l.common[g], 0);
 #pragma unroll 1
         for (int b = tid; b < end; b += kPlanThreads) n += max(l.rest[b], 0);
-#pragma unroll 1
-        for (int x = 32; x >= 1; x /= 2) n += __shfl_xor(n, x);
+        n = wave_sum(n);
         if (lane == 0) atomicAdd(&l.positions, (unsigned)min(n, 1 << 24));
         __syncthreads();
         stream = (int64_t)l.positions * p.Hkv * 2 * kTileRowBytes >= kStreamBytes;
@@ -321,11 +343,8 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
             }
 #pragma unroll 1
             for (int b = lane; b < end; b += 64) waves += (int)((div_up(max(l.rest[b], 0), kWaveTile) + chunk - 1) / chunk);
-#pragma unroll 1
-            for (int x = 32; x >= 1; x /= 2) {
-                wg += __shfl_xor(wg, x);
-                waves += __shfl_xor(waves, x);
-            }
+            wg = wave_sum(wg);
+            waves = wave_sum(waves);
             if (lane == 0) l.work[round][k] = wg + div_up(waves, kSharedWaves);
         }
         __syncthreads();
@@ -1146,8 +1165,11 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(const SharedAttnLaunc
 
 // ---- launchers ----
 
-int launch_shared_plan(const SharedPlanLaunch &p, murmur_stream_t stream) {
-    if (p.find) {
+int launch_shared_plan(const SharedPlanLaunch &call, murmur_stream_t stream) {
+    SharedPlanLaunch p = call;
+    if (p.find && (int64_t)p.B * p.max_keep <= kFindHereEntries) {
+        p.find = kFindHere;
+    } else if (p.find) {
         hipLaunchKernelGGL(shared_scan_kernel, dim3((unsigned)p.caps.n_scan, (unsigned)p.B), dim3(kScanThreads), 0,
                            (hipStream_t)stream, p.idx, p.count, p.group, p.n_groups, p.max_keep, p.B,
                            reinterpret_cast<int32_t *>(p.plan + p.caps.scan_offset));
