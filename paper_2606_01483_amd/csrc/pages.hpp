@@ -43,14 +43,6 @@ static __device__ __forceinline__ int wave_max(int x) {
     return __builtin_amdgcn_readlane(x, 63);
 }
 
-// Loads and stores of words that other workgroups of the launch, or atomics of
-// this one, write: past the caches that are not coherent between XCDs.
-static __device__ __forceinline__ int32_t load_shared_word(const int32_t *p) {
-    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-static __device__ __forceinline__ void store_shared_word(int32_t *p, int32_t x) {
-    __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
 static __device__ __forceinline__ void add_ref(int32_t *ref, int32_t n) {
     __hip_atomic_fetch_add(ref, n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
@@ -270,6 +262,14 @@ __global__ __launch_bounds__(kForkThreads) void fork_push_kernel(int64_t places,
 // stay in registers where a thread has only one: 4.8 us for 4 sequences,
 // 17.7 for 96 (20.9 and 26.1 with every pass reading them again).
 // ---------------------------------------------------------------------------
+// The counts are this workgroup's alone while it runs: atomics in its XCD's L2, where
+// those that other XCDs see go past it.
+static __device__ __forceinline__ int32_t load_count(const int32_t *p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
+static __device__ __forceinline__ void store_count(int32_t *p, int32_t x) {
+    __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
 static __device__ __forceinline__ int32_t place_key(int32_t at) { return (int32_t)(0x80000000u + (uint32_t)at); }
 static __device__ __forceinline__ int64_t seq_position(const murmur_seg &s) {  // of the current token
     return (int64_t)s.prompt_pre + s.speech_len + s.prompt_mid + s.out_len - 1;
@@ -321,7 +321,7 @@ __global__ __launch_bounds__(kThreads) void step_shared_kernel(const murmur_seg 
     for (int b = tid; b < B; b += kThreads)
         each_freed(b, seq_of(b), [&](int32_t *, int32_t phys, int32_t) {
             if (phys < n_blocks)
-                emptied |= __hip_atomic_fetch_add(ref + phys, -1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 1;
+                emptied |= __hip_atomic_fetch_add(ref + phys, -1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) == 1;
             else
                 err |= MURMUR_DEVERR_BLOCK;
         });
@@ -329,30 +329,37 @@ __global__ __launch_bounds__(kThreads) void step_shared_kernel(const murmur_seg 
     if (emptied) {
         for (int b = tid; b < B; b += kThreads)
             each_freed(b, seq_of(b), [&](int32_t *, int32_t phys, int32_t at) {
-                if (phys < n_blocks && load_shared_word(ref + phys) <= 0)
-                    __hip_atomic_fetch_min(ref + phys, place_key(at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                if (phys < n_blocks && load_count(ref + phys) <= 0)
+                    __hip_atomic_fetch_min(ref + phys, place_key(at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
             });
         wait_vmem();
         __syncthreads();
     }
     for (int b0 = 0; b0 < B; b0 += kThreads) {
         const StepSeq s = seq_of(b0 + tid);
-        int to = tp;
+        int to = tp, seen = 0;
+        uint32_t won = 0;  // of the first 32 entries, those that push their blocks
+        const auto wins = [&](int32_t phys, int32_t at) { return phys < n_blocks && load_count(ref + phys) == place_key(at); };
         if (emptied) {
             int n = 0, pushed;
             each_freed(b0 + tid, s, [&](int32_t *, int32_t phys, int32_t at) {
-                n += phys < n_blocks && load_shared_word(ref + phys) == place_key(at);
+                const bool win = wins(phys, at);
+                n += win;
+                won |= win && seen < 32 ? 1u << seen : 0u;
+                ++seen;
             });
+            seen = 0;
             to = tp + wg_exclusive_scan<kThreads>(n, s_scan, tid, pushed);
             tp = tp + pushed < n_blocks ? tp + pushed : n_blocks;
         }
         each_freed(b0 + tid, s, [&](int32_t *entry, int32_t phys, int32_t at) {
-            if (emptied && phys < n_blocks && load_shared_word(ref + phys) == place_key(at)) {
+            if (emptied && (seen < 32 ? won >> seen & 1u : wins(phys, at))) {
                 if (to < n_blocks) stack[to] = phys;
                 else err |= MURMUR_DEVERR_POOL;
                 ++to;
-                store_shared_word(ref + phys, 0);
+                store_count(ref + phys, 0);
             }
+            ++seen;
             *entry = -1;
         });
     }
@@ -373,7 +380,7 @@ __global__ __launch_bounds__(kThreads) void step_shared_kernel(const murmur_seg 
         } else if (s.q.valid && s.x >= n_blocks) {
             err |= MURMUR_DEVERR_BLOCK;
         } else if (s.q.valid) {
-            holders = load_shared_word(ref + s.x);
+            holders = load_count(ref + s.x);
         }
         if (!__syncthreads_or(holders > 1)) return what;
         int before = 0;
@@ -382,7 +389,8 @@ __global__ __launch_bounds__(kThreads) void step_shared_kernel(const murmur_seg 
             s_writer[tid] = o.q.valid && o.q.cur < max_blocks ? int2{o.x, o.pos} : int2{-1, 0};
             __syncthreads();
             if (holders > 1)
-                for (int i = 0; i < min(kThreads, B - o0); ++i) {
+#pragma unroll 8
+                for (int i = 0; i < (min(kThreads, B - o0) + 7) / 8 * 8; ++i) {  // past the last one none
                     const int2 y = s_writer[i];
                     before += y.x == s.x && (y.y >> log2_bs) == s.q.cur &&
                               (y.y < s.pos || (y.y == s.pos && o0 + i < b0 + tid));
@@ -409,9 +417,9 @@ __global__ __launch_bounds__(kThreads) void step_shared_kernel(const murmur_seg 
             const int from = tp - 1 - off;
             const int32_t got = from >= 0 ? stack[from] : -1;
             const bool good = got >= 0 && got < n_blocks;
-            if (good) store_shared_word(ref + got, 1);
+            if (good) store_count(ref + got, 1);
             else err |= MURMUR_DEVERR_POOL;
-            if (what >= 0) add_ref(ref + what, -1);
+            if (what >= 0) __hip_atomic_fetch_add(ref + what, -1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
             bt[(int64_t)b * max_blocks + cur] = good ? got : -1;
             from_block = good ? (what >= 0 ? what : -1) : -2;
         }
@@ -422,8 +430,11 @@ __global__ __launch_bounds__(kThreads) void step_shared_kernel(const murmur_seg 
     if (err) raise_device_error(err);
 }
 
-// A workgroup per (sequence, layer, K or V): the rows of the current block before
-// the token from the block it was copied from, then the token's own rows.
+// A workgroup per sequence and some of its (layer, K or V) planes: the rows of the
+// current block before the token from the block it was copied from, then the
+// token's own rows.  A thread has a 16-byte chunk of a row in each plane, and its
+// loads of kAppendPlanes planes are on their way at once.
+constexpr int kAppendPlanes = 4;
 __global__ __launch_bounds__(256) void append_shared_kernel(const murmur_seg *__restrict__ seg, int32_t B,
                                                             const int32_t *__restrict__ bt, int32_t max_blocks,
                                                             int32_t log2_bs, const int32_t *__restrict__ copied,
@@ -433,26 +444,37 @@ __global__ __launch_bounds__(256) void append_shared_kernel(const murmur_seg *__
                                                             const uint16_t *__restrict__ v_new, int32_t NL,
                                                             int32_t Hkv) {
     const int b = blockIdx.x;
+    const int32_t from = copied[b];
     const int64_t p = seq_position(seg[b]);
     const int64_t blk = p >> log2_bs;
     if (p < 0 || blk >= max_blocks) return;
-    const int32_t phys = bt[(int64_t)b * max_blocks + blk], from = copied[b];
+    const int32_t phys = bt[(int64_t)b * max_blocks + blk];
     if (phys < 0 || from < -1) return;
     const int32_t slot = (int32_t)(p & ((1 << log2_bs) - 1));
     const int64_t row0 = (int64_t)phys << log2_bs, src0 = (int64_t)from << log2_bs;
     if (row0 + slot >= rows || src0 + slot > rows) return;
-    for (int64_t lv = blockIdx.y; lv < 2 * (int64_t)NL; lv += gridDim.y) {
-        const int64_t layer = lv >> 1;
-        uint16_t *base = ((lv & 1) ? v : k) + layer * s_layer;
-        const uint16_t *fresh = ((lv & 1) ? v_new : k_new) + (layer * B + b) * Hkv * kHeadDim;
-        if (from >= 0)
-            for (int t = threadIdx.x; t < slot * Hkv * 16; t += 256) {
-                const int c = t & 15, h = (t >> 4) % Hkv, j = (t >> 4) / Hkv;
-                const int64_t at = h * s_h + j * s_pos + 8 * c;
-                *reinterpret_cast<u32x4 *>(base + row0 * s_pos + at) = load16(base + src0 * s_pos + at);
+    const int planes = 2 * NL, copies = from >= 0 ? slot * Hkv * 16 : 0;
+    for (int t = threadIdx.x; t < copies + Hkv * 16; t += 256) {
+        const bool copy = t < copies;
+        const int r = (copy ? t : t - copies) >> 4, j = copy ? r / Hkv : slot, h = copy ? r - j * Hkv : r;
+        const int64_t to = (row0 + j) * s_pos + h * s_h + 8 * (t & 15);
+        // the source of a copied chunk and of a new one, each with its step from layer to layer
+        const int64_t at = copy ? (src0 + j) * s_pos + h * s_h + 8 * (t & 15) : ((int64_t)b * Hkv + h) * kHeadDim + 8 * (t & 15);
+        const int64_t step = copy ? s_layer : (int64_t)B * Hkv * kHeadDim;
+        const uint16_t *from_k = copy ? k : k_new, *from_v = copy ? v : v_new;
+        for (int lv0 = (int)blockIdx.y * kAppendPlanes; lv0 < planes; lv0 += (int)gridDim.y * kAppendPlanes) {
+            u32x4 x[kAppendPlanes];
+#pragma unroll
+            for (int i = 0; i < kAppendPlanes; ++i) {
+                const int lv = min(lv0 + i, planes - 1);
+                x[i] = load16((lv & 1 ? from_v : from_k) + (lv >> 1) * step + at);
             }
-        for (int t = threadIdx.x; t < Hkv * 16; t += 256)
-            *reinterpret_cast<u32x4 *>(base + (row0 + slot) * s_pos + (t >> 4) * s_h + 8 * (t & 15)) = load16(fresh + 8 * t);
+#pragma unroll
+            for (int i = 0; i < kAppendPlanes; ++i) {
+                const int lv = lv0 + i;
+                if (lv < planes) *reinterpret_cast<u32x4 *>((lv & 1 ? v : k) + (lv >> 1) * s_layer + to) = x[i];
+            }
+        }
     }
 }
 
@@ -603,7 +625,7 @@ int launch_paged_step_shared(const murmur_seg *seg, const murmur_policy *pol, in
 int launch_paged_append_shared(const murmur_seg *seg, int32_t B, const int32_t *bt, int32_t max_blocks,
                                int32_t log2_bs, const int32_t *copied, const murmur_kv &pool, int32_t Hkv,
                                const void *k_new, const void *v_new, murmur_stream_t stream) {
-    const unsigned y = (unsigned)(pool.n_layers < 32768 ? 2 * pool.n_layers : 65535);
+    const unsigned y = (unsigned)std::min<int64_t>((2 * (int64_t)pool.n_layers + kAppendPlanes - 1) / kAppendPlanes, 65535);
     hipLaunchKernelGGL(append_shared_kernel, dim3((unsigned)B, y), dim3(256), 0, (hipStream_t)stream, seg, B, bt,
                        max_blocks, log2_bs, copied, (uint16_t *)pool.k, (uint16_t *)pool.v, pool.stride_layer,
                        pool.stride_h, pool.stride_pos, (int64_t)pool.max_len, (const uint16_t *)k_new,
