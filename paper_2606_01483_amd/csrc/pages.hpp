@@ -390,10 +390,11 @@ __global__ __launch_bounds__(kThreads) void step_shared_kernel(const murmur_seg 
             __syncthreads();
             if (holders > 1)
 #pragma unroll 8
-                for (int i = 0; i < (min(kThreads, B - o0) + 7) / 8 * 8; ++i) {  // past the last one none
+                for (int i = 0; i < (min(kThreads, B - o0) + 7) / 8 * 8; ++i) {  // behind the last sequence none writes
                     const int2 y = s_writer[i];
-                    before += y.x == s.x && (y.y >> log2_bs) == s.q.cur &&
-                              (y.y < s.pos || (y.y == s.pos && o0 + i < b0 + tid));
+                    // (position, index) before this one's; no short cuts, which would be branches
+                    before += (int)(y.x == s.x) & (int)((y.y >> log2_bs) == s.q.cur) &
+                              (int)(y.y <= s.pos - (int)(o0 + i >= b0 + tid));
                 }
             __syncthreads();
         }
