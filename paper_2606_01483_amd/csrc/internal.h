@@ -263,6 +263,7 @@ struct PlanChunk {
 struct SharedCaps {
     int32_t per_round;  // workgroups per (layer, KV head) of one dispatch round
     int32_t n_wg, n_scan;
+    int32_t grid;       // workgroups that are launched, at most n_wg
     bool whole;         // no list is cut (see shared_caps)
     int32_t waves;      // of a workgroup then
     int64_t rows;       // partial rows per (layer, KV head)

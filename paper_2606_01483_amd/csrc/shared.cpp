@@ -135,18 +135,29 @@ SharedCaps shared_caps(int32_t n_layers, int32_t B, int32_t Hq, int32_t Hkv, int
     c.n_wg = (int32_t)std::min<int64_t>(std::max<int64_t>(c.per_round, longest), 0x7fffffff);
     c.rows = std::max<int64_t>((int64_t)c.per_round * kSharedRows, B * G * cuts) + G * (B + (int64_t)c.n_wg);
     // Whether lists are left whole (shared_whole_kernel) or cut (shared_attn_kernel and the merge), from what the host
-    // knows, in us: whole, each workgroup of eight wavefronts takes a list's passes at 1 us a round of them (as many
-    // compute units read at once, from the L2s too), and a dispatch round after the other; cut, every group's list
-    // comes at the memory's rate, and the partials cost about 12 more.
-    const int64_t whole_wg = heads * std::min<int64_t>(B, n_groups + B / (kMaxGroup / G));
-    const double whole_us = (double)div_up(whole_wg, kRoundWorkgroups) * (double)div_up(passes, 8) + 5.0;
-    const double cut_us = (double)heads * std::min(n_groups, B) * max_keep * 512.0 / 5e6 + 17.0;
-    c.whole = whole_us <= cut_us;
-    c.waves = heads * std::min(n_groups, B) > kRoundWorkgroups ? 4 : 8;
-    if (c.whole) {
-        c.n_wg = (int32_t)std::min<int64_t>(B, n_groups + B / (kMaxGroup / G));
-        c.rows = 0;
+    // knows, in us.  A group's lists come at the memory's rate once at least.  A round of passes, one of each of a
+    // workgroup's eight wavefronts, takes 1.2, 2.0 or 2.9 with one, two or three row tiles if a compute unit has nothing
+    // but to compute, and 2.4 if its rows come from memory, less the more workgroups share them.  Whole, a workgroup
+    // takes a list's rounds one after the other, and 6 besides; cut, they are spread over the chip, and the partials
+    // and their join make it 15.  (12 chunks of 8 sequences, lists of 850: 15.4 a layer whole, 16.7 cut; 15 sequences,
+    // lists of 2963, next to nothing shared: 32.6 whole, 15.2 cut.)
+    const int64_t n = div_up(B, std::max(n_groups, 1)), rounds = div_up(passes, 8);  // sequences of a group
+    const double round_us[3] = {1.2, 2.0, 2.9}, wave = (double)kRoundWorkgroups, wg = (double)heads * n_groups;
+    const double read_us = (double)heads * std::min(n_groups, B) * max_keep * 512.0 / 5e6;
+    double alone_us = 0.0, spread_us = 0.0;
+    for (int tiles = 1; tiles <= 3; ++tiles) {
+        const int64_t parts = div_up(n, kMaxGroup * tiles / G);
+        const double compute = round_us[tiles - 1] * (double)(rounds * parts) * wg / wave;
+        const double us = std::max(compute, (double)rounds * std::max(round_us[tiles - 1], 1.2 + 1.2 / (double)std::min<int64_t>(parts, 4)));
+        alone_us = tiles == 1 ? us : std::min(alone_us, us);
+        spread_us = tiles == 1 ? compute : std::min(spread_us, compute);
     }
+    c.whole = 6.0 + std::max(read_us, alone_us) <= 15.0 + std::max(read_us, spread_us);
+    c.waves = heads * std::min(n_groups, B) > kRoundWorkgroups ? 4 : 8;
+    // The buffers hold either schedule, so that those of the largest batch serve a smaller one that goes the other way.
+    const int64_t items = std::min<int64_t>(B, std::max<int64_t>(n_groups + B / (kMaxGroup / G), kRoundWorkgroups / heads));
+    c.n_wg = (int32_t)std::max<int64_t>(c.n_wg, items);
+    c.grid = c.whole ? (int32_t)items : c.n_wg;
     c.n_scan = (max_keep - 1) / kScanLen + 1;
     c.item_offset = sizeof(PlanHeader) + sizeof(PlanSeq) * (size_t)B;
     c.chunk_offset = c.item_offset + sizeof(PlanItem) * (size_t)c.n_wg;
@@ -358,7 +369,7 @@ MURMUR_EXPORT int murmur_decode_attn_shared(const void *q_dev, const murmur_kv *
     a.G = Hq / Hkv;
     a.NL = kv->n_layers;
     a.n_groups = n_groups;
-    a.n_wg = c.n_wg;
+    a.n_wg = c.grid;
     a.waves = c.whole ? c.waves : 0;
     a.out_f32 = out_dtype == MURMUR_DTYPE_F32;
     a.magic_g = (uint32_t)((((uint64_t)1 << 32) + a.G - 1) / a.G - 1);

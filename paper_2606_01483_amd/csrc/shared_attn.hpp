@@ -126,9 +126,11 @@ static __device__ __forceinline__ int item_place(int q, int n, int heads) {
 }
 
 // The plan where no list is cut: a workgroup per (layer, KV head) and some sequences
-// of a group, with one, two or three row tiles, whichever is estimated fastest (in
-// tenths of a pass with one tile; measured: a pass takes half as long again with
-// each further tile, and a workgroup about six passes besides).
+// of a group: as many as fill one, two or three row tiles, or a half, a quarter, ... of
+// what fills one, whichever is estimated fastest (in tenths of a pass with one tile;
+// measured: a pass takes half as long again with each further tile, and a workgroup
+// about six passes besides).  The prefix is read by all, the rests one after the other.
+// The last choice that the launch has no workgroups for is that of one tile.
 template <int kPlanThreads>
 static __device__ __forceinline__ void plan_whole(const SharedPlanLaunch &p, PlanLds &l, PlanHeader *h, PlanSeq *seqs,
                                                   PlanItem *items, int end, int stream, int tid) {
@@ -149,15 +151,17 @@ static __device__ __forceinline__ void plan_whole(const SharedPlanLaunch &p, Pla
         }
     }
     __syncthreads();
-    if (wave < 3) {
-        const int per = small_div(16 * (wave + 1), G);
+    const int one_tile = small_div(16, G), choices = 3 + 31 - __clz(one_tile);
+    const auto per_of = [&](int c) { return c < 3 ? small_div(16 * (c + 1), G) : one_tile >> (c - 2); };
+    for (int c = wave; c < choices; c += kPlanThreads / 64) {
+        const int per = per_of(c), extra = c < 3 ? 5 * c : 0;
         int wg = 0, sum = 0, most = 0;
 #pragma unroll 1
-        for (int g = lane; per > 0 && g < n_groups; g += 64) {
+        for (int g = lane; g < n_groups; g += 64) {
             const int n = l.lo[g + 1] - l.lo[g], parts = small_div_up(n, per);
             if (n == 0) continue;
-            const int rounds = (div_up(max(l.common[g], 0), kWaveTile) + (int)((unsigned)l.row[g] / (unsigned)parts)) / (waves == 8 ? 8 : 4) + 1;
-            const int cost = 60 + (10 + 5 * wave) * rounds;
+            const int passes = div_up(max(l.common[g], 0), kWaveTile) + (int)((unsigned)(l.row[g] + parts - 1) / (unsigned)parts);
+            const int cost = 60 + (10 + extra) * (waves == 8 ? div_up(passes, 8) : div_up(passes, 4));
             wg += parts;
             sum += parts * min(cost, 1 << 18);
             most = max(most, cost);
@@ -165,15 +169,15 @@ static __device__ __forceinline__ void plan_whole(const SharedPlanLaunch &p, Pla
         wg = wave_sum(wg);
         sum = wave_sum(sum);
         most = wave_max(most);
-        if (lane == 0)
-            l.work[0][wave] = per == 0 ? 0x7fffffff
-                                    : (int)min<int64_t>(0x7ffffffe, (int64_t)most + ((int64_t)wg * heads > slots ? (int64_t)((uint64_t)((int64_t)sum * heads) / kRoundWorkgroups / (waves == 8 ? 1 : 2)) : 0));
+        const int64_t all = (int64_t)(((uint64_t)sum * (uint64_t)heads) / kRoundWorkgroups >> (waves == 8 ? 0 : 1));
+        const int64_t time = most + ((int64_t)wg * heads > slots ? all : 0);
+        if (lane == 0) l.work[0][c] = wg > p.caps.grid ? 0x7fffffff : (int)min<int64_t>(time, 0x7ffffffe);
     }
     __syncthreads();
-    int tiles = 0;
+    int choice = 0;
 #pragma unroll 1
-    for (int i = 1; i < 3; ++i) tiles = l.work[0][i] < l.work[0][tiles] ? i : tiles;
-    const int per = small_div(16 * (tiles + 1), G);
+    for (int c = 1; c < choices; ++c) choice = l.work[0][c] < l.work[0][choice] ? c : choice;
+    const int per = per_of(choice);
     int work = 0;
 #pragma unroll 1
     for (int g0 = 0; g0 < n_groups; g0 += kPlanThreads) {
@@ -198,7 +202,7 @@ static __device__ __forceinline__ void plan_whole(const SharedPlanLaunch &p, Pla
     if (tid == 0) {
         h->n_work = work;
         h->rows = 0;
-        h->level = -(tiles + 1);
+        h->level = -per;
     }
 }
 
