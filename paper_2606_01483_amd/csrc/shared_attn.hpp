@@ -663,12 +663,54 @@ static __device__ __forceinline__ void keep_apart(u32x2 (&vf)[16], uint8_t *tile
     read_v_operands(vf, lds_addr(tile), lane & 15, c4);
 }
 
+// softmax_step of a pass that is one of many, with the weights as the sums of kTerms
+// bf16 parts, each the rounding of what the ones before leave: two for bf16 outputs
+// (2^-17 of a weight at most, against an output's 2^-9) and three for fp32 ones (what
+// is left is below fp32's own rounding: over 35 096 positions outputs are 2.5e-7 off,
+// relative, where two parts gave 1.8e-6; 28 layers 700 us instead of 670).
+template <int kTerms>
+static __device__ __forceinline__ void softmax_pass(f32x4 (&s)[2], int valid, float scale, WaveAcc &w, int c4,
+                                                    u32x4 (&p)[kTerms]) {
+    if (valid < kWaveTile) {  // uniform
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[blk][i] = 16 * blk + 4 * c4 + i < valid ? s[blk][i] : kNegInf;
+    }
+    const float lane_max = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                                 fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+    if (__ballot(lane_max > w.m_run)) {
+        const float m_new = fmaxf(w.m_run, max_over_c4(lane_max));
+        const float alpha = __builtin_amdgcn_exp2f((w.m_run - m_new) * scale);  // 0 while the state is empty
+        w.l_run *= alpha;
+#pragma unroll
+        for (int db = 0; db < 8; ++db) w.acc[db] *= alpha;
+        w.m_run = m_new;
+    }
+    float pr[2][4];
+#pragma unroll
+    for (int blk = 0; blk < 2; ++blk)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pr[blk][i] = __builtin_amdgcn_exp2f((s[blk][i] - w.m_run) * scale);
+    w.l_run += ((pr[0][0] + pr[0][1]) + (pr[0][2] + pr[0][3])) + ((pr[1][0] + pr[1][1]) + (pr[1][2] + pr[1][3]));
+#pragma unroll
+    for (int wd = 0; wd < 4; ++wd) {
+        float e0 = pr[wd >> 1][(wd & 1) * 2], e1 = pr[wd >> 1][(wd & 1) * 2 + 1];
+#pragma unroll
+        for (int k = 0; k < kTerms; ++k) {
+            p[k][wd] = pack_bf16(e0, e1);
+            e0 -= __builtin_bit_cast(float, p[k][wd] << 16);
+            e1 -= __builtin_bit_cast(float, p[k][wd] & 0xffff0000u);
+        }
+    }
+}
+
 // The passes of `feed` against kTiles row tiles.  load_queries starts the loads of
 // the queries (4 kTiles of them) into qf.  row_seq: which of the item's sequences
 // the lane's row of a tile belongs to (several lists only).  on_bad(pass) is called
 // for a pass with a position outside the cache.  Returns the positive scale
 // (signed_scale).
-template <int kSrc, bool kNear, int kTiles, typename Feed, typename LoadQ, typename OnBad>
+template <int kTerms, int kSrc, bool kNear, int kTiles, typename Feed, typename LoadQ, typename OnBad>
 static __device__ __forceinline__ float run_passes(const SharedAttnLaunch &a, int layer, int g, bool stream, Feed &feed,
                                                    uint8_t *stage, uint8_t (*slots)[kIdxSlotBytes],
                                                    u32x4 (&qf)[kTiles][4], LoadQ load_queries,
@@ -742,7 +784,7 @@ static __device__ __forceinline__ float run_passes(const SharedAttnLaunch &a, in
             load(in.k, stage);
         }
         const int valid = min(kWaveTile, cur.r_end - cur.r);
-        u32x4 p_hi[kTiles], p_lo[kTiles];
+        u32x4 p[kTiles][kTerms];
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
             f32x4 s[2];
@@ -760,7 +802,7 @@ static __device__ __forceinline__ float run_passes(const SharedAttnLaunch &a, in
 #pragma unroll
                     for (int i = 0; i < 4; ++i) s[blk][i] = mine ? s[blk][i] : kNegInf;
             }
-            softmax_step<true>(s, valid, scale, w[t], c4, p_hi[t], p_lo[t]);
+            softmax_pass<kTerms>(s, valid, scale, w[t], c4, p[t]);
         }
         u32x2 vf[16];
         if (more) wait_vm<8>();  // this pass's V rows; the next pass's K rows came after them
@@ -772,10 +814,9 @@ static __device__ __forceinline__ float run_passes(const SharedAttnLaunch &a, in
         for (int db = 0; db < 8; ++db) {
             const u32x4 av = u32x4{vf[2 * db][0], vf[2 * db][1], vf[2 * db + 1][0], vf[2 * db + 1][1]};
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) {
-                w[t].acc[db] = mfma16x16x32(av, p_hi[t], w[t].acc[db]);
-                w[t].acc[db] = mfma16x16x32(av, p_lo[t], w[t].acc[db]);
-            }
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int k = 0; k < kTerms; ++k) w[t].acc[db] = mfma16x16x32(av, p[t][k], w[t].acc[db]);
         }
         if (!more) break;
         cur = nxt;
@@ -889,7 +930,7 @@ static __device__ __forceinline__ void store_row(const SharedAttnLaunch &a, int6
     if (c == 0 && a.lse) a.lse[row] = (M + __builtin_log2f(L)) * 0.69314718055994530942f;
 }
 
-template <int kSrc, bool kNear, int kTiles>
+template <int kTerms, int kSrc, bool kNear, int kTiles>
 static __device__ __forceinline__ void item_work(const SharedAttnLaunch &a, const PlanItem &it, SharedLds<kSharedWaves> &l,
                                                  int layer, int g, float *part_o, float *part_ml, int tid, int wave) {
     const int lane = tid & 63, n16 = lane & 15, c4 = lane >> 4;
@@ -901,7 +942,7 @@ static __device__ __forceinline__ void item_work(const SharedAttnLaunch &a, cons
     for (int t = 0; t < kTiles; ++t) wave_acc_reset(w[t]);
     OneList feed{it.list, it.r0 + wave * kWaveTile, it.r1, kSharedWaves * kWaveTile};
     int wave_bad = 0;
-    const float scale = run_passes<kSrc, kNear, kTiles>(
+    const float scale = run_passes<kTerms, kSrc, kNear, kTiles>(
         a, layer, g, it.stream, feed, l.stages[wave], l.slots[wave], qf,
         [&] { load_item_queries<kTiles>(a, it, layer, g, n16, c4, qf, row_seq); }, row_seq, w, lane,
         [&](const Pass &) { wave_bad = 1; });
@@ -923,7 +964,7 @@ static __device__ __forceinline__ void item_work(const SharedAttnLaunch &a, cons
     if (bad && tid == 0) raise_device_error(MURMUR_DEVERR_POSITION);
 }
 
-template <int kSrc, bool kNear>
+template <int kTerms, int kSrc, bool kNear>
 static __device__ __forceinline__ void chunk_work(const SharedAttnLaunch &a, const PlanChunk &c, bool stream,
                                                   SharedLds<kSharedWaves> &l, int layer, int g, float *part_o, float *part_ml,
                                                   int tid, int wave) {
@@ -934,7 +975,7 @@ static __device__ __forceinline__ void chunk_work(const SharedAttnLaunch &a, con
     int row_seq[1], wave_bad = 0;
     OneList feed{c.seq, c.r0, c.r1, kWaveTile};  // none: r0 == r1
     const PlanItem one{c.seq, 1, c.seq, 0, 0, 0, 0, 0};
-    const float scale = run_passes<kSrc, kNear, 1>(
+    const float scale = run_passes<kTerms, kSrc, kNear, 1>(
         a, layer, g, stream, feed, l.stages[wave], l.slots[wave], qf,
         [&] { load_item_queries<1>(a, one, layer, g, n16, c4, qf, row_seq); }, row_seq, w, lane,
         [&](const Pass &) { wave_bad = 1; });
@@ -968,7 +1009,7 @@ static __device__ __forceinline__ bool plan_fits(const SharedAttnLaunch &a, cons
            h.Hq == a.Hq && h.Hkv == a.Hkv && h.n_groups == a.n_groups && h.rows <= a.rows_cap && h.n_work <= a.n_wg && (h.level < 0) == (a.waves > 0);
 }
 
-template <int kSrc, bool kNear>
+template <int kTerms, int kSrc, bool kNear>
 __global__ __launch_bounds__(kSharedThreads, 2) void shared_attn_kernel(const SharedAttnLaunch a) {
     __shared__ __attribute__((aligned(16))) SharedLds<kSharedWaves> l;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = blockIdx.y;
@@ -983,13 +1024,13 @@ __global__ __launch_bounds__(kSharedThreads, 2) void shared_attn_kernel(const Sh
     float *part_ml = a.part_ml + (int64_t)blockIdx.x * h.rows * 2;
     const int rows = it.n_seq * a.G;
     if (rows == 0)
-        chunk_work<kSrc, kNear>(a, c, it.stream, l, layer, g, part_o, part_ml, tid, wave);
+        chunk_work<kTerms, kSrc, kNear>(a, c, it.stream, l, layer, g, part_o, part_ml, tid, wave);
     else if (rows <= 16)
-        item_work<kSrc, kNear, 1>(a, it, l, layer, g, part_o, part_ml, tid, wave);
+        item_work<kTerms, kSrc, kNear, 1>(a, it, l, layer, g, part_o, part_ml, tid, wave);
     else if (rows <= 32)
-        item_work<kSrc, kNear, 2>(a, it, l, layer, g, part_o, part_ml, tid, wave);
+        item_work<kTerms, kSrc, kNear, 2>(a, it, l, layer, g, part_o, part_ml, tid, wave);
     else
-        item_work<kSrc, kNear, 3>(a, it, l, layer, g, part_o, part_ml, tid, wave);
+        item_work<kTerms, kSrc, kNear, 3>(a, it, l, layer, g, part_o, part_ml, tid, wave);
 }
 
 // ---------------------------------------------------------------------------
@@ -1000,7 +1041,7 @@ __global__ __launch_bounds__(kSharedThreads, 2) void shared_attn_kernel(const Sh
 // (from the L2s, mostly).  Eight wavefronts and a compute unit each where there are
 // about as many workgroups as compute units, else four, two workgroups on one.
 // ---------------------------------------------------------------------------
-template <int kSrc, bool kNear, int kTiles, int kWaves>
+template <int kTerms, int kSrc, bool kNear, int kTiles, int kWaves>
 static __device__ __forceinline__ void whole_work(const SharedAttnLaunch &a, const PlanItem &it, SharedLds<kWaves> &l,
                                                   int layer, int g, int tid, int wave) {
     const int lane = tid & 63, n16 = lane & 15, c4 = lane >> 4;
@@ -1035,7 +1076,7 @@ static __device__ __forceinline__ void whole_work(const SharedAttnLaunch &a, con
         wave_acc_reset(w[t]);
         w[t].m_run = kNoRows;
     }
-    const float scale = run_passes<kSrc, kNear, kTiles>(
+    const float scale = run_passes<kTerms, kSrc, kNear, kTiles>(
         a, layer, g, it.stream, feed, l.stages[wave], l.slots[wave], qf,
         [&] { load_item_queries<kTiles>(a, it, layer, g, n16, c4, qf, row_seq); }, row_seq, w, lane,
         [&](const Pass &p) {
@@ -1069,7 +1110,7 @@ static __device__ __forceinline__ void whole_work(const SharedAttnLaunch &a, con
     }
 }
 
-template <int kSrc, bool kNear, int kWaves>
+template <int kTerms, int kSrc, bool kNear, int kWaves>
 __global__ __launch_bounds__(kWaves * 64, 2) void shared_whole_kernel(const SharedAttnLaunch a) {
     __shared__ __attribute__((aligned(16))) SharedLds<kWaves> l;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = blockIdx.y;
@@ -1088,11 +1129,11 @@ __global__ __launch_bounds__(kWaves * 64, 2) void shared_whole_kernel(const Shar
     const int layer = (int)blockIdx.x / a.Hkv, g = (int)blockIdx.x - layer * a.Hkv;
     const int rows = it.n_seq * a.G;
     if (rows <= 16)
-        whole_work<kSrc, kNear, 1, kWaves>(a, it, l, layer, g, tid, wave);
+        whole_work<kTerms, kSrc, kNear, 1, kWaves>(a, it, l, layer, g, tid, wave);
     else if (rows <= 32)
-        whole_work<kSrc, kNear, 2, kWaves>(a, it, l, layer, g, tid, wave);
+        whole_work<kTerms, kSrc, kNear, 2, kWaves>(a, it, l, layer, g, tid, wave);
     else
-        whole_work<kSrc, kNear, 3, kWaves>(a, it, l, layer, g, tid, wave);
+        whole_work<kTerms, kSrc, kNear, 3, kWaves>(a, it, l, layer, g, tid, wave);
 }
 
 // kPer half wavefronts per query row, each folding every kPer-th partial: the pairs
@@ -1188,29 +1229,31 @@ int launch_shared_plan(const SharedPlanLaunch &call, murmur_stream_t stream) {
     return (int)hipGetLastError();
 }
 
-template <int kSrc, bool kNear>
+template <int kTerms, int kSrc, bool kNear>
 static void launch_shared_attn_near(const SharedAttnLaunch &a, hipStream_t stream) {
     const dim3 grid((unsigned)(a.NL * a.Hkv), (unsigned)a.n_wg);
     if (a.waves == 8)
-        hipLaunchKernelGGL((shared_whole_kernel<kSrc, kNear, 8>), grid, dim3(8 * 64), 0, stream, a);
+        hipLaunchKernelGGL((shared_whole_kernel<kTerms, kSrc, kNear, 8>), grid, dim3(8 * 64), 0, stream, a);
     else if (a.waves == 4)
-        hipLaunchKernelGGL((shared_whole_kernel<kSrc, kNear, 4>), grid, dim3(4 * 64), 0, stream, a);
+        hipLaunchKernelGGL((shared_whole_kernel<kTerms, kSrc, kNear, 4>), grid, dim3(4 * 64), 0, stream, a);
     else
-        hipLaunchKernelGGL((shared_attn_kernel<kSrc, kNear>), grid, dim3(kSharedThreads), 0, stream, a);
+        hipLaunchKernelGGL((shared_attn_kernel<kTerms, kSrc, kNear>), grid, dim3(kSharedThreads), 0, stream, a);
 }
 
-template <int kSrc>
+template <int kTerms>
 static void launch_shared_attn(const SharedAttnLaunch &a, hipStream_t stream) {
     // rows of at least 256 bytes (one if the cache has one row) within 2^32: positions below 2^24
     const bool near = a.s_pos < kRunRowLimit && (a.s_pos >= kHeadDim || a.max_len == 1) &&
                       (__int128)(a.max_len - 1) * a.s_pos * 2 + kTileRowBytes < ((__int128)1 << 32);
-    if (near) launch_shared_attn_near<kSrc, true>(a, stream);
-    else launch_shared_attn_near<kSrc, false>(a, stream);
+    if (a.ranges && near) launch_shared_attn_near<kTerms, kSrcRanges, true>(a, stream);
+    else if (a.ranges) launch_shared_attn_near<kTerms, kSrcRanges, false>(a, stream);
+    else if (near) launch_shared_attn_near<kTerms, kSrcIndex, true>(a, stream);
+    else launch_shared_attn_near<kTerms, kSrcIndex, false>(a, stream);
 }
 
 int launch_decode_attn_shared(const SharedAttnLaunch &a, murmur_stream_t stream) {
-    if (a.ranges) launch_shared_attn<kSrcRanges>(a, (hipStream_t)stream);
-    else launch_shared_attn<kSrcIndex>(a, (hipStream_t)stream);
+    if (a.out_f32) launch_shared_attn<3>(a, (hipStream_t)stream);
+    else launch_shared_attn<2>(a, (hipStream_t)stream);
     const int e = (int)hipGetLastError();
     if (e != 0 || a.waves > 0) return e;
     // Half wavefronts per row: as many as keep the rows' workgroups below two per compute unit; few rows have many
