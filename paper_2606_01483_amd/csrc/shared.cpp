@@ -117,11 +117,11 @@ int check_shared_sizes(int32_t n_layers, int32_t B, int32_t Hq, int32_t Hkv, int
 }  // namespace
 
 // Bounds of any plan for these sizes.  A plan that fits one dispatch round has at
-// most per_round workgroups per (layer, KV head) (one on a compute unit), each
-// with at most kSharedRows partial rows of a prefix.  Any other is cut at the highest level: a group of n
-// sequences has at most n / (sequences per item) + 1 sets of rows, each list at most
-// max_keep entries.  Each sequence's rest has a partial per workgroup that it
-// touches: one, and one more for every workgroup boundary.
+// most per_round workgroups per (layer, KV head) (one on a compute unit), each with
+// at most kSharedRows partial rows of a prefix.  Any other is cut at the highest
+// level: a group of n sequences has at most n / (sequences per item) + 1 sets of
+// rows, each list at most max_keep entries.  Each sequence's rest has a partial per
+// workgroup that it touches: one, and one more for every workgroup boundary.
 SharedCaps shared_caps(int32_t n_layers, int32_t B, int32_t Hq, int32_t Hkv, int32_t max_keep, int32_t n_groups) {
     SharedCaps c{};
     const int64_t G = Hq / Hkv, heads = (int64_t)n_layers * Hkv;

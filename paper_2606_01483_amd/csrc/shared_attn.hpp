@@ -2,14 +2,16 @@
 //
 //   shared_scan_kernel   where each list leaves the first one of its group
 //   shared_plan_kernel   what the groups share, and the work of every workgroup
+//   shared_whole_kernel  the attention, each list left whole; or
 //   shared_attn_kernel   partial softmax sums of the prefixes and of the rests
-//   shared_merge_kernel  their log-sum-exp join
+//   shared_merge_kernel  and their log-sum-exp join
 //
 // out = sum_i softmax_i(s q.K_i) V_i over a list R = P ++ T is
 // (e^(mP-m) OP + e^(mT-m) OT) / (e^(mP-m) lP + e^(mT-m) lT), m = max(mP, mT), for
 // the (max, sum, unscaled sum) of each part, so the part P that the sequences of
 // a group have in common is read once for all of their query rows: a workgroup
-// multiplies each pass of 32 positions with up to 48 rows (three MFMA row tiles).  Bound: the K/V bytes, each distinct row once.
+// multiplies each pass of 32 positions with up to 48 rows (three MFMA row tiles).
+// Bound: the K/V bytes, each distinct row once.
 #pragma once
 
 namespace murmur {
@@ -91,17 +93,19 @@ struct Dealt {
 };
 
 // SharedPlanLaunch::find where the planner compares the lists itself: few entries, a
-// load or two of a thread, are cheaper than another launch (4 lists of 266: 2.7 us).
+// load or two of a thread, are cheaper than another launch (4 lists of 266: 17 us for
+// plan and attention, 19 with it).
 constexpr int kFindHere = 2;
 constexpr int kFindHereEntries = 4096;
 
 // One workgroup; what it needs of every sequence and group is in LDS, so that the
 // global round trips are the counts with the groups, the scans, and the stores.  It
 // runs each line once, on code that no cache holds yet, so what bounds it is the
-// size of the code (loops are not unrolled, divisions are by reciprocal): 17 KB
-// took 9.1 us for 96 sequences.  The lowest level of cut whose workgroups fit one
-// dispatch round is taken, or the highest; the wavefronts add up eight levels side
-// by side, then the eight between two of them.
+// size of the code (loops are not unrolled, divisions are by reciprocal, sums over
+// lanes go by DPP): 5.3 us for 4 sequences, 7.9 for 96, 9.1 when it had 17 KB.
+// The lowest level of cut whose workgroups fit one dispatch round is taken, or the
+// highest; the wavefronts add up eight levels side by side, then the eight between
+// two of them.
 struct PlanLds {
     int rest[kSharedMaxSeqs];           // by sequence: length of the rest, -1 if the sequence is left out
     uint16_t of[kSharedMaxSeqs];        // its group
@@ -849,7 +853,8 @@ static __device__ __forceinline__ void load_item_queries(const SharedAttnLaunch 
 // or remainders, each wavefront a chunk of some sequence's.  Eight wavefronts and
 // 138 KiB of LDS, a compute unit for a workgroup: with four, two on one, there are
 // twice the partials to write and to join (35 096 positions, 5 hypotheses, 4 KV
-// heads: 21.8 + 4.0 us a layer, 22.5 + 5.1 with four).
+// heads: 21.8 + 4.0 us a layer, 22.5 + 5.1 with four; 20.8 + 4.0 since the levels go
+// by quarters of a pass).  Two thirds of it is the read: 73 MB at 5.5 TB/s.
 // ---------------------------------------------------------------------------
 constexpr int kSharedThreads = kSharedWaves * 64;
 template <int kWaves>
@@ -1006,7 +1011,8 @@ static __device__ __forceinline__ void chunk_work(const SharedAttnLaunch &a, con
 // Whether a plan was made for a call of these sizes.
 static __device__ __forceinline__ bool plan_fits(const SharedAttnLaunch &a, const PlanHeader &h) {
     return h.magic == kPlanMagic && !h.bad && h.B == a.B && h.max_keep == a.max_keep && h.n_layers == a.NL &&
-           h.Hq == a.Hq && h.Hkv == a.Hkv && h.n_groups == a.n_groups && h.rows <= a.rows_cap && h.n_work <= a.n_wg && (h.level < 0) == (a.waves > 0);
+           h.Hq == a.Hq && h.Hkv == a.Hkv && h.n_groups == a.n_groups && h.rows <= a.rows_cap && h.n_work <= a.n_wg &&
+           (h.level < 0) == (a.waves > 0);
 }
 
 template <int kTerms, int kSrc, bool kNear>
@@ -1039,7 +1045,11 @@ __global__ __launch_bounds__(kSharedThreads, 2) void shared_attn_kernel(const Sh
 // them and each rest with the other sequences' rows masked, and writes the outputs.
 // No partials, no second launch.  Workgroups of one group read the same prefix
 // (from the L2s, mostly).  Eight wavefronts and a compute unit each where there are
-// about as many workgroups as compute units, else four, two workgroups on one.
+// about as many workgroups as compute units, else four, two workgroups on one, whose
+// prologues and epilogues overlap.  12 groups of 8, lists of 850, 4 KV heads: 16.4 us a
+// layer, of which 5 are the first round trips (plan, entries, rows) and 4 the passes,
+// at 91 bytes a nanosecond and compute unit; 28 layers of 16 groups of 6 drafted tokens
+// in one launch: 2.67 GB in 483 us (5.5 TB/s).
 // ---------------------------------------------------------------------------
 template <int kTerms, int kSrc, bool kNear, int kTiles, int kWaves>
 static __device__ __forceinline__ void whole_work(const SharedAttnLaunch &a, const PlanItem &it, SharedLds<kWaves> &l,
