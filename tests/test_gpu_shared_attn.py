@@ -435,6 +435,18 @@ def test_two_calls_at_once(extra_keep):
 
 
 @pytest.mark.parametrize("extra_keep", [0, CUT])
+@pytest.mark.parametrize("groups", [[(3, [1] * 4096)], [(0, [2])] * 4096, [(40, [5, 6])] * 1500])
+def test_the_most_sequences_and_groups(groups, extra_keep):
+    announce(f"{len(groups)} groups of {len(groups[0][1])}, keep + {extra_keep}")
+    c = Case(18, groups, hq=2, hkv=2, extra_keep=extra_keep)
+    c.make_plan()
+    c.attend()
+    c.check(only=[0, 1, c.B // 2, c.B - 2, c.B - 1])
+    assert np.array_equal(c.shared.cpu().numpy(), c.common)
+    assert torch.isfinite(c.out).all() and M.murmur_device_error() == 0
+
+
+@pytest.mark.parametrize("extra_keep", [0, CUT])
 def test_a_pool_past_2_gib(extra_keep):
     """Rows whose offsets pass 32 bits, in bytes and in elements."""
     announce("offsets past 32 bits")

@@ -232,6 +232,51 @@ def test_step_many_sequences_of_one_block():
     assert np.array_equal(d.copied.cpu().numpy(), copied) and copied[300] == -1 and copied[0] == 0
 
 
+@pytest.mark.parametrize("B", [1024, 1025, 2300])
+def test_step_of_more_sequences_than_the_workgroup_has_threads(B):
+    announce(f"steps of {B} sequences")
+    rng = np.random.default_rng(B)
+    bs, steps = 4, 6
+    lo = np.arange(B) // 3 * 3
+    seg = np.tile(np.array([[3, 9, 1, 8]], dtype=np.int32), (B, 1))
+    seg[:, 3] += rng.integers(0, 12, (B + 2) // 3)[np.arange(B) // 3].astype(np.int32)
+    pol = np.tile(np.array([[4, 2, 1, 5, 1]], dtype=np.int32), (B, 1))
+    length = seg.sum(axis=1) - 1
+    max_blocks = int(-(-(length.max() + steps) // bs))
+    n_blocks = B * max_blocks
+    free = [int(x) for x in rng.permutation(n_blocks)]
+    table = np.full((B, max_blocks), -1, dtype=np.int32)
+    for b in range(B):
+        for c in range(-(-int(length[b]) // bs)):
+            table[b, c] = free.pop() if b == lo[b] else table[lo[b], c]
+    st = {"table": table, "ref": OS.recount(table, n_blocks), "stack": free}
+    d = Device(st)
+    for s in range(steps):
+        parent = np.minimum(lo + rng.integers(0, 3, B), B - 1)
+        d.fork(i32(parent))
+        OS.fork(st, parent)
+        d.step(i32(seg), i32(pol), bs, s == 0)
+        copied = OS.step(st, seg, pol, bs)
+        d.check(st, f"step {s}")
+        assert np.array_equal(d.copied.cpu().numpy(), copied), f"step {s}"
+        seg[:, 3] += 1
+
+
+def test_2500_sharers_of_one_block():
+    announce("2500 sharers")
+    B, bs = 2500, 4096
+    st = {"table": np.zeros((B, 1), dtype=np.int32), "stack": list(range(B, 0, -1))}
+    st["ref"] = OS.recount(st["table"], B + 1)
+    seg = np.zeros((B, 4), dtype=np.int32)
+    seg[:, 3] = 1 + np.random.default_rng(5).integers(0, 900, B)
+    pol = np.tile(np.array([-1, 0, 0, -1, 0], dtype=np.int32), (B, 1))
+    d = Device(st)
+    d.step(i32(seg), i32(pol), bs, True)
+    copied = OS.step(st, seg, pol, bs)
+    d.check(st)
+    assert np.array_equal(d.copied.cpu().numpy(), copied) and (copied == -1).sum() == 1
+
+
 def test_step_on_unshared_rows_is_paged_step():
     announce("unshared rows against murmur_paged_step")
     rng = np.random.default_rng(9)
