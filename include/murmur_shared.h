@@ -112,6 +112,8 @@ int murmur_paged_compact(int32_t B, int32_t *block_table_dev, int32_t max_blocks
  * call of these sizes needs: a plan (16-byte aligned), which murmur_shared_plan
  * writes and murmur_decode_attn_shared reads, and a workspace (256-byte aligned)
  * for the partial sums.  Neither needs to be initialised; a larger buffer is fine.
+ * The sizes grow with B, max_keep and n_groups, so the buffers of the largest batch
+ * serve every smaller one.
  * At most 4096 sequences (MURMUR_EUNSUPPORTED beyond) and as many groups.
  * Calls that run at the same time need workspaces of their own, and may share a
  * plan. */
