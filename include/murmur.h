@@ -192,7 +192,9 @@ int murmur_evict_compact(const murmur_seg *seg_dev, const murmur_policy *pol_dev
  *   block_table_dev: device int32 [B][max_blocks], physical block numbers;
  *   block_size: a power of two;
  *   count_dev, ranges_dev: as murmur_evict_compact (ranges in sequence
- *               positions, not pool rows).
+ *               positions, not pool rows); for a murmur_seg of zeros, a sequence
+ *               that is not there (see murmur_shared.h), count -1, all slots -1, a
+ *               first length of -1 and zeros in ranges, and no error.
  * Errors as murmur_evict_compact; device error MURMUR_DEVERR_BLOCK (entry -1)
  * for a retained position past max_blocks blocks, in a block whose table
  * entry is negative (a freed block, see murmur_freeable_blocks_host), or in a

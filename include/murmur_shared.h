@@ -10,6 +10,14 @@
  *   murmur_shared_plan         -- what the groups share, and the work it makes;
  *   murmur_decode_attn_shared  -- per layer (or for all of them);
  * and now and then murmur_paged_compact.
+ *
+ * A sequence that is not there (a hypothesis that ended, a row of a padded batch) has
+ * a murmur_seg of zeros.  murmur_paged_step_shared leaves its row as it is, gives it
+ * no block and writes nothing for it; murmur_evict_compact_paged gives it the count
+ * -1; murmur_shared_plan takes a list of the count -1 (or a range table whose lengths
+ * add up to -1) for one that is not there, wherever it stands in its group: the others
+ * share as if it were not in it, and its outputs stay as they were.  None of this sets
+ * a bit of the device error word.
  */
 #ifndef MURMUR_SHARED_H
 #define MURMUR_SHARED_H
@@ -49,8 +57,8 @@ int murmur_paged_workspace(int32_t B, int32_t max_blocks, int32_t n_blocks, size
  * -1).  Rows copy names, not blocks; the first write into a block that several
  * rows name copies it (murmur_paged_step_shared).  Blocks that no row names any
  * more go onto the free stack, in the order of the first entry (by row, then
- * column) that named them.  What the new row's sequence is (its murmur_seg, its
- * tokens) is the caller's.
+ * column) that named them.  What the new row's sequence is (its murmur_seg, zeros if
+ * it has ended; its tokens) is the caller's.
  *   parent_dev: device int32 [B];
  *   ws_dev, ws_bytes: see murmur_paged_workspace.
  * Errors: MURMUR_EINVAL, MURMUR_ENOSPACE (workspace), MURMUR_EHIP; device error
@@ -73,7 +81,8 @@ int murmur_paged_fork(const int32_t *parent_dev, int32_t B, int32_t *block_table
  *   3. the current token's K and V are written into its row.
  *   copied_dev: device int32 [B], output: the block that a sequence's current block
  *               was copied from, -1 if it was not copied, -2 if nothing is written
- *               for the sequence (an invalid layout or policy, or no free block);
+ *               for the sequence (not there, an invalid layout or policy, or no
+ *               free block);
  *   every other argument as murmur_paged_step; with a pool, pool->max_len >=
  *   n_blocks * block_size.  Without one the copies that copied_dev names are the
  *   caller's to make.
@@ -131,14 +140,15 @@ int murmur_decode_attn_shared_workspace(int32_t n_layers, int32_t B, int32_t Hq,
  *               as they were;
  *   shared_dev: device int32 [n_groups]: how many leading list entries the group's
  *               sequences share.  find_shared 1: output, the most that the index
- *               lists allow (ranges_dev NULL; for a group of one its whole list);
+ *               lists allow (ranges_dev NULL; for a group of one its whole list;
+ *               0 if none of the group is there);
  *               0: input, a promise of the caller, who may share less than that;
  *   n_layers, Hq, Hkv: of each murmur_decode_attn_shared call that uses the plan;
  *   plan_dev, plan_bytes: see murmur_decode_attn_shared_workspace.
  * Errors: MURMUR_EINVAL, MURMUR_EUNSUPPORTED, MURMUR_ENOSPACE, MURMUR_EHIP.  Device
- * errors: MURMUR_DEVERR_COUNT for a sequence whose count is outside [1, max_keep] or
- * below what its group shares, and for all of a group that shares more than its
- * first sequence's count (NaN outputs); MURMUR_DEVERR_GROUP for groups out of order (every output is
+ * errors: MURMUR_DEVERR_COUNT for a sequence whose count is outside [1, max_keep] and
+ * not -1 or below what its group shares, and for all of a group that shares more than
+ * the count of its first sequence that is there (NaN outputs); MURMUR_DEVERR_GROUP for groups out of order (every output is
  * NaN). */
 int murmur_shared_plan(const int32_t *idx_dev, const int32_t *ranges_dev, const int32_t *count_dev, int32_t max_keep,
                        int32_t B, const int32_t *group_dev, int32_t n_groups, int32_t *shared_dev,
@@ -147,7 +157,7 @@ int murmur_shared_plan(const int32_t *idx_dev, const int32_t *ranges_dev, const 
 
 /* Decode-step attention (Equation 1) of every sequence over its list, as
  * murmur_decode_attn, reading what a group shares once: from the list, and in
- * sequence-ordered caches from the cache, of the group's first sequence.
+ * sequence-ordered caches from the cache, of the group's first sequence that is there.
  *   idx_dev, ranges_dev: the lists the plan was made from, unchanged since;
  *   n_groups:   of the plan;
  *   plan_dev, plan_bytes, ws_dev, ws_bytes: see

@@ -7,7 +7,7 @@ a dict ``st`` of ``table`` [B, max_blocks], ``ref`` [n_blocks] and ``stack`` (a 
                    entries are all gone is pushed when its first entry is met (row by row, column by column);
   * ``step``    -- one decode step: freeable blocks (oracle/paged.py's scan of later retained sets) are given up
                    sequence by sequence; then the writers, least far ahead first, each take a block, or copy one that
-                   someone else still names;
+                   someone else still names; a sequence whose layout is all zeros is not there;
   * ``compact`` -- the blocks in use, those behind the last one that is to stay moved one by one into the first free;
   * ``attend``  -- Equation 1 over a list of pool rows, in fp64;
   * ``common``  -- the leading entries that several lists share.
@@ -42,7 +42,8 @@ def step(st: dict, seg, pol, bs: int, freeable=None) -> np.ndarray:
     """Returns copied [B].  freeable(b): the sequence's blocks to give up (default: the oracle's scan)."""
     table, ref, stack, B = st["table"], st["ref"], st["stack"], len(seg)
     given = []
-    for b in range(B):
+    here = [b for b in range(B) if np.any(seg[b])]
+    for b in here:
         for blk in (freeable(b) if freeable else OP.freeable_blocks(seg[b], pol[b], bs)):
             if blk < table.shape[1] and table[b, blk] >= 0:
                 given.append(int(table[b, blk]))
@@ -52,10 +53,11 @@ def step(st: dict, seg, pol, bs: int, freeable=None) -> np.ndarray:
         if ref[x] == 0 and x not in stack:
             stack.append(x)
     pos = seg.sum(axis=1) - 1
-    copied = np.full(B, -1, dtype=np.int32)
+    copied = np.full(B, -2, dtype=np.int32)
+    copied[here] = -1
     wants = np.zeros(B, dtype=bool)
     named = ref.copy()
-    for b in sorted(range(B), key=lambda b: (pos[b], b)):
+    for b in sorted(here, key=lambda b: (pos[b], b)):
         x = table[b, pos[b] // bs]
         if x < 0:
             wants[b] = True

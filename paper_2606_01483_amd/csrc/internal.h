@@ -248,7 +248,7 @@ struct PlanHeader {
     int32_t rows, level, unused[4];       // partial rows per (layer, KV head); the cut (below 0: no list is cut)
 };
 struct PlanSeq {
-    int32_t state;  // 0: not in any group (outputs untouched), 1: computed, 2: invalid count (NaN outputs)
+    int32_t state;  // 0: not there or in no group (outputs untouched), 1: computed, 2: invalid count (NaN outputs)
     int32_t pre_row, pre_stride, n_pre;  // partials over the prefix: rows pre_row + i * pre_stride + head
     int32_t rest_row, n_rest;            // over the rest: rows rest_row + i * G + head
     int32_t rest, unused;                // length of the rest (plans without cuts)

@@ -53,7 +53,8 @@ static __device__ __forceinline__ void raise_device_error(int32_t bit) { atomicO
 // With a block table (paged cache, bt != null) the index list holds pool rows
 // (paged_pool_row): a position past the table's max_blocks entries, in a freed
 // block (negative entry) or in a row beyond 2^31 - 1 gives -1 and
-// MURMUR_DEVERR_BLOCK.
+// MURMUR_DEVERR_BLOCK; and a sequence that is not there (layout_absent) has no list
+// and is no error.
 static __device__ __forceinline__ int32_t paged_row(const int32_t *bt_row, int32_t max_blocks, int32_t log2_bs,
                                                     int32_t p, int &bad) {
     const int32_t row = paged_pool_row(bt_row, max_blocks, log2_bs, p);
@@ -77,11 +78,13 @@ __global__ __launch_bounds__(256) void evict_compact_kernel(const murmur_seg *__
                                    p.speech_delay, p.speech_sink, p.out_window, p.out_sink, &pc);
     int32_t *row = idx + (int64_t)b * max_keep;
     if (rc != 0) {
+        const bool absent = bt && layout_absent(s.prompt_pre, s.speech_len, s.prompt_mid, s.out_len);
         if (tid == 0) {
-            count[b] = 0;
-            raise_device_error(MURMUR_DEVERR_POLICY);
+            count[b] = absent ? kAbsent : 0;
+            if (!absent) raise_device_error(MURMUR_DEVERR_POLICY);
         }
-        if (ranges && tid < 2 * kPieces) ranges[b * 2 * kPieces + tid] = 0;
+        // the lengths of a table add up to the count
+        if (ranges && tid < 2 * kPieces) ranges[b * 2 * kPieces + tid] = absent && tid == 1 ? kAbsent : 0;
         for (int r = tid; r < max_keep; r += blockDim.x) row[r] = -1;
         return;
     }

@@ -299,7 +299,10 @@ __global__ __launch_bounds__(kThreads) void step_shared_kernel(const murmur_seg 
     tp = tp < 0 ? 0 : (tp > n_blocks ? n_blocks : tp);
     int err = 0;
     const auto load_seq = [&](int b) {
-        StepSeq s{paged_seq(seg, pol, pol_per_seq, b, B, max_blocks, log2_bs, full_scan, err), 0, -1};
+        int bad = 0;
+        StepSeq s{paged_seq(seg, pol, pol_per_seq, b, B, max_blocks, log2_bs, full_scan, bad), 0, -1};
+        // a sequence that is not there gives up, takes and writes nothing, and is no error
+        if (bad && !layout_absent(seg[b].prompt_pre, seg[b].speech_len, seg[b].prompt_mid, seg[b].out_len)) err |= bad;
         if (s.q.valid) {
             s.pos = (int32_t)seq_position(seg[b]);
             if (s.q.cur < max_blocks) s.x = bt[(int64_t)b * max_blocks + s.q.cur];

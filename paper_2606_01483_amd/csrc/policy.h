@@ -62,6 +62,14 @@ MURMUR_HD inline bool layout_valid(int32_t p_pre, int32_t l_s, int32_t p_mid, in
     return (int64_t)p_pre + l_s + p_mid + j <= 0x7fffffffLL;
 }
 
+// Whether a layout says that there is no sequence (a hypothesis that ended, a row
+// of a padded batch): all zeros.  The calls on shared pages pass over it; the rest
+// find an invalid layout (j < 1).
+MURMUR_HD inline bool layout_absent(int32_t p_pre, int32_t l_s, int32_t p_mid, int32_t j) {
+    return (p_pre | l_s | p_mid | j) == 0;
+}
+constexpr int32_t kAbsent = -1;  // the retained count of such a sequence
+
 // 32-bit sums and differences that wrap instead of overflowing: for a valid
 // layout every intermediate value fits, so they are exact there.
 MURMUR_HD inline int32_t wrap_add(int32_t a, int32_t b) { return (int32_t)((uint32_t)a + (uint32_t)b); }

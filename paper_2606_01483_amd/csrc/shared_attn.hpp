@@ -28,8 +28,9 @@ static __device__ __forceinline__ int list_count(const int32_t *ranges, const in
 }
 
 // Workgroup (x, b) compares entries [kScanLen x, kScanLen (x + 1)) of list b with
-// those of the first list of its group: the first rank that differs, or max_keep.
-// Three round trips: the groups, the counts, the entries (16 a thread at once).
+// those of the first list of its group that is there: the first rank that differs, or
+// max_keep.  Three round trips: the groups, the counts, the entries (16 a thread at
+// once); two more where the group's first sequence is not there.
 constexpr int kScanThreads = 256;
 constexpr int kScanEach = kScanLen / kScanThreads;
 __global__ __launch_bounds__(kScanThreads) void shared_scan_kernel(const int32_t *__restrict__ idx,
@@ -37,11 +38,12 @@ __global__ __launch_bounds__(kScanThreads) void shared_scan_kernel(const int32_t
                                                                    const int32_t *__restrict__ group,
                                                                    int32_t n_groups, int32_t max_keep, int32_t B,
                                                                    int32_t *__restrict__ scan) {
-    __shared__ int s_lead, s_min;
+    __shared__ int s_lead, s_min, s_first;
     const int tid = threadIdx.x, b = blockIdx.y;
     if (tid == 0) {
         s_lead = -1;
         s_min = max_keep;
+        s_first = b;
     }
     __syncthreads();
     int start = -1;  // the last group start at or before b
@@ -53,7 +55,7 @@ __global__ __launch_bounds__(kScanThreads) void shared_scan_kernel(const int32_t
     __syncthreads();
     const int lead = s_lead;
     if (lead >= 0 && lead < b) {
-        const int n = min(min(count[b], count[lead]), max_keep);
+        int n = min(min(count[b], count[lead]), max_keep);
         const int32_t *mine = idx + (int64_t)b * max_keep, *first = idx + (int64_t)lead * max_keep;
         const int r0 = (int)blockIdx.x * kScanLen + tid, last = max_keep - 1;
         int32_t x[kScanEach], y[kScanEach];
@@ -62,6 +64,18 @@ __global__ __launch_bounds__(kScanThreads) void shared_scan_kernel(const int32_t
             const int r = min(r0 + j * kScanThreads, last);
             x[j] = mine[r];
             y[j] = first[r];
+        }
+        if (__builtin_expect(count[lead] == kAbsent, 0)) {  // uniform
+            for (int i = lead + 1 + tid; i < b; i += kScanThreads)
+                if (count[i] != kAbsent) {
+                    atomicMin(&s_first, i);
+                    break;
+                }
+            __syncthreads();
+            n = min(min(count[b], count[s_first]), max_keep);  // itself, if none before it is there: nothing differs
+            first = idx + (int64_t)s_first * max_keep;
+#pragma unroll
+            for (int j = 0; j < kScanEach; ++j) y[j] = first[min(r0 + j * kScanThreads, last)];
         }
         int at = max_keep;
 #pragma unroll
@@ -107,15 +121,19 @@ constexpr int kFindHereEntries = 4096;
 // highest; the wavefronts add up eight levels side by side, then the eight between
 // two of them.
 struct PlanLds {
-    int rest[kSharedMaxSeqs];           // by sequence: length of the rest, -1 if the sequence is left out
+    int rest[kSharedMaxSeqs];           // by sequence: length of the rest, or one of the two below
     uint16_t of[kSharedMaxSeqs];        // its group
     int lo[kSharedMaxSeqs + 1];         // by group: first sequence
+    int lead[kSharedMaxSeqs];           // the first one that is there, whose list is read (the next group's first: none)
     int common[kSharedMaxSeqs];         // what it shares
     int row[kSharedMaxSeqs], item[kSharedMaxSeqs];  // its first partial row and item
     int cuts[kSharedMaxSeqs];
     int scan[16], work[2][8], bad;
     unsigned positions;
 };
+constexpr int kInvalid = -1, kNotThere = -2;  // PlanLds::rest: the count is invalid; kAbsent
+static __device__ __forceinline__ int32_t seq_state(int rest) { return rest >= 0 ? 1 : (rest == kInvalid ? 2 : 0); }
+
 // Workgroups that read the same rows should share an L2.  Workgroup w of a launch runs
 // on XCD w mod 8, and the (layer, KV head) is the fastest index of the grid, so with
 // `heads` of them item i of a head runs on one of 8 / gcd(8, heads) XCDs in turn.  Item
@@ -148,7 +166,7 @@ static __device__ __forceinline__ void plan_whole(const SharedPlanLaunch &p, Pla
         const int rest = b < end ? max(l.rest[b], 0) : 0;
         if (b < end) {
             PlanSeq s = {};
-            s.state = l.rest[b] >= 0 ? 1 : 2;
+            s.state = seq_state(l.rest[b]);
             s.rest = rest;
             seqs[b] = s;
             atomicAdd(&l.row[l.of[b]], div_up(rest, kWaveTile));
@@ -194,13 +212,13 @@ static __device__ __forceinline__ void plan_whole(const SharedPlanLaunch &p, Pla
     __syncthreads();
 #pragma unroll 1
     for (int g = wave; g < n_groups; g += kPlanThreads / 64) {
-        const int lo = l.lo[g], n = l.lo[g + 1] - lo, parts = small_div_up(n, per);
+        const int lo = l.lo[g], lead = l.lead[g], n = l.lo[g + 1] - lo, parts = small_div_up(n, per);
         const Dealt dealt(n, max(parts, 1));
 #pragma unroll 1
         for (int i = lane; i < parts; i += 64) {
             const int s0 = dealt.start(i), s1 = dealt.start(i + 1);
             items[item_place(l.item[g] + i, work, heads)] =
-                PlanItem{lo + s0, s1 - s0, lo, 0, max(l.common[g], 0), 0, stream && parts <= 2, 0};
+                PlanItem{lo + s0, s1 - s0, lead, 0, max(l.common[g], 0), 0, stream && parts <= 2, 0};
         }
     }
     if (tid == 0) {
@@ -233,8 +251,14 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     for (int g = tid; g < n_groups; g += kPlanThreads) l.common[g] = p.find ? max_keep : p.shared[g];
     __syncthreads();
 #pragma unroll 1
-    for (int g = tid; g < n_groups; g += kPlanThreads)
-        if (l.lo[g] < 0 || l.lo[g] > l.lo[g + 1] || l.lo[g + 1] > B || (g == 0 && l.lo[0] != 0)) l.bad = 1;
+    for (int g = tid; g < n_groups; g += kPlanThreads) {
+        const int lo = l.lo[g], hi = l.lo[g + 1];
+        int lead = lo;
+        if (lo < 0 || lo > hi || hi > B || (g == 0 && lo != 0)) l.bad = 1;
+        else
+            while (lead < hi && l.rest[lead] == kAbsent) ++lead;
+        l.lead[g] = lead;
+    }
     __syncthreads();
     const int bad = l.bad, end = bad ? 0 : l.lo[n_groups];
     if (tid == 0) {
@@ -265,7 +289,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
         }
         l.of[b] = (uint16_t)lo;
         const int c = l.rest[b];
-        if (p.find && ((c >= 1 && c <= max_keep) || b == l.lo[lo])) atomicMin(&l.common[lo], max(c, 0));
+        if (p.find && ((c >= 1 && c <= max_keep) || b == l.lead[lo])) atomicMin(&l.common[lo], max(c, 0));
     }
     __syncthreads();
     if (p.find == kFindHere) {
@@ -280,7 +304,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
                 b[j] = small_div(t, max_keep);
                 r[j] = t - b[j] * max_keep;
                 x[j] = p.idx[t];
-                y[j] = p.idx[l.lo[l.of[b[j]]] * max_keep + r[j]];
+                y[j] = p.idx[min(l.lead[l.of[b[j]]], b[j]) * max_keep + r[j]];  // a list that is not there: any one
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -297,13 +321,14 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
         }
         __syncthreads();
     }
-    // what is shared has to be in the group's first list, which is the one that is read (-1: it is not)
+    // what is shared has to be in the list that is read, the first one that is there (-1: it is not)
 #pragma unroll 1
     for (int g = tid; g < n_groups; g += kPlanThreads) {
-        const int lo = l.lo[g];
-        int common = lo < l.lo[g + 1] ? l.common[g] : 0;
+        const int lead = l.lead[g];
+        const bool some = lead < l.lo[g + 1];
+        int common = some ? l.common[g] : 0;
         if (p.find) p.shared[g] = common;
-        else if (common != 0 && lo < l.lo[g + 1] && !(common > 0 && common <= l.rest[lo] && l.rest[lo] <= max_keep)) common = -1;
+        else if (common != 0 && some && !(common > 0 && common <= l.rest[lead] && l.rest[lead] <= max_keep)) common = -1;
         l.common[g] = common;
     }
     __syncthreads();
@@ -312,9 +337,10 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     for (int b = tid; b < B; b += kPlanThreads) {
         const int c = l.rest[b], common = b < end ? l.common[l.of[b]] : 0;
         const bool good = c >= 1 && c <= max_keep && common >= 0 && c >= common;
-        if (b < end && !good) err |= MURMUR_DEVERR_COUNT;
-        seqs[b].state = b >= end ? 0 : (good ? 1 : 2);
-        l.rest[b] = b < end && good ? c - common : -1;
+        const int rest = b >= end || c == kAbsent ? kNotThere : (good ? c - common : kInvalid);
+        if (rest == kInvalid) err |= MURMUR_DEVERR_COUNT;
+        seqs[b].state = seq_state(rest);
+        l.rest[b] = rest;
     }
     if (err) raise_device_error(err);
     __syncthreads();
@@ -392,7 +418,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
             const int cut = small_div(i, parts), part = i - cut * parts;
             const int s0 = to_parts.start(part), s1 = to_parts.start(part + 1);
             const int r0 = to_cuts.start(cut) * kWaveTile, r1 = min(to_cuts.start(cut + 1) * kWaveTile, common);
-            items[item_place(l.item[g] + i, work, heads)] = PlanItem{lo + s0, s1 - s0, lo, r0, r1, l.row[g] + (cut * n + s0) * G,
+            items[item_place(l.item[g] + i, work, heads)] = PlanItem{lo + s0, s1 - s0, l.lead[g], r0, r1, l.row[g] + (cut * n + s0) * G,
                          stream && parts <= 2, 0};
         }
     }
@@ -421,7 +447,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
                                                 row + ((at + i) / kSharedWaves - at / kSharedWaves) * G};
         }
         PlanSeq s = {};
-        s.state = l.rest[b] >= 0 ? 1 : 2;
+        s.state = seq_state(l.rest[b]);
         s.pre_row = l.row[g] + (b - lo) * G;
         s.pre_stride = n_seq * G;
         s.n_pre = l.cuts[g];
@@ -864,7 +890,8 @@ struct SharedLds {
     float ml[kWaves][32][2];  // per wavefront and row of a round: max (log2 units), sum
     int flag[kWaves];
     int seq[kWaves + 1], row[kWaves];
-    unsigned long long bad;   // sequences of the item with a position outside the cache
+    unsigned long long bad;   // sequences of the item with a position outside the cache or an invalid count
+    unsigned long long gone;  // those that are not there
 };
 
 // Up to two of a wavefront's tiles into its own stage and the pairs, for the sums
@@ -1065,8 +1092,11 @@ static __device__ __forceinline__ void whole_work(const SharedAttnLaunch &a, con
     if (tid == 0) l.bad = 0;
     __syncthreads();
     if (wave == 0) {
-        const uint64_t invalid = __ballot(state != 1);
-        if (lane == 0 && invalid) atomicOr(&l.bad, invalid);
+        const uint64_t invalid = __ballot(state == 2), gone = __ballot(state == 0);
+        if (lane == 0) {
+            if (invalid) atomicOr(&l.bad, invalid);
+            l.gone = gone;
+        }
     }
     const int passes = (rest + kWaveTile - 1) / kWaveTile;
     int upto = passes;
@@ -1096,10 +1126,11 @@ static __device__ __forceinline__ void whole_work(const SharedAttnLaunch &a, con
             }
         });
     const auto store = [&](int t0, int n_tiles) {
-        const uint64_t bad = l.bad;
+        const uint64_t bad = l.bad, gone = l.gone;
 #pragma unroll 1
         for (int j = tid >> 5; j < min(16 * n_tiles, rows - 16 * t0); j += kWaves * 2) {
             const uint32_t rr = (uint32_t)(16 * t0 + j), s = div16(rr, a.magic_g);
+            if (gone >> s & 1) continue;
             float M, L;
             f32x4 O;
             gather_row<kWaves>(l, 0, kWaves, j, tid & 31, M, L, O);

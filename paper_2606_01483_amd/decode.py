@@ -11,6 +11,8 @@ synchronisation.
 """
 from __future__ import annotations
 
+import contextlib
+
 import numpy as np
 import torch
 
@@ -558,7 +560,11 @@ class BeamBatch:
     Memory plumbing only: the pool [NL][n_blocks * block_size][Hkv][D], the block table [chunks * width][max_blocks],
     reference counts, free stack, workspaces and outputs.  The host prefill gives every position before step 0's
     current token of each chunk a block, which all of its sequences name.  What the hypotheses are is the caller's:
-    step() takes their parents, queries and current-token K/V."""
+    step() takes their parents, queries and current-token K/V.
+
+    `live` [chunks * width, 1] follows the parents on the device: 0 from a parent of -1 on, until the row continues a
+    live one again.  A row that is not live holds no block, its queries and K/V are not looked at (zeros in the
+    murmur_seg of its step, `now`), and its outputs stay as they were."""
 
     def __init__(self, wl: Workload, width: int, block_size: int, n_blocks: int, device: str = "cuda",
                  out_dtype: int = M.MURMUR_DTYPE_F32):
@@ -600,6 +606,8 @@ class BeamBatch:
         self.stack, self.top = i32(stack + [0] * (self.n_blocks - len(stack))), i32([len(stack)])
         self.pol = i32(np.repeat(np.asarray(wl.policy), self.width, axis=0))
         self.seg = i32(np.stack([np.repeat(wl.seg(s), self.width, axis=0) for s in range(wl.steps)]))
+        self.live, self.now = i32(np.ones((self.B, 1))), i32(np.zeros((self.B, 4)))
+        self.row = i32(np.arange(self.B))
         self.group = i32(np.arange(chunks + 1) * self.width)
         self.shared, self.copied, self.map = i32(np.zeros(chunks)), i32(np.zeros(self.B)), i32(np.zeros(self.n_blocks))
         self.idx, self.count = i32(np.full((self.B, self.max_keep), -1)), i32(np.zeros(self.B))
@@ -613,17 +621,29 @@ class BeamBatch:
         self.ws = torch.zeros(self.ws_bytes // 4, dtype=torch.int32, device=dev)
 
     def state(self) -> tuple:
-        """Copies of everything a step changes (pool, table, counts, stack, top)."""
-        return tuple(t.clone() for t in (self.k, self.v, self.bt, self.ref, self.stack, self.top))
+        """Copies of everything a step changes (pool, table, counts, stack, top, live)."""
+        return tuple(t.clone() for t in (self.k, self.v, self.bt, self.ref, self.stack, self.top, self.live))
 
     def restore(self, st: tuple) -> None:
-        for t, s in zip((self.k, self.v, self.bt, self.ref, self.stack, self.top), st):
+        for t, s in zip((self.k, self.v, self.bt, self.ref, self.stack, self.top, self.live), st):
             t.copy_(s)
+
+    @staticmethod
+    def _on(stream):
+        """The context of torch's own operations on `stream` (as the calls take it)."""
+        if stream is None:
+            return contextlib.nullcontext()
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+        return torch.cuda.stream(stream)
 
     def fork(self, parent, stream=None) -> None:
         """Sequence b continues what sequence parent[b] was (int32 [B] on the device; -1 ends it)."""
         M.murmur_paged_fork(parent, self.B, self.bt, self.max_blocks, self.ref, self.n_blocks, self.stack, self.top,
                             self.n_blocks, self.pages_ws, self.pages_bytes, stream)
+        with self._on(stream):  # a parent outside [-1, B) leaves the row as it is
+            source = torch.where(parent == parent.clamp(-1, self.B - 1), parent, self.row)
+            self.live.copy_(torch.where(source < 0, 0, self.live[source.clamp(min=0).long(), 0])[:, None])
 
     def compact(self, stream=None) -> None:
         """Moves the blocks in use to the front of the pool."""
@@ -634,10 +654,12 @@ class BeamBatch:
         """Step i: fork, then the current token (k_new, v_new [NL, B, Hkv, D]) and its attention (q [NL, B, Hq, D])."""
         if parent is not None:
             self.fork(parent, stream)
-        M.murmur_paged_step_shared(self.seg[i], self.pol, 1, self.B, self.bt, self.max_blocks, self.bs, self.ref,
+        with self._on(stream):
+            torch.mul(self.seg[i], self.live, out=self.now)
+        M.murmur_paged_step_shared(self.now, self.pol, 1, self.B, self.bt, self.max_blocks, self.bs, self.ref,
                                    self.n_blocks, self.stack, self.top, self.n_blocks, i == 0, self.copied, self.kv,
                                    self.Hkv, k_new, v_new, stream)
-        M.murmur_evict_compact_paged(self.seg[i], self.pol, 1, self.B, self.bt, self.max_blocks, self.bs, self.idx,
+        M.murmur_evict_compact_paged(self.now, self.pol, 1, self.B, self.bt, self.max_blocks, self.bs, self.idx,
                                      self.max_keep, self.count, None, stream)
         M.murmur_shared_plan(self.idx, None, self.count, self.max_keep, self.B, self.group, self.groups, self.shared,
                              True, self.NL, self.Hq, self.Hkv, self.plan, self.plan_bytes, stream)
