@@ -80,9 +80,10 @@ int murmur_paged_fork(const int32_t *parent_dev, int32_t B, int32_t *block_table
  *      block, if nobody else names it.  Blocks are popped in sequence order;
  *   3. the current token's K and V are written into its row.
  *   copied_dev: device int32 [B], output: the block that a sequence's current block
- *               was copied from, -1 if it was not copied, -2 if nothing is written
- *               for the sequence (not there, an invalid layout or policy, or no
- *               free block);
+ *               was copied from, -1 if it was not copied (nor is a token past the
+ *               table, which has no row to be written to), -2 if nothing is written
+ *               for the sequence (not there, an invalid layout or policy, a current
+ *               block of n_blocks or more, or no free block);
  *   every other argument as murmur_paged_step; with a pool, pool->max_len >=
  *   n_blocks * block_size.  Without one the copies that copied_dev names are the
  *   caller's to make.

@@ -382,6 +382,7 @@ __global__ __launch_bounds__(kThreads) void step_shared_kernel(const murmur_seg 
         } else if (s.q.valid && s.x < 0) {
             what = kTakeBlock;
         } else if (s.q.valid && s.x >= n_blocks) {
+            what = -2;  // a caller's pool may be larger than its blocks: no rows behind them are written
             err |= MURMUR_DEVERR_BLOCK;
         } else if (s.q.valid) {
             holders = load_count(ref + s.x);
