@@ -89,7 +89,8 @@ enum {
     MURMUR_DEVERR_BLOCK = 32,    /* evict_compact_paged: a retained position past the block table or in a freed block */
     MURMUR_DEVERR_POOL = 64,     /* paged_step: the free stack ran out (or overflowed its capacity) */
     MURMUR_DEVERR_PARENT = 128,  /* paged_fork: a parent outside [-1, B) */
-    MURMUR_DEVERR_GROUP = 256,   /* shared_plan: groups out of order; decode_attn_shared: a plan of another call */
+    MURMUR_DEVERR_GROUP = 256,   /* shared_plan: groups out of order; decode_attn_shared: a plan of another call, or
+                                  * shares found from lists where sequences have caches of their own */
 };
 
 /* One sequence (audio chunk) of the batch, Section 3.2's layout

@@ -143,7 +143,8 @@ int murmur_decode_attn_shared_workspace(int32_t n_layers, int32_t B, int32_t Hq,
  *               sequences share.  find_shared 1: output, the most that the index
  *               lists allow (ranges_dev NULL; for a group of one its whole list;
  *               0 if none of the group is there);
- *               0: input, a promise of the caller, who may share less than that;
+ *               0: input, a promise of the caller, who may share less than that
+ *               (the way for sequence-ordered caches, whose lists do not tell);
  *   n_layers, Hq, Hkv: of each murmur_decode_attn_shared call that uses the plan;
  *   plan_dev, plan_bytes: see murmur_decode_attn_shared_workspace.
  * Errors: MURMUR_EINVAL, MURMUR_EUNSUPPORTED, MURMUR_ENOSPACE, MURMUR_EHIP.  Device
@@ -166,8 +167,9 @@ int murmur_shared_plan(const int32_t *idx_dev, const int32_t *ranges_dev, const 
  *   every other argument and the outputs as murmur_decode_attn.
  * Accumulation is fp32 throughout.  Errors as murmur_decode_attn; device errors
  * MURMUR_DEVERR_POSITION (NaN for the sequences whose lists hold the position) and
- * MURMUR_DEVERR_GROUP for a plan that was not made for these sizes (every output is
- * NaN). */
+ * MURMUR_DEVERR_GROUP for a plan that was not made for these sizes, or with
+ * find_shared 1 where kv->stride_b is not 0 and lists of several sequences begin alike:
+ * equal positions of two caches are different rows (every output is NaN). */
 int murmur_decode_attn_shared(const void *q_dev, const murmur_kv *kv, const int32_t *idx_dev,
                               const int32_t *ranges_dev, int32_t max_keep, int32_t B, int32_t n_groups, int32_t Hq,
                               int32_t Hkv, int32_t D, float scale, void *out_dev, int32_t out_dtype, float *lse_dev,

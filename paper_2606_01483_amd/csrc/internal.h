@@ -243,10 +243,14 @@ constexpr int chunk_passes(int level) { return level * 3 / 8; }
 constexpr int kScanLen = 4096;
 constexpr int32_t kPlanMagic = 0x6d75726d;
 struct PlanHeader {
-    int32_t magic, n_work, bad, unused0;  // bad: the groups are not in order; every output is NaN
+    int32_t magic, n_work, bad, kind;     // bad: the groups are not in order; every output is NaN; kind: see plan_kind
     int32_t B, max_keep, n_layers, Hq, Hkv, n_groups;  // what the plan was made for
     int32_t rows, level, unused[4];       // partial rows per (layer, KV head); the cut (below 0: no list is cut)
 };
+// A plan's kind, one bit of four: whether lists are cut or whole, and whether lists of
+// several sequences were found to begin alike (then they name the same rows in one
+// cache only, and the plan does not serve caches of the sequences' own).
+constexpr int32_t plan_kind(bool whole, bool found) { return (whole ? 2 : 1) << (found ? 2 : 0); }
 struct PlanSeq {
     int32_t state;  // 0: not there or in no group (outputs untouched), 1: computed, 2: invalid count (NaN outputs)
     int32_t pre_row, pre_stride, n_pre;  // partials over the prefix: rows pre_row + i * pre_stride + head
@@ -292,9 +296,11 @@ struct SharedAttnLaunch {
     float *part_ml;  // [layers * KV heads][rows][2]  (running max in log2 units, sum)
     int64_t rows_cap;
     int32_t max_len, max_keep, B, Hq, Hkv, G, NL, n_groups, n_wg, out_f32;
-    int32_t waves;     // SharedCaps::waves, 0 where lists are cut
+    int32_t kinds;     // plans that serve the call, bits of plan_kind (16 bytes with n_wg: one load at a kernel's
+                       // start; behind magic_g and scale_log2 it came later, 0.3 us a launch)
     uint32_t magic_g;  // magic16(G): row / G for rows below 2^16
     float scale_log2;
+    int32_t waves;     // SharedCaps::waves, 0 where lists are cut
 };
 int launch_decode_attn_shared(const SharedAttnLaunch &a, murmur_stream_t stream);
 

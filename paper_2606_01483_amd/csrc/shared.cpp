@@ -371,6 +371,7 @@ MURMUR_EXPORT int murmur_decode_attn_shared(const void *q_dev, const murmur_kv *
     a.n_groups = n_groups;
     a.n_wg = c.grid;
     a.waves = c.whole ? c.waves : 0;
+    a.kinds = plan_kind(c.whole, false) | (kv->stride_b == 0 ? plan_kind(c.whole, true) : 0);
     a.out_f32 = out_dtype == MURMUR_DTYPE_F32;
     a.magic_g = (uint32_t)((((uint64_t)1 << 32) + a.G - 1) / a.G - 1);
     a.scale_log2 = scale * 1.4426950408889634f;

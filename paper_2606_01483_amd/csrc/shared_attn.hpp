@@ -128,7 +128,7 @@ struct PlanLds {
     int common[kSharedMaxSeqs];         // what it shares
     int row[kSharedMaxSeqs], item[kSharedMaxSeqs];  // its first partial row and item
     int cuts[kSharedMaxSeqs];
-    int scan[16], work[2][8], bad;
+    int scan[16], work[2][8], bad, found;
     unsigned positions;
 };
 constexpr int kInvalid = -1, kNotThere = -2;  // PlanLds::rest: the count is invalid; kAbsent
@@ -223,6 +223,7 @@ static __device__ __forceinline__ void plan_whole(const SharedPlanLaunch &p, Pla
     }
     if (tid == 0) {
         h->n_work = work;
+        h->kind = plan_kind(true, l.found);
         h->rows = 0;
         h->level = -per;
     }
@@ -242,7 +243,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     const int n_scan = p.caps.n_scan;
 
     // the groups, and every sequence's count (in `rest` for now)
-    if (tid == 0) l.bad = l.positions = 0;
+    if (tid == 0) l.bad = l.found = l.positions = 0;
 #pragma unroll 1
     for (int b = tid; b < B; b += kPlanThreads) l.rest[b] = list_count(p.ranges, p.count, b);
 #pragma unroll 1
@@ -339,6 +340,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
         const bool good = c >= 1 && c <= max_keep && common >= 0 && c >= common;
         const int rest = b >= end || c == kAbsent ? kNotThere : (good ? c - common : kInvalid);
         if (rest == kInvalid) err |= MURMUR_DEVERR_COUNT;
+        if (p.find && rest >= 0 && common > 0 && b != l.lead[l.of[b]]) l.found = 1;
         seqs[b].state = seq_state(rest);
         l.rest[b] = rest;
     }
@@ -462,6 +464,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     for (int w = tid; w < rest_wg; w += kPlanThreads) items[work + w] = PlanItem{0, 0, 0, 0, 0, 0, stream, 0};
     if (tid == 0) {
         h->n_work = work + rest_wg;
+        h->kind = plan_kind(false, l.found);
         h->rows = rows;
         h->level = level;
     }
@@ -1039,7 +1042,7 @@ static __device__ __forceinline__ void chunk_work(const SharedAttnLaunch &a, con
 static __device__ __forceinline__ bool plan_fits(const SharedAttnLaunch &a, const PlanHeader &h) {
     return h.magic == kPlanMagic && !h.bad && h.B == a.B && h.max_keep == a.max_keep && h.n_layers == a.NL &&
            h.Hq == a.Hq && h.Hkv == a.Hkv && h.n_groups == a.n_groups && h.rows <= a.rows_cap && h.n_work <= a.n_wg &&
-           (h.level < 0) == (a.waves > 0);
+           (h.kind & a.kinds);
 }
 
 template <int kTerms, int kSrc, bool kNear>

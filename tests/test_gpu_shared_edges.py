@@ -5,6 +5,8 @@ import torch
 
 from oracle import shared as OS
 from paper_2606_01483_amd import murmur as M
+from _shared import attn_bounds
+from test_gpu_shared_attn import CUT, bf16
 from test_gpu_shared_pages import Device, grown_pool, i32
 
 pytestmark = pytest.mark.gpu
@@ -48,3 +50,55 @@ def test_a_current_block_behind_the_pools_blocks(block):
         y[:, 12] = y[:, 4]
         y[:, 12 + 1] = 77
         assert torch.equal(x, y)
+
+
+def own_caches(lists, extra_keep, stride_b=True):
+    """Lists of positions over sequence-ordered caches [1, B, 2, 64, 128] (one for all without stride_b)."""
+    rng = np.random.default_rng(41)
+    B, keep = len(lists), max(len(x) for x in lists) + extra_keep
+    idx = np.full((B, keep), -1, dtype=np.int32)
+    for b, x in enumerate(lists):
+        idx[b, :len(x)] = x
+    q, k, v = bf16(rng, 1, B, 4, 128), bf16(rng, 1, B, 2, 64, 128), bf16(rng, 1, B, 2, 64, 128)
+    if not stride_b:
+        k[:], v[:] = k[:, :1].clone(), v[:, :1].clone()
+    kv = M.make_kv(k, v, 1, 64, (B * 2 * 64 * 128, 2 * 64 * 128 if stride_b else 0, 64 * 128, 128))
+    return q, k, v, kv, i32(idx), i32([len(x) for x in lists]), keep
+
+
+@pytest.mark.parametrize("extra_keep", [0, CUT])
+@pytest.mark.parametrize("refused,group,find,stride_b", [
+    (True, [0, 2, 3], True, True),     # equal positions of two caches: other rows
+    (False, [0, 2, 3], False, True),   # the caller's promise
+    (False, [0, 1, 2, 3], True, True),  # every sequence by itself
+    (False, [0, 1, 3], True, True),    # two that share nothing
+    (False, [0, 2, 3], True, False),   # one cache for all
+])
+def test_shares_found_in_caches_of_their_own(refused, group, find, stride_b, extra_keep):
+    """Equal positions are the same rows in one cache only: found shares are refused where sequences have their own."""
+    announce(f"groups {group}, find {find}, caches of their own {stride_b}, +{extra_keep}")
+    lists = [list(range(40)), list(range(35)) + [50, 51], [9] + list(range(20, 45))]
+    q, k, v, kv, idx, count, keep = own_caches(lists, extra_keep, stride_b)
+    n = len(group) - 1
+    ws_bytes, plan_bytes = M.murmur_decode_attn_shared_workspace(1, 3, 4, 2, keep, n)
+    ws, plan = (torch.zeros(x // 4, dtype=torch.int32, device="cuda") for x in (ws_bytes, plan_bytes))
+    out, lse, shared = torch.full((1, 3, 4, 128), 55.0, device="cuda"), torch.full((1, 3, 4), 55.0, device="cuda"), i32([20] + [0] * (n - 1))
+    if not find:
+        for x in (k, v):
+            x[0, 1, :, :20] = x[0, 0, :, :20]
+    M.murmur_shared_plan(idx, None, count, keep, 3, i32(group), n, shared, find, 1, 4, 2, plan, plan_bytes)
+    M.murmur_decode_attn_shared(q, kv, idx, None, keep, 3, n, 4, 2, 128, 0.1, out, M.MURMUR_DTYPE_F32, lse, plan, plan_bytes,
+                                ws, ws_bytes)
+    torch.cuda.synchronize()
+    if refused:
+        assert M.murmur_device_error() == M.MURMUR_DEVERR_GROUP
+        assert torch.isnan(out).all() and torch.isnan(lse).all()
+        return
+    assert M.murmur_device_error() == 0
+    for b, x in enumerate(lists):
+        rows = [y[0, b].float().cpu().numpy()[:, x].transpose(1, 0, 2) for y in (k, v)]
+        args = q[0, b].float().cpu().numpy(), *rows, 0.1
+        want, want_lse = OS.attend(*args)
+        far, far_lse = attn_bounds(*args, want, want_lse)
+        assert (np.abs(out[0, b].cpu().numpy() - want) <= far).all(), b
+        assert (np.abs(lse[0, b].cpu().numpy() - want_lse) <= far_lse).all(), b
