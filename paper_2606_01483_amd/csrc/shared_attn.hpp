@@ -649,6 +649,10 @@ struct WholeLists {  // every step-th pass of an item: those of the prefix, then
 // A running max that is below every logit and finite, so that a row which a pass
 // leaves out entirely (every logit -inf) stays as it is: exp2 of -inf, not of NaN.
 constexpr float kNoRows = -3.0e38f;
+static __device__ __forceinline__ void start_rows(WaveAcc &w) {
+    wave_acc_reset(w);
+    w.m_run = kNoRows;
+}
 
 // A pass of one sequence's rest is multiplied with the rows of other sequences too,
 // whose weights are zero, but zero times an infinity or a NaN is NaN.  Where the
@@ -974,7 +978,7 @@ static __device__ __forceinline__ void item_work(const SharedAttnLaunch &a, cons
     int row_seq[kTiles];
     WaveAcc w[kTiles];
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) wave_acc_reset(w[t]);
+    for (int t = 0; t < kTiles; ++t) start_rows(w[t]);
     OneList feed{it.list, it.r0 + wave * kWaveTile, it.r1, kSharedWaves * kWaveTile};
     int wave_bad = 0;
     const float scale = run_passes<kTerms, kSrc, kNear, kTiles>(
@@ -1005,7 +1009,7 @@ static __device__ __forceinline__ void chunk_work(const SharedAttnLaunch &a, con
                                                   int tid, int wave) {
     const int lane = tid & 63, n16 = lane & 15, c4 = lane >> 4;
     WaveAcc w[1];
-    wave_acc_reset(w[0]);
+    start_rows(w[0]);
     u32x4 qf[1][4];
     int row_seq[1], wave_bad = 0;
     OneList feed{c.seq, c.r0, c.r1, kWaveTile};  // none: r0 == r1
@@ -1115,10 +1119,7 @@ static __device__ __forceinline__ void whole_work(const SharedAttnLaunch &a, con
     int row_seq[kTiles];
     WaveAcc w[kTiles];
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-        wave_acc_reset(w[t]);
-        w[t].m_run = kNoRows;
-    }
+    for (int t = 0; t < kTiles; ++t) start_rows(w[t]);
     const float scale = run_passes<kTerms, kSrc, kNear, kTiles>(
         a, layer, g, it.stream, feed, l.stages[wave], l.slots[wave], qf,
         [&] { load_item_queries<kTiles>(a, it, layer, g, n16, c4, qf, row_seq); }, row_seq, w, lane,

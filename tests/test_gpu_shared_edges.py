@@ -6,7 +6,7 @@ import torch
 from oracle import shared as OS
 from paper_2606_01483_amd import murmur as M
 from _shared import attn_bounds
-from test_gpu_shared_attn import CUT, bf16
+from test_gpu_shared_attn import CUT, Case, bf16
 from test_gpu_shared_pages import Device, grown_pool, i32
 
 pytestmark = pytest.mark.gpu
@@ -102,3 +102,22 @@ def test_shares_found_in_caches_of_their_own(refused, group, find, stride_b, ext
         far, far_lse = attn_bounds(*args, want, want_lse)
         assert (np.abs(out[0, b].cpu().numpy() - want) <= far).all(), b
         assert (np.abs(lse[0, b].cpu().numpy() - want_lse) <= far_lse).all(), b
+
+
+@pytest.mark.parametrize("extra_keep", [0, CUT])
+@pytest.mark.parametrize("hq,hkv", [(28, 4), (3, 3)])
+def test_logits_of_minus_infinity_weigh_nothing(hq, hkv, extra_keep):
+    """Keys that a caller has set to minus infinity, whole passes of them, at the start of what is shared, of a rest and
+    within both: the result is the attention over the other positions."""
+    announce(f"logits of minus infinity, {hq}/{hkv}, +{extra_keep}")
+    c = Case(42, [(400, [300, 0, 90, 5]), (0, [64, 200]), (33, [1])], NL=2, hq=hq, hkv=hkv, extra_keep=extra_keep)
+    c.q[..., 0] = c.q[..., 0].abs() + 1
+    out = set(c.lists[0][:130] + c.lists[0][200:300] + c.lists[0][400:490] + c.lists[2][400:440] + c.lists[5][:150])
+    c.k[:, sorted(out), :, 0] = float("-inf")
+    c.make_plan()
+    c.attend()
+    kept = [[x for x in xs if x not in out] for xs in c.lists]
+    assert min(len(x) for x in kept) > 4
+    c.lists = kept
+    c.check()
+    assert M.murmur_device_error() == 0
