@@ -562,24 +562,26 @@ class BeamBatch:
     current token of each chunk a block, which all of its sequences name.  What the hypotheses are is the caller's:
     step() takes their parents, queries and current-token K/V.
 
-    `live` [chunks * width, 1] follows the parents on the device: 0 from a parent of -1 on, until the row continues a
-    live one again.  A row that is not live holds no block, its queries and K/V are not looked at (zeros in the
-    murmur_seg of its step, `now`), and its outputs stay as they were."""
+    A parent of -1 ends a hypothesis, until its row continues a live one again.  Which ones live is in the table
+    itself: its last column, behind the blocks, names block 0 in every live row, so the fork moves it with the row.
+    An ended row holds no block, its murmur_seg in a step (`now`) is zeros, its queries and K/V are not looked at,
+    and its outputs stay as they were."""
 
     def __init__(self, wl: Workload, width: int, block_size: int, n_blocks: int, device: str = "cuda",
                  out_dtype: int = M.MURMUR_DTYPE_F32):
         if np.ndim(wl.policy) == 3:
             raise ValueError("paged steps take per-sequence policies")
-        self.wl, self.width, self.bs, self.n_blocks = wl, int(width), int(block_size), int(n_blocks)
+        self.wl, self.width, self.bs, self.n_blocks = wl, int(width), int(block_size), int(n_blocks) + 1
         self.rows, self.out_dtype = self.n_blocks * self.bs, out_dtype
         chunks, NL, Hq, Hkv, D = wl.batch, wl.n_layers, wl.hq, wl.hkv, wl.head_dim
         self.groups, self.B, self.NL, self.Hq, self.Hkv, self.D = chunks, chunks * self.width, NL, Hq, Hkv, D
-        self.max_blocks = int((-(-wl.seg(wl.steps - 1).sum(axis=1) // self.bs)).max())
+        self.max_blocks = int((-(-wl.seg(wl.steps - 1).sum(axis=1) // self.bs)).max()) + 1
         self.max_keep = int(max(int(retained_counts(wl, s).max()) for s in range(wl.steps)))
         dev = torch.device(device)
         table = np.full((self.B, self.max_blocks), -1, dtype=np.int32)
         ref = np.zeros(self.n_blocks, dtype=np.int32)
-        stack = list(range(self.n_blocks))
+        table[:, -1], ref[0] = 0, self.B  # live; block 0 stays where it is when the pool is compacted
+        stack = list(range(1, self.n_blocks))
         k = np.zeros((NL, self.rows, Hkv, D), dtype=np.uint16)
         v = np.zeros_like(k)
         seg0 = wl.seg(0)
@@ -606,8 +608,7 @@ class BeamBatch:
         self.stack, self.top = i32(stack + [0] * (self.n_blocks - len(stack))), i32([len(stack)])
         self.pol = i32(np.repeat(np.asarray(wl.policy), self.width, axis=0))
         self.seg = i32(np.stack([np.repeat(wl.seg(s), self.width, axis=0) for s in range(wl.steps)]))
-        self.live, self.now = i32(np.ones((self.B, 1))), i32(np.zeros((self.B, 4)))
-        self.row = i32(np.arange(self.B))
+        self.now = i32(np.zeros((self.B, 4)))
         self.group = i32(np.arange(chunks + 1) * self.width)
         self.shared, self.copied, self.map = i32(np.zeros(chunks)), i32(np.zeros(self.B)), i32(np.zeros(self.n_blocks))
         self.idx, self.count = i32(np.full((self.B, self.max_keep), -1)), i32(np.zeros(self.B))
@@ -621,16 +622,16 @@ class BeamBatch:
         self.ws = torch.zeros(self.ws_bytes // 4, dtype=torch.int32, device=dev)
 
     def state(self) -> tuple:
-        """Copies of everything a step changes (pool, table, counts, stack, top, live)."""
-        return tuple(t.clone() for t in (self.k, self.v, self.bt, self.ref, self.stack, self.top, self.live))
+        """Copies of everything a step changes (pool, table, counts, stack, top)."""
+        return tuple(t.clone() for t in (self.k, self.v, self.bt, self.ref, self.stack, self.top))
 
     def restore(self, st: tuple) -> None:
-        for t, s in zip((self.k, self.v, self.bt, self.ref, self.stack, self.top, self.live), st):
+        for t, s in zip((self.k, self.v, self.bt, self.ref, self.stack, self.top), st):
             t.copy_(s)
 
     @staticmethod
     def _on(stream):
-        """The context of torch's own operations on `stream` (as the calls take it)."""
+        """The context of torch's own operation on `stream` (as the calls take it)."""
         if stream is None:
             return contextlib.nullcontext()
         if isinstance(stream, int):
@@ -641,9 +642,6 @@ class BeamBatch:
         """Sequence b continues what sequence parent[b] was (int32 [B] on the device; -1 ends it)."""
         M.murmur_paged_fork(parent, self.B, self.bt, self.max_blocks, self.ref, self.n_blocks, self.stack, self.top,
                             self.n_blocks, self.pages_ws, self.pages_bytes, stream)
-        with self._on(stream):  # a parent outside [-1, B) leaves the row as it is
-            source = torch.where(parent == parent.clamp(-1, self.B - 1), parent, self.row)
-            self.live.copy_(torch.where(source < 0, 0, self.live[source.clamp(min=0).long(), 0])[:, None])
 
     def compact(self, stream=None) -> None:
         """Moves the blocks in use to the front of the pool."""
@@ -654,8 +652,8 @@ class BeamBatch:
         """Step i: fork, then the current token (k_new, v_new [NL, B, Hkv, D]) and its attention (q [NL, B, Hq, D])."""
         if parent is not None:
             self.fork(parent, stream)
-        with self._on(stream):
-            torch.mul(self.seg[i], self.live, out=self.now)
+        with self._on(stream):  # seg + seg * (0 or -1)
+            torch.addcmul(self.seg[i], self.seg[i], self.bt[:, -1:], out=self.now)
         M.murmur_paged_step_shared(self.now, self.pol, 1, self.B, self.bt, self.max_blocks, self.bs, self.ref,
                                    self.n_blocks, self.stack, self.top, self.n_blocks, i == 0, self.copied, self.kv,
                                    self.Hkv, k_new, v_new, stream)
