@@ -260,8 +260,10 @@ __global__ __launch_bounds__(kForkThreads) void fork_push_kernel(int64_t places,
 // ahead, so what it writes lies behind every row that the others copy.
 // Round trips to memory bound it, so a sequence's layout, policy and current block
 // stay in registers where a thread has only one, and the counts in its XCD's L2: 4.6
-// us for 4 sequences, 11.0 for 96 that all copy (17.0 with the counts past the L2;
-// 3.5 of the 11 rank the writers).
+// us for 4 sequences, 11.2 for 96 of which 35 copy (17.0 with the counts past the L2;
+// 3.5 of the 11 rank the writers).  The ranking compares every row that may have to
+// copy with every row of the batch, one workgroup for all: with seven of eight
+// copying, timed around the call, 13 us for 96 sequences, 88 for 1024, 1222 for 4096.
 // ---------------------------------------------------------------------------
 // The counts are this workgroup's alone while it runs: atomics in its XCD's L2, where
 // those that other XCDs see go past it.
@@ -439,8 +441,9 @@ __global__ __launch_bounds__(kThreads) void step_shared_kernel(const murmur_seg 
 // A workgroup per sequence and some of its (layer, K or V) planes: the rows of the
 // current block before the token from the block it was copied from, then the
 // token's own rows.  A thread has a 16-byte chunk of a row in each plane, and its
-// loads of kAppendPlanes planes are on their way at once (96 sequences, 28 layers, 9
-// rows each on average: 31.8 MB moved in 9.2 us, 10.0 with a plane at a time).
+// loads of kAppendPlanes planes are on their way at once (96 sequences, 28 layers, 181
+// rows copied for 35 of them: 31.8 MB read and written in 9.4 us, 10.0 with a plane at
+// a time).
 constexpr int kAppendPlanes = 4;
 __global__ __launch_bounds__(256) void append_shared_kernel(const murmur_seg *__restrict__ seg, int32_t B,
                                                             const int32_t *__restrict__ bt, int32_t max_blocks,

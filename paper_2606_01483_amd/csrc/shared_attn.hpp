@@ -107,8 +107,8 @@ struct Dealt {
 };
 
 // SharedPlanLaunch::find where the planner compares the lists itself: few entries, a
-// load or two of a thread, are cheaper than another launch (4 lists of 266: 17 us for
-// plan and attention, 19 with it).
+// load or two of a thread, are cheaper than another launch (4 lists of 192: 15.0 us for
+// plan and attention, 17.6 with it).
 constexpr int kFindHere = 2;
 constexpr int kFindHereEntries = 4096;
 
@@ -116,7 +116,8 @@ constexpr int kFindHereEntries = 4096;
 // global round trips are the counts with the groups, the scans, and the stores.  It
 // runs each line once, on code that no cache holds yet, so what bounds it is the
 // size of the code (loops are not unrolled, divisions are by reciprocal, sums over
-// lanes go by DPP): 5.3 us for 4 sequences, 7.9 for 96, 9.1 when it had 17 KB.
+// lanes go by DPP): 5.6 us for 4 sequences, 7.0 for 96 in whole lists, 8.3 to 11.5 with
+// cuts.
 // The lowest level of cut whose workgroups fit one dispatch round is taken, or the
 // highest; the wavefronts add up eight levels side by side, then the eight between
 // two of them.
@@ -347,6 +348,10 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     if (err) raise_device_error(err);
     __syncthreads();
 
+    // Rows that are read once or twice go past the caches where a layer reads kStreamBytes or more, so that they do not
+    // push out what several workgroups read (us with and without: an hour of five hypotheses 706 and 744, 16 x 6 drafted
+    // tokens 485 and 524; small lists of their own behind a long shared prefix lose, 64 chunks 121 and 115, 23 ragged
+    // groups 64 and 61; all rows past the caches: 706, 485, 122, 65).
     int stream;
     {  // positions that a layer reads
         int n = 0;
@@ -884,12 +889,16 @@ static __device__ __forceinline__ void load_item_queries(const SharedAttnLaunch 
 // Workgroup (layer and KV head, i) does item i of the plan: a stretch of a prefix,
 // whose passes its wavefronts take in turn, each for all of the item's query rows;
 // or remainders, each wavefront a chunk of some sequence's.  Eight wavefronts and
-// 138 KiB of LDS, a compute unit for a workgroup: with four, two on one, there are
+// 134 KiB of LDS, a compute unit for a workgroup: with four, two on one, there are
 // twice the partials to write and to join (35 096 positions, 5 hypotheses, 4 KV
-// heads: 21.8 + 4.0 us a layer, 22.5 + 5.1 with four; 20.8 + 4.0 since the levels go
+// heads: 21.8 + 4.0 us a layer, 22.5 + 5.1 with four; 21.1 + 4.0 since the levels go
 // by quarters of a pass).  Two thirds of it is the read: 73 MB at 5.5 TB/s.
+// Two wavefronts on a SIMD leave 256 vector registers each, which three row tiles fill:
+// none is spilled with index lists within 32-bit offsets, 17 with range tables and fp32
+// outputs (none with bf16 ones), 14 and 57 where rows go by 64-bit addresses.
 // ---------------------------------------------------------------------------
 constexpr int kSharedThreads = kSharedWaves * 64;
+constexpr size_t kComputeUnitLds = 160 * 1024;
 template <int kWaves>
 struct SharedLds {
     uint8_t stages[kWaves][kStageBytes];
@@ -1049,6 +1058,9 @@ static __device__ __forceinline__ bool plan_fits(const SharedAttnLaunch &a, cons
            (h.kind & a.kinds);
 }
 
+static_assert(sizeof(SharedLds<8>) <= kComputeUnitLds && 2 * sizeof(SharedLds<4>) <= kComputeUnitLds,
+              "eight wavefronts on a compute unit");
+
 template <int kTerms, int kSrc, bool kNear>
 __global__ __launch_bounds__(kSharedThreads, 2) void shared_attn_kernel(const SharedAttnLaunch a) {
     __shared__ __attribute__((aligned(16))) SharedLds<kSharedWaves> l;
@@ -1083,7 +1095,11 @@ __global__ __launch_bounds__(kSharedThreads, 2) void shared_attn_kernel(const Sh
 // prologues and epilogues overlap.  12 groups of 8, lists of 850, 4 KV heads: 16.4 us a
 // layer, of which 5 are the first round trips (plan, entries, rows) and 4 the passes,
 // at 91 bytes a nanosecond and compute unit; 28 layers of 16 groups of 6 drafted tokens
-// in one launch: 2.67 GB in 483 us (5.5 TB/s).
+// in one launch: 2.67 GB in 482 us (5.5 TB/s).
+// Every instance fills the 256 vector registers of its wavefronts.  With index lists
+// within 32-bit offsets 1 (bf16 outputs) or 5 (fp32) are spilled, with range tables 16
+// or 26 (the table is live through the passes), with 64-bit row addresses 20, or 48 to 53
+// with range tables too.
 // ---------------------------------------------------------------------------
 template <int kTerms, int kSrc, bool kNear, int kTiles, int kWaves>
 static __device__ __forceinline__ void whole_work(const SharedAttnLaunch &a, const PlanItem &it, SharedLds<kWaves> &l,
