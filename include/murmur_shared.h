@@ -156,10 +156,10 @@ int murmur_decode_attn_shared_workspace(int32_t n_layers, int32_t B, int32_t Hq,
  *   n_layers, Hq, Hkv: of each murmur_decode_attn_shared call that uses the plan;
  *   plan_dev, plan_bytes: see murmur_decode_attn_shared_workspace.
  * Errors: MURMUR_EINVAL, MURMUR_EUNSUPPORTED, MURMUR_ENOSPACE, MURMUR_EHIP.  Device
- * errors: MURMUR_DEVERR_COUNT for a sequence whose count is outside [1, max_keep] and
- * not -1 or below what its group shares, and for all of a group that shares more than
- * the count of its first sequence that is there (NaN outputs); MURMUR_DEVERR_GROUP for groups out of order (every output is
- * NaN). */
+ * errors: MURMUR_DEVERR_COUNT for a sequence whose count is neither -1 nor in
+ * [1, max_keep], or is below what its group shares, and for all of a group that shares
+ * more than the count of its first sequence that is there (NaN outputs);
+ * MURMUR_DEVERR_GROUP for groups out of order (every output is NaN). */
 int murmur_shared_plan(const int32_t *idx_dev, const int32_t *ranges_dev, const int32_t *count_dev, int32_t max_keep,
                        int32_t B, const int32_t *group_dev, int32_t n_groups, int32_t *shared_dev,
                        int32_t find_shared, int32_t n_layers, int32_t Hq, int32_t Hkv, void *plan_dev,
