@@ -149,8 +149,9 @@ int murmur_decode_attn_shared_workspace(int32_t n_layers, int32_t B, int32_t Hq,
  *               as they were;
  *   shared_dev: device int32 [n_groups]: how many leading list entries the group's
  *               sequences share.  find_shared 1: output, the most that the index
- *               lists allow (ranges_dev NULL; for a group of one its whole list;
- *               0 if none of the group is there);
+ *               lists allow (ranges_dev NULL; for a group of one its whole list; 0
+ *               if none of the group has a valid count, or its first sequence that
+ *               is there one below 1; other invalid lists are passed over);
  *               0: input, a promise of the caller, who may share less than that
  *               (the way for sequence-ordered caches, whose lists do not tell);
  *   n_layers, Hq, Hkv: of each murmur_decode_attn_shared call that uses the plan;

@@ -250,7 +250,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
 #pragma unroll 1
     for (int g = tid; g <= n_groups; g += kPlanThreads) l.lo[g] = p.group[g];
 #pragma unroll 1
-    for (int g = tid; g < n_groups; g += kPlanThreads) l.common[g] = p.find ? max_keep : p.shared[g];
+    for (int g = tid; g < n_groups; g += kPlanThreads) l.common[g] = p.find ? max_keep + 1 : p.shared[g];
     __syncthreads();
 #pragma unroll 1
     for (int g = tid; g < n_groups; g += kPlanThreads) {
@@ -329,7 +329,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
         const int lead = l.lead[g];
         const bool some = lead < l.lo[g + 1];
         int common = some ? l.common[g] : 0;
-        if (p.find) p.shared[g] = common;
+        if (p.find) p.shared[g] = common = common <= max_keep ? common : 0;  // above: none has a valid count
         else if (common != 0 && some && !(common > 0 && common <= l.rest[lead] && l.rest[lead] <= max_keep)) common = -1;
         l.common[g] = common;
     }

@@ -121,3 +121,21 @@ def test_logits_of_minus_infinity_weigh_nothing(hq, hkv, extra_keep):
     c.lists = kept
     c.check()
     assert M.murmur_device_error() == 0
+
+
+@pytest.mark.parametrize("extra_keep", [0, CUT])
+@pytest.mark.parametrize("common", [40, 1500])
+def test_groups_of_nothing_but_counts_too_large(common, extra_keep):
+    """Counts above max_keep are errors of the count alone: a group without a valid list shares nothing and reads
+    nothing, and one whose first list is too long shares what the others' lists have in common with it."""
+    announce(f"counts too large, common {common}, +{extra_keep}")
+    c = Case(43, [(common, [10]), (common, [3, 5, 9]), (20, [4, 0]), (7, [1, 2])], hq=8, hkv=2, extra_keep=extra_keep)
+    for b in (0, 1, 4, 5):
+        c.count[b] = c.keep + 1
+    c.make_plan()
+    c.attend()
+    torch.cuda.synchronize()
+    assert M.murmur_device_error() == M.MURMUR_DEVERR_COUNT
+    assert c.shared.cpu().tolist() == [0, common, 0, 7]
+    assert torch.isnan(c.out[:, [0, 1, 4, 5]]).all() and torch.isnan(c.lse[:, [0, 1, 4, 5]]).all()
+    c.check([2, 3, 6, 7])
