@@ -1,0 +1,625 @@
+"""The operators of speculative decoding whose speed counts: placing requests in a paged pool, rotary positions on the
+way into the cache, attention of a tree of drafted tokens, and the accepted path's way into the cache.
+
+    reserve  murmur_paged_reserve: blocks and slot maps for new tokens, from the requests' lengths
+    rope     murmur_rope_append: q and k rotated, K and V written to the rows of a slot map
+    tree     murmur_decode_attn_tree: every node of a tree over the retained cache and its ancestors
+    accept   murmur_tree_accept: the longest path that the decoder agrees with, its K and V into the cache
+
+Sequences have Murmur's layout (prompt, speech, second prompt, outputs) and one eviction policy.  Sizes, lengths, trees
+and tables' shapes come from the case alone; keys, values, queries, tokens and the order of the pool's blocks from the
+seed.  Cache rows that no node retains are bf16 NaN, so a stray read shows in the outputs.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+D = 128
+OFF = -1
+
+RESERVE = dict(op="reserve", batch=1, len_lo=0, len_hi=0, new_lo=1, new_hi=1, block=16, padded=False, counted=True, short=False)
+ROPE = dict(op="rope", batch=1, per=1, layers=1, hq=28, hkv=4, rot=128, interleaved=False, f32=False, kind="plain",
+            base=1e6, factor=1.0, far=4096, ragged=False)
+TREE = dict(op="tree", batch=1, nodes=8, few=8, wide=3, layers=1, per_call=1, prompt=32, prompt_mid=0, speech_lo=450,
+            speech_hi=450, out_lo=72, out_hi=72, w_s=OFF, delay=0, sink_s=0, w_o=OFF, sink_o=0, block=16, hq=28, hkv=4,
+            out_f32=False, ended=0)
+ACCEPT = dict(op="accept", batch=1, nodes=8, few=8, wide=3, layers=1, hkv=4, agree=0.7, block=16, ended=0)
+
+
+def listed():
+    evict = dict(w_s=562, delay=512, w_o=256)
+    return [
+        # One more token of one sequence: the smallest call of the bookkeeping, latency alone.
+        dict(RESERVE, name="reserve_one", len_lo=553, len_hi=553),
+        # Twelve five-minute chunks come in: prompt and speech of each, 27396 tokens in one packed prefill.
+        dict(RESERVE, name="reserve_prompts12", batch=12, new_lo=2283, new_hi=2283),
+        # Room for the drafts of 1024 sequences at every stage of their decode, in tables of up to 8000 tokens.
+        dict(RESERVE, name="reserve_draft1024", batch=1024, len_lo=1, len_hi=8000, new_lo=0, new_hi=17, padded=True),
+        # The current token of twelve sequences in one layer of a decoder.
+        dict(ROPE, name="rope_token12", batch=12),
+        # The prompts of twelve chunks in one layer: a prefill's rotation and append.
+        dict(ROPE, name="rope_prompts12", batch=12, per=2283, far=2283),
+        # 33 drafted tokens of sixteen sequences in all layers, half of each head rotated, pairs interleaved, positions
+        # in the millions, projections in fp32, some sequences with fewer tokens.
+        dict(ROPE, name="rope_far", batch=16, per=33, layers=28, rot=64, interleaved=True, f32=True, kind="yarn",
+             base=5e5, factor=16.0, far=1 << 22, ragged=True),
+        # Eight nodes for one minute of audio, one layer, fp32 out: the smallest tree.
+        dict(TREE, name="tree_minute", w_s=128, delay=72, w_o=32, out_f32=True),
+        # The headline batch with sixteen nodes a chunk, one call per layer of the decoder.
+        dict(TREE, name="tree_12x16", batch=12, nodes=16, few=16, layers=28, speech_lo=2250, speech_hi=2250, out_lo=600,
+             out_hi=1200, **evict),
+        # An hour in one pass without eviction, 31 nodes, four layers: one long cache, few rows.
+        dict(TREE, name="tree_hour31", nodes=31, few=31, layers=4, speech_lo=27000, speech_hi=27000, out_lo=8064,
+             out_hi=8064),
+        # 64 chunks of 64 nodes at every stage in caches of their own, all layers of the call at once: matrix work.
+        dict(TREE, name="tree_64x64", batch=64, nodes=64, few=20, wide=8, layers=4, per_call=4, block=0, speech_lo=300,
+             speech_hi=2250, out_lo=1, out_hi=1200, delay=512, w_s=1125, ended=3),
+        # A chain of eight for one sequence, one layer.
+        dict(ACCEPT, name="accept_one", wide=1),
+        # The accepted paths of 64 sequences in all layers of a decoder.
+        dict(ACCEPT, name="accept_64x64", batch=64, nodes=64, few=20, wide=4, layers=28, agree=0.9, ended=3),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _cost(c):
+    """(bytes, flops) as the plain form sees them: whole caches in 32 bits."""
+    if c["op"] != "tree":
+        w = work(c)
+        return w["bytes"], w["flops"]
+    lay = _layout(c)
+    length = int(lay["seg"].sum(axis=1).max()) + c["nodes"]
+    rows = c["layers"] * c["batch"] * length * c["hkv"]
+    return rows * (D * 4 + c["nodes"] * c["hq"] // c["hkv"] * 4), work(c)["flops"]
+
+
+def draw(rng):
+    """One more case: any operator, 1 to 64 sequences (1 to 1024 for the bookkeeping), 1 to 64 nodes, a minute to an
+    hour, 1 to 28 layers, blocks of 1 to 64 rows or caches of the sequences' own, any policy, any rotation."""
+    most = {}
+    for c in listed():
+        most[c["op"]] = [max(a, b) for a, b in zip(most.get(c["op"], (0, 0)), _cost(c))]
+    while True:
+        op = rng.choice(["reserve", "reserve", "rope", "rope", "tree", "tree", "tree", "tree", "accept"])
+        hq, hkv = rng.choice([(28, 4), (28, 4), (28, 4), (16, 4), (16, 1), (8, 2), (4, 4)])
+        layers = _log_int(rng, 1, 28)
+        nodes = _log_int(rng, 1, 64)
+        few, wide = rng.choice([nodes, rng.randint(1, nodes)]), rng.choice([1, 2, 4, 8])
+        batch = _log_int(rng, 1, 64)
+        block = rng.choice([1, 4, 8, 16, 16, 16, 32, 64])
+        if op == "reserve":
+            new_hi = _log_int(rng, 1, 3000)
+            len_hi = rng.choice([0, _log_int(rng, 1, 30000)])
+            c = dict(RESERVE, batch=_log_int(rng, 1, 1024), len_lo=rng.choice([len_hi, 0]), len_hi=len_hi, new_hi=new_hi,
+                     new_lo=rng.choice([new_hi, 0, rng.randint(0, new_hi)]), block=block, padded=rng.random() < 0.4,
+                     counted=rng.random() < 0.7, short=rng.random() < 0.2)
+        elif op == "rope":
+            c = dict(ROPE, batch=batch, per=_log_int(rng, 1, 3000), layers=layers, hq=hq, hkv=hkv,
+                     rot=rng.choice([128, 128, 64, 96, 32, 2, 50]), interleaved=rng.random() < 0.4, f32=rng.random() < 0.3,
+                     kind=rng.choice(["plain", "linear", "base", "bands", "yarn"]), base=rng.choice([1e4, 5e5, 1e6]),
+                     factor=rng.choice([2.0, 4.0, 16.0]), far=_log_int(rng, 3000, 1 << 24), ragged=rng.random() < 0.4)
+        elif op == "tree":
+            speech_hi, out_hi = _log_int(rng, 100, 27000), _log_int(rng, 2, 8000)
+            c = dict(TREE, batch=batch, nodes=nodes, few=few, wide=wide, layers=layers, per_call=rng.choice([1, layers]),
+                     prompt=rng.choice([rng.randint(0, 64), _log_int(rng, 1, 5000)]), prompt_mid=rng.choice([0, 0, rng.randint(1, 40)]),
+                     speech_hi=speech_hi, speech_lo=rng.choice([speech_hi, rng.randint(speech_hi // 3, speech_hi)]),
+                     out_hi=out_hi, out_lo=rng.choice([out_hi, rng.randint(1, out_hi)]), block=rng.choice([0, block]), hq=hq,
+                     hkv=hkv, out_f32=rng.random() < 0.4, ended=rng.choice([0, 0, 1 if batch > 1 else 0]))
+            if rng.random() < 0.6:  # speech eviction
+                c.update(w_s=_log_int(rng, 32, max(33, speech_hi)), delay=rng.choice([0, 256, 512]),
+                         sink_s=rng.choice([0, 0, rng.randint(1, 64)]))
+            if rng.random() < 0.6:  # output eviction
+                c.update(w_o=_log_int(rng, 4, max(17, out_hi)), sink_o=rng.choice([0, 4, 8]))
+        else:
+            c = dict(ACCEPT, batch=batch, nodes=nodes, few=few, wide=wide, layers=layers, hkv=hkv, agree=rng.uniform(0.3, 1.0),
+                     block=block, ended=rng.choice([0, 0, 1 if batch > 1 else 0]))
+        if op == "reserve" and c["batch"] * c["new_hi"] > 60000:
+            continue
+        if op == "rope" and c["batch"] * c["per"] * c["layers"] > 30000:
+            continue
+        if all(a <= b for a, b in zip(_cost(c), most[op])):
+            return c
+
+
+# ---- lengths, trees and tables (plain numpy, from the case alone) ---------------------------------------------------
+
+def _rng(c, *extra):
+    return np.random.default_rng([c["batch"], c.get("nodes", 0), c.get("speech_hi", 0), c.get("new_hi", 0), *extra])
+
+
+def _trees(c):
+    """Parents [batch, nodes]: -1 for the root, -2 for a node that is not there (a tree of fewer nodes); and depths."""
+    rng = _rng(c, 3)
+    n, T = c["batch"], c["nodes"]
+    size = rng.integers(c["few"], T, size=n, endpoint=True)
+    i = np.arange(T)
+    back = rng.integers(1, c["wide"], size=(n, T), endpoint=True)
+    parent = np.maximum(i - back, 0)
+    parent[:, 0] = -1
+    depth = np.zeros((n, T), dtype=np.int64)
+    for t in range(1, T):
+        depth[:, t] = depth[np.arange(n), parent[:, t]] + 1
+    parent[i >= size[:, None]] = -2
+    if c["ended"]:
+        parent[-c["ended"]:] = -2
+    return parent.astype(np.int32), depth, size
+
+
+def _layout(c):
+    rng = _rng(c, 5, c["out_hi"], c["block"])
+    n, T = c["batch"], c["nodes"]
+    parent, depth, _ = _trees(c)
+    speech = rng.integers(c["speech_lo"], c["speech_hi"], size=n, endpoint=True)
+    out = rng.integers(c["out_lo"], c["out_hi"], size=n, endpoint=True)
+    seg = np.stack([np.full(n, c["prompt"]), speech, np.full(n, c["prompt_mid"]), out], axis=1).astype(np.int32)
+    if c["ended"]:
+        seg[-c["ended"]:] = 0
+    deepest = np.where(parent >= -1, depth, 0).max(axis=1)
+    kept = []  # cached positions that any node retains, per sequence
+    for b in range(n):
+        p0, ls, p1, j = (int(x) for x in seg[b])
+        t, o = np.arange(ls), np.arange(max(j - 1, 0))
+        s_ok, o_ok = np.ones(ls, bool), np.ones(len(o), bool)
+        if c["w_s"] != OFF:
+            first, last = (min(max(j + e - max(c["delay"], 1) + 1, 0), max(ls - c["w_s"], 0)) for e in (0, int(deepest[b])))
+            s_ok = (t < c["sink_s"]) | ((t >= first) & (t < last + c["w_s"]))
+        if c["w_o"] != OFF:
+            o_ok = (o < c["sink_o"]) | (o >= j - c["w_o"])
+        kept.append(np.flatnonzero(np.concatenate([np.ones(p0, bool), s_ok, np.ones(p1, bool), o_ok])))
+    return {"seg": seg, "parent": parent, "depth": depth, "kept": kept}
+
+
+def _requests(c):
+    """Lengths and new tokens of every request, the table before the call and the blocks that are free."""
+    rng = _rng(c, 7, c["len_hi"], c["block"])
+    n, bs = c["batch"], c["block"]
+    length = rng.integers(c["len_lo"], c["len_hi"], size=n, endpoint=True)
+    new = rng.integers(c["new_lo"], c["new_hi"], size=n, endpoint=True)
+    held = -(-length // bs)
+    held = held + (rng.random(n) < 0.3) * rng.integers(0, 2, size=n, endpoint=True)  # left by an earlier draft
+    cols = max(int((-(-(length + new) // bs)).max()), int(held.max()), 1)
+    need = np.maximum(-(-(length + new) // bs) - np.maximum(held, length // bs), 0) * (new > 0)
+    used = int(held.sum())
+    free = int(need.sum()) * 2 // 3 if c["short"] else int(need.sum()) + 64
+    return dict(length=length, new=new, held=held, cols=cols, need=need, used=used, free=free, n_blocks=used + free + 8)
+
+
+def work(c):
+    if c["op"] == "reserve":
+        r = _requests(c)
+        named = int(((-(-(r["length"] + r["new"]) // c["block"]) - r["length"] // c["block"]) * (r["new"] > 0)).sum())
+        taken = min(int(r["need"].sum()), r["free"])
+        return {"bytes": 16 * c["batch"] + 4 * named + taken * (8 + 4 * c["counted"]) + 12 * int(r["new"].sum()), "flops": 0}
+    if c["op"] == "rope":
+        n = int(_tokens(c).sum()) * c["layers"]
+        values = (c["hq"] + 2 * c["hkv"]) * D
+        pairs = n * (c["hq"] + c["hkv"]) * c["rot"] // 2
+        return {"bytes": n * values * (6 if c["f32"] else 4) + 8 * int(_tokens(c).sum()), "flops": 6 * pairs}
+    if c["op"] == "accept":
+        n = int(_accepted(c).sum())
+        return {"bytes": n * c["layers"] * c["hkv"] * D * 8 + c["batch"] * (c["nodes"] * 20 + 8), "flops": 0}
+    lay = _layout(c)
+    live = (lay["parent"] >= -1).sum(axis=1)
+    counts = np.array([len(p) for p in lay["kept"]])
+    row = c["layers"] * c["hkv"] * 2 * D * 2
+    io = c["layers"] * int(live.sum()) * c["hq"] * ((4 if c["out_f32"] else 2) * D + 2 * D + 4)
+    return {"bytes": int((counts + live).sum()) * row + io, "flops": int((live * (counts + (live + 1) // 2)).sum()) * c["layers"] * c["hq"] * D * 4}
+
+
+def _tokens(c):
+    """Tokens of every sequence of a rotation."""
+    n = np.full(c["batch"], c["per"])
+    return n if not c["ragged"] else _rng(c, 9, c["per"]).integers(0, c["per"], size=c["batch"], endpoint=True)
+
+
+def _agreeing(c):
+    """Where the decoder agrees with one child of a node, and which (by a number), from the case alone."""
+    rng = _rng(c, 11)
+    return rng.random((c["batch"], c["nodes"])) < c["agree"], rng.random((c["batch"], c["nodes"]))
+
+
+def _accepted(c):
+    """Nodes of the accepted path of every sequence (the cost of a case; run() finds them from the tokens)."""
+    parent, _, _ = _trees(c)
+    agree, which = _agreeing(c)
+    n = np.zeros(c["batch"], dtype=np.int64)
+    for b in range(c["batch"]):
+        at = 0 if parent[b, 0] == -1 else -1
+        while at >= 0:
+            n[b] += 1
+            kids = np.flatnonzero(parent[b] == at)
+            at = int(kids[int(which[b, at] * len(kids))]) if len(kids) and agree[b, at] else -1
+    return n
+
+
+# ---- inputs ---------------------------------------------------------------------------------------------------------
+
+def _gen(seed, *extra):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(int(np.random.SeedSequence([seed, *extra]).generate_state(1, np.uint64)[0] >> 1))
+    return g
+
+
+def _i32(x):
+    return torch.from_numpy(np.ascontiguousarray(x, dtype=np.int32)).cuda()
+
+
+def _randn(seed, which, *shape, dtype=torch.bfloat16):
+    return torch.randn(shape, generator=_gen(seed, which), device="cuda", dtype=dtype)
+
+
+def _frequencies(c):
+    """Turns per position of every pair, and the gain (64 bits, numpy): the definition that both sides start from."""
+    i, rot, s = np.arange(c["rot"] // 2), c["rot"], c["factor"]
+    base = c["base"]
+    if c["kind"] == "base" and rot > 2:
+        base = base * s ** (rot / (rot - 2.0))
+    f = base ** (-2.0 * i / rot) / (2.0 * math.pi)
+    gain = 1.0
+    if c["kind"] == "linear":
+        f = f / s
+    if c["kind"] in ("bands", "yarn"):  # turns within the original context of 4096: 1 and less are scaled, 32 and more not
+        keep = np.clip((4096.0 * f - 1.0) / 31.0, 0.0, 1.0)
+        f = f * keep + f / s * (1.0 - keep)
+        gain = 1.0 + 0.1 * math.log(s) if c["kind"] == "yarn" else 1.0
+    return f, gain
+
+
+def prepare(c, seed):
+    host = np.random.default_rng([seed, 13])
+    s = {"case": c}
+    if own:
+        from paper_2606_01483_amd import murmur as M
+    if c["op"] == "reserve":
+        r = _requests(c)
+        order = host.permutation(r["n_blocks"])
+        col = np.arange(r["cols"])
+        first = np.concatenate([[0], np.cumsum(r["held"])])[:-1]
+        table = np.where(col < r["held"][:, None], order[np.minimum(first[:, None] + col, len(order) - 1)], -1).astype(np.int32)
+        stack = np.concatenate([order[r["used"]:r["used"] + r["free"]], np.zeros(r["n_blocks"] - r["free"], dtype=np.int64)])
+        ref = np.bincount(table[table >= 0], minlength=r["n_blocks"])
+        # table, counts and the stack's top in one buffer, so that a pass starts from all of them at once
+        s.update(book0=_i32(np.concatenate([table.ravel(), ref, [r["free"]]])), shape=table.shape, n_blocks=r["n_blocks"],
+                 stack=_i32(stack), length=_i32(r["length"]), new=_i32(r["new"]))
+        s["per"] = max(int(r["new"].max()), 1) if c["padded"] else 0
+        s["n_tokens"] = s["per"] * c["batch"] if c["padded"] else int(r["new"].sum()) + 3
+        if own:
+            s["book"] = s["book0"].clone()
+            s["ws_bytes"] = M.murmur_paged_reserve_workspace(c["batch"])
+            s["ws"] = torch.zeros(s["ws_bytes"] // 4, dtype=torch.int32, device="cuda")
+            s["start"], s["got"] = _i32(np.zeros(c["batch"] + 1)), _i32(np.zeros(c["batch"]))
+            s["maps"] = _i32(np.zeros((3, s["n_tokens"])))
+        return s
+    if c["op"] == "rope":
+        n, per, nl = _tokens(c), c["per"], c["layers"]
+        total, values = c["batch"] * per, (c["hq"] + 2 * c["hkv"]) * D
+        at = np.arange(per)
+        begin = host.integers(0, max(c["far"] - per, 1), size=c["batch"], endpoint=True)
+        there = at < n[:, None]
+        rows = total + 64
+        slot = host.permutation(rows)[:total].reshape(c["batch"], per)
+        s.update(pos=_i32(np.where(there, begin[:, None] + at, -1).ravel()), slot=_i32(np.where(there, slot, -1).ravel()),
+                 rows=rows, n=total)
+        s["qkv"] = _randn(seed, 1, nl, total, values, dtype=torch.float32 if c["f32"] else torch.bfloat16)
+        s["q_out"] = torch.zeros((nl, total, c["hq"], D), dtype=torch.bfloat16, device="cuda")
+        s["k"], s["v"] = (torch.zeros((nl, rows + 1, c["hkv"], D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        f, s["gain"] = _frequencies(c)
+        s["freq"] = torch.from_numpy(f).cuda()
+        if own:
+            turns, gain = M.murmur_rope_freqs_host(c["rot"], c["base"], c["kind"], c["factor"], 4096.0)
+            s["turns"] = torch.from_numpy(turns.view(np.int64)).cuda()
+            s["rope"] = M.make_rope(c["rot"], c["interleaved"], s["turns"], gain)
+            step = 4 if c["f32"] else 2
+            q = s["qkv"].data_ptr()
+            s["in"] = M.make_qkv(q, q + c["hq"] * D * step, q + (c["hq"] + c["hkv"]) * D * step,
+                                 M.MURMUR_DTYPE_F32 if c["f32"] else M.MURMUR_DTYPE_BF16, total * values, values, total * values, values)
+            s["kv"] = M.make_kv(s["k"], s["v"], nl, rows, ((rows + 1) * c["hkv"] * D, 0, D, c["hkv"] * D))
+        return s
+    B, T, nl, hkv = c["batch"], c["nodes"], c["layers"], c["hkv"]
+    parent, _, _ = _trees(c)
+    s["parent"] = _i32(parent)
+    s["k_tree"], s["v_tree"] = (_randn(seed, w, nl, B, T, hkv, D) for w in (2, 3))
+    if c["op"] == "accept":
+        agree, which = _agreeing(c)
+        token = host.integers(0, 150000, size=(B, T))
+        said = np.full((B, T), 150001)
+        for b in range(B):
+            for t in range(T):
+                kids = np.flatnonzero(parent[b] == t)
+                if len(kids) and agree[b, t]:
+                    said[b, t] = token[b, kids[int(which[b, t] * len(kids))]]
+        token[parent[:, 0] != -1, 0] = -1  # not there
+        blocks = -(-T // c["block"]) + 1
+        rows = B * blocks * c["block"]
+        place = host.permutation(B * blocks).reshape(B, blocks)
+        p = host.integers(0, c["block"] - 1, size=(B, 1), endpoint=True) + np.arange(T)
+        s.update(token=_i32(token), said=_i32(said), slot=_i32(place[np.arange(B)[:, None], p // c["block"]] * c["block"] + p % c["block"]), rows=rows)
+        s["k"], s["v"] = (torch.zeros((nl, rows + 1, hkv, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        if own:
+            s["kv"] = M.make_kv(s["k"], s["v"], nl, rows, ((rows + 1) * hkv * D, 0, D, hkv * D))
+            s["path"], s["count"], s["last"] = _i32(np.zeros((B, T))), _i32(np.zeros(B)), _i32(np.zeros(B))
+        return s
+    lay = _layout(c)
+    seg = lay["seg"].astype(np.int64)
+    total = np.maximum(seg.sum(axis=1) - 1, 0)
+    s.update(seg=_i32(seg), pol=_i32([[c["w_s"], c["delay"], c["sink_s"], c["w_o"], c["sink_o"]]]), scale=D ** -0.5,
+             keep=max(len(p) for p in lay["kept"]) + T, q=_randn(seed, 4, nl, B, T, c["hq"], D))
+    which = np.concatenate([np.full(len(p), b) for b, p in enumerate(lay["kept"])]).astype(np.int64)
+    pos = np.concatenate(lay["kept"]).astype(np.int64)
+    if c["block"]:
+        bs = c["block"]
+        cols = max(int((-(-total // bs)).max()), 1)
+        held = np.zeros((B, cols), dtype=bool)
+        held[which, pos // bs] = True
+        n_blocks = int(held.sum()) + 8
+        table = np.full((B, cols), -1, dtype=np.int64)
+        table[held] = host.permutation(n_blocks)[:int(held.sum())]
+        shape, live = (nl, n_blocks * bs, hkv, D), table[which, pos // bs] * bs + pos % bs
+        s.update(table=_i32(table), rows=n_blocks * bs, length=max(int(total.max()), 1))
+    else:
+        length = int(-(-max(int(total.max()), 1) // 8) * 8)
+        shape, live = (nl, B * length, hkv, D), which * length + pos
+        s.update(table=None, rows=length, length=length)
+    dead = torch.ones(shape[1], dtype=torch.bool, device="cuda")
+    dead[torch.from_numpy(live).cuda()] = False
+    s["k"], s["v"] = (_randn(seed, w, *shape) for w in (5, 6))
+    s["k"].masked_fill_(dead.view(1, -1, 1, 1), float("nan"))
+    s["v"].masked_fill_(dead.view(1, -1, 1, 1), float("nan"))
+    s["out"] = torch.zeros((nl, B, T, c["hq"], D), dtype=torch.float32 if c["out_f32"] else torch.bfloat16, device="cuda")
+    s["lse"] = torch.zeros((nl, B, T, c["hq"]), dtype=torch.float32, device="cuda")
+    if own:
+        per = c["per_call"]
+        s["kv"] = [M.make_kv(s["k"][at:], s["v"][at:], per, s["rows"], (shape[1] * hkv * D, 0 if c["block"] else s["rows"] * hkv * D, D, hkv * D))
+                   for at in range(0, nl, per)]
+        s["ws_bytes"] = M.murmur_decode_attn_tree_workspace(per, B, c["hq"], hkv, T, s["keep"])
+        s["ws"] = torch.zeros(max(s["ws_bytes"], 256) // 4, dtype=torch.int32, device="cuda")
+        s["parts"] = [[x[at:at + per] for x in (s["q"], s["k_tree"], s["v_tree"], s["out"], s["lse"])] for at in range(0, nl, per)]
+    return s
+
+
+# ---- one pass -------------------------------------------------------------------------------------------------------
+
+def run(s):
+    c = s["case"]
+    if own:
+        return _own(s, c)
+    return {"reserve": _reserve, "rope": _rope, "tree": _tree, "accept": _accept}[c["op"]](s, c)
+
+
+def _own(s, c):
+    from paper_2606_01483_amd import murmur as M
+    if c["op"] == "reserve":
+        s["book"].copy_(s["book0"])
+        n = s["shape"][0] * s["shape"][1]
+        table, ref, top = s["book"][:n], s["book"][n:n + s["n_blocks"]], s["book"][n + s["n_blocks"]:]
+        slot, pos, seq = s["maps"]
+        M.murmur_paged_reserve(s["length"], s["new"], c["batch"], table, s["shape"][1], c["block"], ref if c["counted"] else None,
+                               s["n_blocks"], s["stack"], top, s["n_blocks"], s["per"], s["n_tokens"], s["start"], s["got"],
+                               slot, pos, seq, s["ws"], s["ws_bytes"])
+        return s["book"], s["start"], s["got"], s["maps"]
+    if c["op"] == "rope":
+        M.murmur_rope_append(s["rope"], s["in"], s["pos"], s["slot"], None, s["n"], c["hq"], c["hkv"], D, s["q_out"], s["kv"])
+        return s["q_out"], s["k"][:, :s["rows"]], s["v"][:, :s["rows"]]
+    if c["op"] == "accept":
+        M.murmur_tree_accept(s["parent"], 1, c["nodes"], s["token"], s["said"], s["slot"], c["batch"], s["k_tree"], s["v_tree"],
+                             s["kv"], c["hkv"], s["path"], s["count"], s["last"])
+        return s["path"], s["count"], s["last"], s["k"][:, :s["rows"]], s["v"][:, :s["rows"]]
+    dtype = M.MURMUR_DTYPE_F32 if c["out_f32"] else M.MURMUR_DTYPE_BF16
+    cols = s["table"].shape[1] if c["block"] else 0
+    for kv, (q, k_tree, v_tree, out, lse) in zip(s["kv"], s["parts"]):
+        M.murmur_decode_attn_tree(s["seg"], s["pol"], 0, s["parent"], 1, c["nodes"], q, kv, k_tree, v_tree, s["table"], cols,
+                                  c["block"], s["keep"], c["batch"], c["hq"], c["hkv"], D, s["scale"], out, dtype, lse,
+                                  s["ws"], s["ws_bytes"])
+    return s["out"], s["lse"]
+
+
+def _reserve(s, c):
+    bs, (B, cols) = c["block"], s["shape"]
+    n = B * cols
+    table, ref, top = s["book0"][:n].view(B, cols), s["book0"][n:-1], s["book0"][-1:]
+    length, new = s["length"].long(), s["new"].long()
+    col = torch.arange(cols, device="cuda")
+    end = length + new
+    named = (col >= (length // bs)[:, None]) & (col <= ((end - 1) // bs)[:, None]) & (new > 0)[:, None]
+    missing = named & (table < 0)
+    need = missing.sum(1)
+    upto = need.cumsum(0)
+    served = (need == 0) | (upto <= top)
+    rank = (upto - need)[:, None] + missing.cumsum(1) - 1
+    take = missing & served[:, None]
+    got = s["stack"][(top.long() - 1 - rank).clamp(0, len(s["stack"]) - 1)]
+    table2 = torch.where(take, got, table)
+    ref2 = ref
+    if c["counted"]:
+        hits = torch.zeros(s["n_blocks"] + 1, dtype=torch.int32, device="cuda")
+        hits[torch.where(take, got, s["n_blocks"]).long().view(-1)] = 1
+        ref2 = torch.where(hits[:-1] > 0, hits[:-1], ref)
+    top2 = top - torch.where(served & (need > 0), upto, 0).max()
+    start = torch.cat([torch.zeros_like(new[:1]), new.cumsum(0)])
+    token = torch.arange(s["n_tokens"], device="cuda")
+    if s["per"]:
+        start = torch.arange(B + 1, device="cuda") * s["per"]
+        seq = token // s["per"]
+    else:
+        seq = (torch.searchsorted(start, token, right=True) - 1).clamp(max=B - 1)
+    off = token - start[seq]
+    there = off < new[seq]
+    pos = length[seq] + off
+    block = table2[seq, (pos // bs).clamp(max=cols - 1)]
+    slot = torch.where(there & served[seq], block.long() * bs + pos % bs, -1)
+    maps = torch.stack([slot, torch.where(there, pos, -1), torch.where(there, seq, -1)]).int()
+    book = torch.cat([table2.reshape(-1), ref2, top2.int()])
+    return book, start.int(), torch.where(served, new, -1).int(), maps
+
+
+def _rope(s, c):
+    hq, hkv, rot, nl = c["hq"], c["hkv"], c["rot"], c["layers"]
+    x = s["qkv"].view(nl, s["n"], hq + 2 * hkv, D).float()
+    turn = s["pos"].double()[:, None] * s["freq"]
+    turn = (turn - torch.floor(turn)) * (2.0 * math.pi)
+    cos, sin = (torch.cos(turn) * s["gain"]).float()[:, None], (torch.sin(turn) * s["gain"]).float()[:, None]
+    r = x[:, :, :hq + hkv]
+    a, b = (r[..., 0:rot:2], r[..., 1:rot:2]) if c["interleaved"] else (r[..., :rot // 2], r[..., rot // 2:rot])
+    u, w = a * cos - b * sin, a * sin + b * cos
+    turned = torch.stack([u, w], -1).flatten(-2) if c["interleaved"] else torch.cat([u, w], -1)
+    r = torch.cat([turned, r[..., rot:]], -1)
+    q = torch.where((s["pos"] >= 0)[:, None, None], r[:, :, :hq], 0.0).to(torch.bfloat16)
+    row = torch.where(s["slot"] >= 0, s["slot"], s["rows"]).long()  # the row behind the last takes what is not there
+    s["k"][:, row] = r[:, :, hq:].to(torch.bfloat16)
+    s["v"][:, row] = x[:, :, hq + hkv:].to(torch.bfloat16)
+    return q, s["k"][:, :s["rows"]], s["v"][:, :s["rows"]]
+
+
+def _ancestors(parent):
+    """[B, T, T]: whether node j is node i or above it; and depths."""
+    T = parent.shape[1]
+    at = torch.arange(T, device="cuda")
+    one = (parent[:, :, None] == at).double() + torch.eye(T, dtype=torch.float64, device="cuda")
+    above = torch.linalg.matrix_power(one, T) > 0
+    return above, above.sum(-1) - 1
+
+
+def _tree(s, c):
+    hq, hkv, nl, B, T = c["hq"], c["hkv"], c["layers"], c["batch"], c["nodes"]
+    pre, ls, mid, j = (x[:, None, None] for x in s["seg"].long().unbind(1))
+    above, depth = _ancestors(s["parent"].long())
+    step = j + depth[:, :, None]
+    p = torch.arange(s["length"], device="cuda")
+    t, o = p - pre, p - pre - ls - mid
+    first = torch.minimum((step - max(c["delay"], 1) + 1).clamp(min=0), (ls - c["w_s"]).clamp(min=0))
+    speech = (t < c["sink_s"]) | ((t >= first) & (t < first + c["w_s"])) if c["w_s"] != OFF else t >= 0
+    outs = (o < c["sink_o"]) | (o >= step - c["w_o"]) if c["w_o"] != OFF else o >= 0
+    cached = (p < pre) | ((t >= 0) & (t < ls) & speech) | ((t >= ls) & (o < 0)) | ((o >= 0) & (o < j - 1) & outs)
+    index = (j - 1 + depth[:, None, :])
+    near = (index < c["sink_o"]) | (index >= step - c["w_o"]) if c["w_o"] != OFF else index >= 0
+    there = (s["parent"] >= -1) & (s["seg"][:, 3:] > 0)
+    mask = torch.cat([cached.expand(B, T, -1), above & near], -1) & there[:, :, None]
+    live = cached.any(1) & (s["seg"][:, 3:] > 0)
+    if c["block"]:
+        row = s["table"].long()[:, p // c["block"]] * c["block"] + p % c["block"]
+    else:
+        row = torch.arange(B, device="cuda")[:, None] * s["length"] + p
+    row = torch.where(live, row, 0)
+
+    def whole(cache, tree):  # [nl, B, hkv, positions and nodes, D]
+        x = torch.where(live[None, :, :, None, None], cache[:, row].float(), 0.0)
+        return torch.cat([x, tree.float()], 2).transpose(2, 3)
+
+    k, v = whole(s["k"], s["k_tree"]), whole(s["v"], s["v_tree"])
+    q = s["q"].float().view(nl, B, T, hkv, hq // hkv, D).permute(0, 1, 3, 2, 4, 5).reshape(nl, B, hkv, -1, D)
+    x = torch.matmul(q, k.transpose(-1, -2)).mul_(s["scale"]).view(nl, B, hkv, T, hq // hkv, -1)
+    x.masked_fill_(~mask[None, :, None, :, None], float("-inf"))
+    top = x.amax(-1, keepdim=True).clamp(min=-3e38)
+    x = x.sub_(top).exp_()
+    total = x.sum(-1, keepdim=True)
+    o = torch.matmul(x.view(nl, B, hkv, T * (hq // hkv), -1), v).view(nl, B, hkv, T, hq // hkv, D) / total
+    out = torch.where(there[None, :, None, :, None, None], o, 0.0).permute(0, 1, 3, 2, 4, 5).reshape(nl, B, T, hq, D)
+    lse = torch.where(there[None, :, None, :, None], (total.log() + top)[..., 0], 0.0).permute(0, 1, 3, 2, 4).reshape(nl, B, T, hq)
+    return out.to(s["out"].dtype), lse.contiguous()
+
+
+def _accept(s, c):
+    B, T, hkv, nl = c["batch"], c["nodes"], c["hkv"], c["layers"]
+    parent = s["parent"].long()
+    above, depth = _ancestors(parent)
+    same = (parent[:, :, None] == parent[:, None, :]) & (s["token"][:, :, None] == s["token"][:, None, :])
+    before = torch.tril(torch.ones(T, T, dtype=torch.bool, device="cuda"), -1)
+    said = torch.gather(s["said"], 1, parent.clamp(min=0))
+    root = (parent == -1) & (s["token"] >= 0)
+    match = root | ((parent >= 0) & (s["token"] == said) & (s["token"] >= 0) & ~(same & before).any(-1))
+    on = ((above & ~match[:, None, :]).sum(-1) == 0) & (parent >= -1) & root.any(1)[:, None]
+    count = on.sum(1)
+    node = torch.arange(T, device="cuda").expand(B, T)
+    path = torch.where(on, node, T).sort(1).values
+    last = torch.where(count > 0, torch.gather(s["said"], 1, torch.where(on, node, 0).amax(1, keepdim=True))[:, 0], -1)
+    row = torch.where(path < T, s["slot"].long(), s["rows"])
+    pick = path.clamp(max=T - 1)[None, :, :, None, None].expand(nl, B, T, hkv, D)
+    for cache, tree in ((s["k"], s["k_tree"]), (s["v"], s["v_tree"])):
+        cache[:, row.view(-1)] = torch.gather(tree, 2, pick).view(nl, B * T, hkv, D)
+    return (torch.where(path < T, path, -1).int(), count.int(), last.int(), s["k"][:, :s["rows"]], s["v"][:, :s["rows"]])
+
+
+# ---- the definitions in 64 bits -------------------------------------------------------------------------------------
+
+def exact(c, seed):
+    s = prepare(c, seed)
+    if c["op"] == "reserve":
+        return None  # whole numbers
+    if c["op"] == "accept":  # whole numbers, and rows as they were, by following the tree from its root
+        parent, token, said = (s[x].cpu().numpy() for x in ("parent", "token", "said"))
+        k, v = (torch.zeros((c["layers"], s["rows"], c["hkv"], D), dtype=torch.float64, device="cuda") for _ in range(2))
+        for b in range(c["batch"]):
+            at, n = 0 if token[b, 0] >= 0 else -1, 0
+            while at >= 0:
+                row, n = int(s["slot"][b, n]), n + 1
+                k[:, row], v[:, row] = s["k_tree"][:, b, at].double(), s["v_tree"][:, b, at].double()
+                at = next((t for t in range(c["nodes"]) if parent[b, t] == at and token[b, t] == said[b, at]), -1)
+        return None, None, None, k, v
+    if c["op"] == "rope":
+        pos, slot = s["pos"].cpu().numpy(), s["slot"].cpu().numpy()
+        there = np.flatnonzero(pos >= 0)
+        f, gain = _frequencies(c)
+        ang = 2.0 * math.pi * np.modf(np.maximum(pos, 0)[:, None].astype(np.float64) * f)[0]
+        half = c["rot"] // 2
+        turn = torch.from_numpy(gain * np.exp(1j * ang)).cuda()[:, None, :]
+        x = s["qkv"].double().view(c["layers"], s["n"], -1, D)
+        i = np.arange(half)
+        re, im = (2 * i, 2 * i + 1) if c["interleaved"] else (i, half + i)
+        k = torch.zeros((c["layers"], s["rows"], c["hkv"], D), dtype=torch.float64, device="cuda")
+        v, q = torch.zeros_like(k), torch.zeros((c["layers"], s["n"], c["hq"], D), dtype=torch.float64, device="cuda")
+        heads = c["hq"] + c["hkv"]
+        for layer in range(c["layers"]):
+            y = x[layer, :, :heads].clone()
+            z = torch.complex(x[layer, :, :heads][..., re], x[layer, :, :heads][..., im]) * turn
+            y[..., re], y[..., im] = z.real, z.imag
+            q[layer, there] = y[there, :c["hq"]]
+            k[layer, slot[there]] = y[there, c["hq"]:]
+            v[layer, slot[there]] = x[layer, there, heads:]
+        return q, k, v
+    lay = _layout(c)
+    hq, hkv, nl, B, T = c["hq"], c["hkv"], c["layers"], c["batch"], c["nodes"]
+    out = torch.zeros((nl, B, T, hq, D), dtype=torch.float64, device="cuda")
+    lse = torch.zeros((nl, B, T, hq), dtype=torch.float64, device="cuda")
+    for b in range(B):
+        p0, ls, p1, j = (int(x) for x in lay["seg"][b])
+        nodes = [t for t in range(T) if lay["parent"][b, t] >= -1] if j > 0 else []
+        if not nodes:
+            continue
+        pos = lay["kept"][b]
+        allowed = np.zeros((len(nodes), len(pos) + T), dtype=bool)
+        for n, t in enumerate(nodes):
+            now = j + int(lay["depth"][b, t])  # the step that this node's token is
+            sp, ou = pos - p0, pos - p0 - ls - p1
+            ok = (pos < p0) | ((sp >= ls) & (ou < 0))
+            lo = min(max(now - max(c["delay"], 1) + 1, 0), max(ls - c["w_s"], 0))
+            in_speech = (sp >= 0) & (sp < ls)
+            ok |= in_speech & ((sp < c["sink_s"]) | ((sp >= lo) & (sp < lo + c["w_s"])) | (c["w_s"] == OFF))
+            ok |= (ou >= 0) & ((ou < c["sink_o"]) | (ou >= now - c["w_o"]) | (c["w_o"] == OFF))
+            allowed[n, :len(pos)] = ok
+            a = t
+            while a >= 0:  # itself and what it follows, as outputs of their steps
+                o = j - 1 + int(lay["depth"][b, a])
+                allowed[n, len(pos) + a] = c["w_o"] == OFF or o < c["sink_o"] or o >= now - c["w_o"]
+                a = int(lay["parent"][b, a])
+        if c["block"]:
+            rows = s["table"].cpu().numpy()[b, pos // c["block"]].astype(np.int64) * c["block"] + pos % c["block"]
+        else:
+            rows = b * s["length"] + pos
+        rows, ok, nodes = torch.from_numpy(rows).cuda(), torch.from_numpy(allowed).cuda()[:, None, :], torch.tensor(nodes, device="cuda")
+        for layer in range(nl):
+            k, v = (torch.cat([x[layer, rows], y[layer, b]]).double() for x, y in ((s["k"], s["k_tree"]), (s["v"], s["v_tree"])))
+            for h in range(hkv):
+                heads = slice(h * (hq // hkv), (h + 1) * (hq // hkv))
+                q = s["q"][layer, b, nodes, heads].double()
+                w = ((q.reshape(-1, D) @ k[:, h].T) * s["scale"]).view(len(nodes), hq // hkv, -1)
+                w = torch.where(ok, w, -math.inf)
+                z = torch.logsumexp(w, -1)
+                out[layer, b, nodes, heads] = (torch.exp(w - z[..., None]).view(-1, w.shape[-1]) @ v[:, h]).view(len(nodes), -1, D)
+                lse[layer, b, nodes, heads] = z
+    return out, lse
