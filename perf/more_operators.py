@@ -312,7 +312,7 @@ def prepare(c, seed):
         f, s["gain"] = _frequencies(c)
         s["freq"] = torch.from_numpy(f).cuda()
         if own:
-            turns, gain = M.murmur_rope_freqs_host(c["rot"], c["base"], c["kind"], c["factor"], 4096.0)
+            turns, gain = M.murmur_rope_freqs_host(c["rot"], c["base"], getattr(M, "MURMUR_ROPE_" + c["kind"].upper()), c["factor"], 4096.0)
             s["turns"] = torch.from_numpy(turns.view(np.int64)).cuda()
             s["rope"] = M.make_rope(c["rot"], c["interleaved"], s["turns"], gain)
             step = 4 if c["f32"] else 2
@@ -404,7 +404,7 @@ def _own(s, c):
                                slot, pos, seq, s["ws"], s["ws_bytes"])
         return s["book"], s["start"], s["got"], s["maps"]
     if c["op"] == "rope":
-        M.murmur_rope_append(s["rope"], s["in"], s["pos"], s["slot"], None, s["n"], c["hq"], c["hkv"], D, s["q_out"], s["kv"])
+        M.murmur_rope_append(s["rope"], s["in"], s["pos"], s["slot"], None, 1, s["n"], c["hq"], c["hkv"], D, s["q_out"], s["kv"])
         return s["q_out"], s["k"][:, :s["rows"]], s["v"][:, :s["rows"]]
     if c["op"] == "accept":
         M.murmur_tree_accept(s["parent"], 1, c["nodes"], s["token"], s["said"], s["slot"], c["batch"], s["k_tree"], s["v_tree"],
