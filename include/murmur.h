@@ -27,7 +27,9 @@
  * A batch of hypotheses (beams, samples, drafted tokens) of the same chunks has
  * caches that agree up to where the hypotheses part.  murmur_shared.h has the calls
  * that keep block tables whose rows name the same blocks, and that attend over what
- * a group of sequences shares once for all of them.
+ * a group of sequences shares once for all of them.  murmur_draft.h has those that
+ * place requests in a paged pool, rotate queries and keys, and check trees of drafted
+ * tokens.
  *
  * Conventions shared by every call:
  *   - Pointers named *_dev are device memory (HIP, the current device); all
@@ -91,6 +93,7 @@ enum {
     MURMUR_DEVERR_PARENT = 128,  /* paged_fork: a parent outside [-1, B) */
     MURMUR_DEVERR_GROUP = 256,   /* shared_plan: groups out of order; decode_attn_shared: a plan of another call, or
                                   * shares found from lists where sequences have caches of their own */
+    MURMUR_DEVERR_TREE = 512,    /* decode_attn_tree, tree_accept: parents that are no tree (murmur_draft.h) */
 };
 
 /* One sequence (audio chunk) of the batch, Section 3.2's layout

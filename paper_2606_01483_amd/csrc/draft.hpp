@@ -1,0 +1,428 @@
+// Device code of requests into a paged pool, rotary positions and accepted paths
+// (included by kernels.hip).
+//
+//   reserve_count_kernel, reserve_take_kernel  blocks and slot maps for new tokens
+//   rope_wide_kernel, rope_pair_kernel         q and k rotated, K and V into the cache
+//   tree_accept_kernel                         the accepted path into the cache
+#pragma once
+
+namespace murmur {
+
+// ---------------------------------------------------------------------------
+// reserve.  Sequences are served in order, so a sequence's blocks are found from the
+// number that those before it need: the first launch counts (a wavefront per sequence,
+// and sums over kReserveGroup of them), the second pops and writes the maps, a
+// workgroup per sequence.  A sequence is refused where its blocks end behind the
+// stack, or its tokens behind the maps; then so is every later one that needs a block,
+// so those that are served pop without holes and the top is the minimum of what they
+// leave (an integer atomic, whose order does not matter).
+// ---------------------------------------------------------------------------
+constexpr int kReserveThreads = 64 * kReserveGroup;
+
+static __device__ __forceinline__ int64_t wave_sum64(int64_t x) {
+#pragma unroll
+    for (int d = 32; d >= 1; d /= 2) x += __shfl_xor(x, d);
+    return x;
+}
+
+__global__ __launch_bounds__(kReserveThreads) void reserve_count_kernel(const ReserveLaunch p) {
+    __shared__ ReserveSums s_sums[kReserveGroup];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int b = blockIdx.x * kReserveGroup + wave;
+    int need = 0, err = 0;
+    int32_t n = 0;
+    if (b < p.B) {
+        const int32_t len = p.len[b];
+        n = p.fresh[b];
+        const int64_t end = (int64_t)len + n;
+        if (len < 0 || n < 0) {
+            err = MURMUR_DEVERR_COUNT;
+            n = 0;
+        } else if (n > 0) {
+            const int64_t last = (end - 1) >> p.log2_bs;
+            if (last >= p.max_blocks) err = MURMUR_DEVERR_BLOCK;
+            else if (p.per_seq > 0 && n > p.per_seq) err = MURMUR_DEVERR_OVERFLOW;
+            else {
+                const int32_t *row = p.bt + (int64_t)b * p.max_blocks;
+                for (int c0 = len >> p.log2_bs; c0 <= (int)last; c0 += 64) {
+                    const int32_t x = c0 + lane <= (int)last ? row[c0 + lane] : 0;
+                    const bool in = c0 + lane <= (int)last;
+                    need += __popcll(__ballot(in && x < 0));
+                    const bool wrong = in && (x >= p.n_blocks || (p.ref && x >= 0 && p.ref[x] > 1));
+                    if (__ballot(wrong)) err = MURMUR_DEVERR_BLOCK;
+                }
+            }
+        }
+        if (lane == 0) p.need[b] = err ? -1 : need;
+        if (err) need = 0;
+    }
+    if (lane == 0) {
+        s_sums[wave] = ReserveSums{n, need, 0};
+        if (err) raise_device_error(err);
+    }
+    __syncthreads();
+    if (tid == 0) {
+        ReserveSums t{0, 0, 0};
+        for (int w = 0; w < kReserveGroup; ++w) {
+            t.tokens += s_sums[w].tokens;
+            t.blocks += s_sums[w].blocks;
+        }
+        p.sums[blockIdx.x] = t;
+        if (blockIdx.x == 0) *p.top0 = *p.top;
+    }
+}
+
+template <int kThreads>
+__global__ __launch_bounds__(kThreads) void reserve_take_kernel(const ReserveLaunch p) {
+    __shared__ int64_t s_tokens[2][kThreads / 64];
+    __shared__ int s_blocks[kThreads / 64];
+    __shared__ int s_bad;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = blockIdx.x;
+    const int groups = (p.B + kReserveGroup - 1) / kReserveGroup, mine = b / kReserveGroup;
+    if (tid == 0) s_bad = 0;
+    // tokens and blocks of the sequences before this one, and all tokens
+    int64_t tokens = 0, all = 0;
+    int blocks = 0;
+    for (int i = tid; i < groups; i += kThreads) {
+        const ReserveSums t = p.sums[i];
+        tokens += i < mine ? t.tokens : 0;
+        blocks += i < mine ? t.blocks : 0;
+        all += t.tokens;
+    }
+    if (tid < b - mine * kReserveGroup) {
+        const int o = mine * kReserveGroup + tid;
+        const int32_t n = p.need[o];
+        blocks += max(n, 0);
+        tokens += p.len[o] >= 0 ? max(p.fresh[o], 0) : 0;
+    }
+    tokens = wave_sum64(tokens);
+    all = wave_sum64(all);
+    blocks = wave_sum(blocks);
+    if (lane == 0) {
+        s_tokens[0][wave] = tokens;
+        s_tokens[1][wave] = all;
+        s_blocks[wave] = blocks;
+    }
+    __syncthreads();
+    tokens = all = blocks = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; ++w) {
+        tokens += s_tokens[0][w];
+        all += s_tokens[1][w];
+        blocks += s_blocks[w];
+    }
+    const auto start_at = [&](int64_t packed, int q) {
+        return (int32_t)min(p.per_seq > 0 ? (int64_t)q * p.per_seq : packed, (int64_t)0x7fffffff);
+    };
+    const int32_t len = p.len[b], fresh = len >= 0 ? max(p.fresh[b], 0) : 0, need = p.need[b];
+    const int64_t at = p.per_seq > 0 ? (int64_t)b * p.per_seq : tokens;
+    const int32_t top = min(max(*p.top0, 0), p.n_blocks);
+    int err = 0;
+    bool served = need >= 0;
+    if (served && at + fresh > p.n_tokens) {
+        served = false;
+        err |= MURMUR_DEVERR_OVERFLOW;
+    } else if (served && need > 0 && (int64_t)blocks + need > top) {
+        served = false;
+        err |= MURMUR_DEVERR_POOL;
+    }
+    const int first = served && fresh > 0 ? len >> p.log2_bs : 0;
+    const int last = served && fresh > 0 ? (int)(((int64_t)len + fresh - 1) >> p.log2_bs) : -1;
+    int32_t *row = p.bt + (int64_t)b * p.max_blocks;
+    // the blocks: the k-th that is missing is the k-th from the top behind those of the sequences before
+    if (served && need > 0) {
+        int k = top - 1 - blocks;
+        for (int c0 = first; c0 <= last; c0 += kThreads) {
+            const int c = c0 + tid;
+            const bool missing = c <= last && row[c] < 0;
+            int total;
+            const int off = wg_exclusive_scan<kThreads>(missing, s_blocks, tid, total);
+            if (missing) {
+                const int32_t x = p.stack[k - off];
+                if (x >= 0 && x < p.n_blocks) {
+                    row[c] = x;
+                    if (p.ref) p.ref[x] = 1;
+                } else {
+                    s_bad = 1;
+                }
+            }
+            k -= total;
+        }
+        if (tid == 0)
+            __hip_atomic_fetch_min(p.top, top - blocks - need, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (s_bad) {
+        served = false;
+        err |= MURMUR_DEVERR_POOL;
+    }
+    // the maps
+    const int64_t end = p.per_seq > 0 ? min(at + p.per_seq, (int64_t)p.n_tokens) : min(at + fresh, (int64_t)p.n_tokens);
+    for (int64_t i = at + tid; i < end; i += kThreads) {
+        const int64_t pos = len + (i - at);
+        const bool there = i - at < fresh;
+        int32_t slot = -1;
+        if (there && served) slot = (row[pos >> p.log2_bs] << p.log2_bs) | (int32_t)(pos & ((1 << p.log2_bs) - 1));
+        p.slot[i] = slot;
+        if (p.pos) p.pos[i] = there ? (int32_t)min(pos, (int64_t)0x7fffffff) : -1;
+        if (p.seq) p.seq[i] = there ? b : -1;
+    }
+    for (int64_t i = (p.per_seq > 0 ? (int64_t)p.B * p.per_seq : all) + (int64_t)b * kThreads + tid; i < p.n_tokens;
+         i += (int64_t)p.B * kThreads) {
+        p.slot[i] = -1;
+        if (p.pos) p.pos[i] = -1;
+        if (p.seq) p.seq[i] = -1;
+    }
+    if (tid == 0) {
+        p.got[b] = served ? fresh : -1;
+        p.start[b] = start_at(tokens, b);
+        if (b == p.B - 1) p.start[p.B] = start_at(all, p.B);
+        if (err) raise_device_error(err);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// rope.  Position p turns pair i by the fraction p * freq[i] mod 2^64, an integer
+// product that is exact at any position; its nearest quarter turn is taken off and the
+// rest, at most pi / 4, goes through the Taylor series of sine and cosine.
+// ---------------------------------------------------------------------------
+static __device__ __forceinline__ void turn_of(uint64_t freq, int32_t p, float gain, float &cos, float &sin) {
+    const uint64_t turn = freq * (uint64_t)(uint32_t)p;
+    const uint32_t t = (uint32_t)(turn >> 32), quarter = (t + 0x20000000u) >> 30;
+    const float x = (float)(int32_t)(t - (quarter << 30)) * 1.4629180792671596e-9f;  // 2 pi / 2^32: at most pi / 4
+    const float x2 = x * x;
+    // what is left off is below 2^-28: x^11 / 11! and x^12 / 12!
+    float s = fmaf(x2, fmaf(x2, fmaf(x2, 2.7557319e-6f, -1.9841270e-4f), 8.3333333e-3f), -1.6666667e-1f);
+    s = fmaf(x * x2, s, x);
+    float c = fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, -2.7557319e-7f, 2.4801587e-5f), -1.3888889e-3f), 4.1666667e-2f), -0.5f);
+    c = fmaf(x2, c, 1.f);
+    const bool swap = quarter & 1;
+    const float cs = swap ? s : c, sn = swap ? c : s;
+    // quarters 1 and 2 negate the cosine, 2 and 3 the sine
+    cos = ((quarter + 1) & 2 ? -cs : cs) * gain;
+    sin = (quarter & 2 ? -sn : sn) * gain;
+}
+
+// Where a token's heads go: q, then k, then v.
+struct RopeToken {
+    int layer, t;
+    int32_t pos;
+    int64_t cache;  // of its K and V in the cache, or -1
+};
+static __device__ __forceinline__ bool rope_token(const RopeLaunch &p, int64_t item, bool raise, RopeToken &x) {
+    if (item >= (int64_t)p.NL * p.n_tokens) return false;
+    x.layer = (int)(item / p.n_tokens);
+    x.t = (int)(item - (int64_t)x.layer * p.n_tokens);
+    x.pos = p.pos[x.t];
+    if (x.pos < 0) return false;
+    const int32_t slot = p.slot[x.t], seq = p.seq ? p.seq[x.t] : 0;
+    const bool good = slot < p.max_len && (uint32_t)seq < (uint32_t)p.n_seqs;
+    x.cache = slot >= 0 && good ? x.layer * p.s_layer + seq * p.s_b + slot * p.s_pos : -1;
+    if (slot >= 0 && !good && raise) raise_device_error(MURMUR_DEVERR_POSITION);
+    return true;
+}
+template <typename T>
+static __device__ __forceinline__ const T *rope_source(const RopeLaunch &p, const RopeToken &x, int h) {
+    const int64_t kv = x.layer * p.kv_layer + x.t * p.kv_token;
+    if (h < p.Hq) return reinterpret_cast<const T *>(p.q) + x.layer * p.q_layer + x.t * p.q_token + (int64_t)h * kHeadDim;
+    if (h < p.Hq + p.Hkv) return reinterpret_cast<const T *>(p.k) + kv + (int64_t)(h - p.Hq) * kHeadDim;
+    return reinterpret_cast<const T *>(p.v) + kv + (int64_t)(h - p.Hq - p.Hkv) * kHeadDim;
+}
+// null: not kept
+static __device__ __forceinline__ uint16_t *rope_target(const RopeLaunch &p, const RopeToken &x, int h) {
+    if (h < p.Hq) return p.q_out + (((int64_t)x.layer * p.n_tokens + x.t) * p.Hq + h) * kHeadDim;
+    if (x.cache < 0) return nullptr;
+    return h < p.Hq + p.Hkv ? p.k_cache + x.cache + (h - p.Hq) * p.s_h : p.v_cache + x.cache + (h - p.Hq - p.Hkv) * p.s_h;
+}
+
+// Eight values of a head as floats.
+static __device__ __forceinline__ void load8(const uint16_t *from, float (&x)[8]) {
+    const u32x4 y = load16(from);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __builtin_bit_cast(float, y[i] << 16);
+        x[2 * i + 1] = __builtin_bit_cast(float, y[i] & 0xffff0000u);
+    }
+}
+static __device__ __forceinline__ void load8(const float *from, float (&x)[8]) {
+    const f32x4 y0 = *reinterpret_cast<const f32x4 *>(from), y1 = *reinterpret_cast<const f32x4 *>(from + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[i] = y0[i];
+        x[4 + i] = y1[i];
+    }
+}
+static __device__ __forceinline__ void store8(uint16_t *to, const float (&x)[8]) {
+    *reinterpret_cast<u32x4 *>(to) = u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+}
+
+// A wavefront per (layer, token).  A head is eight units of two 16-byte (bf16) chunks,
+// a lane has one of them in every eighth head: eight pairs that turn alike in all
+// heads, so the sines are computed once.
+template <typename T, bool kInterleaved>
+__global__ __launch_bounds__(256) void rope_wide_kernel(const RopeLaunch p) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int u = lane & 7;
+    RopeToken x;
+    if (!rope_token(p, (int64_t)blockIdx.x * 4 + wave, lane == 0, x)) return;
+    const bool turns = 16 * u < p.rot;
+    const int at0 = kInterleaved || !turns ? 16 * u : 8 * u, at1 = kInterleaved || !turns ? 16 * u + 8 : p.rot / 2 + 8 * u;
+    float cos[8], sin[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        cos[i] = 1.f;
+        sin[i] = 0.f;
+        if (turns) turn_of(p.freq[8 * u + i], x.pos, p.gain, cos[i], sin[i]);
+    }
+    const int heads = p.Hq + 2 * p.Hkv;
+    for (int h = lane >> 3; h < heads; h += 8) {
+        uint16_t *to = rope_target(p, x, h);
+        if (!to) continue;
+        const T *from = rope_source<T>(p, x, h);
+        float a[8], b[8];
+        load8(from + at0, a);
+        load8(from + at1, b);
+        if (turns && h < p.Hq + p.Hkv) {
+            if (kInterleaved) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    float &e = i < 4 ? a[2 * i] : b[2 * i - 8], &o = i < 4 ? a[2 * i + 1] : b[2 * i - 7];
+                    const float y = fmaf(e, cos[i], -(o * sin[i]));
+                    o = fmaf(e, sin[i], o * cos[i]);
+                    e = y;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float y = fmaf(a[i], cos[i], -(b[i] * sin[i]));
+                    b[i] = fmaf(a[i], sin[i], b[i] * cos[i]);
+                    a[i] = y;
+                }
+            }
+        }
+        store8(to + at0, a);
+        store8(to + at1, b);
+    }
+}
+
+// The same for any rot_dim and alignment: a lane has a pair of elements of every head.
+template <typename T>
+__global__ __launch_bounds__(256) void rope_pair_kernel(const RopeLaunch p) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    RopeToken x;
+    if (!rope_token(p, (int64_t)blockIdx.x * 4 + wave, lane == 0, x)) return;
+    const int half = p.rot / 2;
+    const bool turns = lane < half;
+    const int at0 = p.interleaved || !turns ? 2 * lane : lane, at1 = p.interleaved || !turns ? 2 * lane + 1 : half + lane;
+    float cos = 1.f, sin = 0.f;
+    if (turns) turn_of(p.freq[lane], x.pos, p.gain, cos, sin);
+    const auto value = [](auto y) {
+        if constexpr (sizeof(y) == 2) return __builtin_bit_cast(float, (uint32_t)y << 16);
+        else return (float)y;
+    };
+    const int heads = p.Hq + 2 * p.Hkv;
+#pragma unroll 4
+    for (int h = 0; h < heads; ++h) {
+        uint16_t *to = rope_target(p, x, h);
+        if (!to) continue;
+        const T *from = rope_source<T>(p, x, h);
+        float a = value(from[at0]), b = value(from[at1]);
+        if (turns && h < p.Hq + p.Hkv) {
+            const float y = fmaf(a, cos, -(b * sin));
+            b = fmaf(a, sin, b * cos);
+            a = y;
+        }
+        const uint32_t both = pack_bf16(a, b);
+        to[at0] = (uint16_t)both;
+        to[at1] = (uint16_t)(both >> 16);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// accept.  A wavefront follows the path from the root, a step a ballot; every
+// workgroup of a sequence does so for itself, then they copy the path's rows.
+// ---------------------------------------------------------------------------
+constexpr int kAcceptPlanes = 4;  // (layer, K or V) planes of a workgroup
+
+__global__ __launch_bounds__(256) void tree_accept_kernel(const AcceptLaunch p) {
+    const int tid = threadIdx.x, lane = tid & 63, b = blockIdx.x, T = p.T;
+    const int par = lane < T ? p.parent[(p.parent_per_seq ? (int64_t)b * T : 0) + lane] : -2;
+    const int32_t token = lane < T ? p.token[(int64_t)b * T + lane] : -1, next = lane < T ? p.next[(int64_t)b * T + lane] : -1;
+    const int32_t slot = lane < T ? p.slot[(int64_t)b * T + lane] : -1;
+    const uint64_t there = __ballot(par != -2);
+    const bool ok = par == -2 || (lane == 0 ? par == -1 : par >= 0 && par < lane && (there >> (par & 63) & 1));
+    const bool invalid = __ballot(!ok) != 0;
+    int n = 0, at = 0;
+    int32_t mine = -1, last = -1;  // lane i: the path's node i
+    if (!invalid && (there & 1) && __builtin_amdgcn_readfirstlane(token) >= 0) {
+        for (;;) {
+            if (lane == n) mine = at;
+            ++n;
+            last = __builtin_amdgcn_readlane(next, at);
+            const uint64_t child = __ballot(par == at && token == last && token >= 0);
+            if (!child) break;
+            at = __builtin_ctzll(child);
+        }
+    }
+    const bool far = lane < n && slot >= p.max_len;
+    if (blockIdx.y == 0 && tid < 64) {
+        if (lane < T) p.path[(int64_t)b * T + lane] = mine;
+        if (lane == 0) {
+            p.count[b] = n;
+            p.last[b] = last;
+        }
+        const int err = (invalid ? MURMUR_DEVERR_TREE : 0) | (__ballot(far) ? MURMUR_DEVERR_POSITION : 0);
+        if (lane == 0 && err) raise_device_error(err);
+    }
+    const int chunks = p.Hkv * 16, planes = 2 * p.NL;
+    for (int lv = blockIdx.y * kAcceptPlanes; lv < min((int)blockIdx.y * kAcceptPlanes + kAcceptPlanes, planes); ++lv) {
+        const int layer = lv >> 1;
+        const uint16_t *from = ((lv & 1) ? p.v_tree : p.k_tree) + ((int64_t)layer * p.B + b) * T * p.Hkv * kHeadDim;
+        uint16_t *to = ((lv & 1) ? p.v : p.k) + layer * p.s_layer + b * p.s_b;
+        for (int i0 = 0; i0 < n * chunks; i0 += 256) {  // every lane goes along: it may hold what another one needs
+            const int i = i0 + tid, step = min(i / chunks, n - 1), c = i - step * chunks;
+            const int32_t node = __shfl(mine, step), row = __shfl(slot, step);
+            if (i < n * chunks && row >= 0 && row < p.max_len)
+                *reinterpret_cast<u32x4 *>(to + row * p.s_pos + (c >> 4) * p.s_h + 8 * (c & 15)) =
+                    load16(from + (int64_t)node * p.Hkv * kHeadDim + 8 * c);
+        }
+    }
+}
+
+// ---- launchers ----
+
+int launch_paged_reserve(const ReserveLaunch &p, murmur_stream_t stream) {
+    hipLaunchKernelGGL(reserve_count_kernel, dim3((unsigned)((p.B + kReserveGroup - 1) / kReserveGroup)), dim3(kReserveThreads),
+                       0, (hipStream_t)stream, p);
+    const int e = (int)hipGetLastError();
+    if (e != 0) return e;
+    if (p.n_tokens / p.B <= 256)
+        hipLaunchKernelGGL(reserve_take_kernel<64>, dim3((unsigned)p.B), dim3(64), 0, (hipStream_t)stream, p);
+    else
+        hipLaunchKernelGGL(reserve_take_kernel<1024>, dim3((unsigned)p.B), dim3(1024), 0, (hipStream_t)stream, p);
+    return (int)hipGetLastError();
+}
+
+int launch_rope_append(const RopeLaunch &p, murmur_stream_t stream) {
+    const dim3 grid((unsigned)(((int64_t)p.NL * p.n_tokens + 3) / 4)), threads(256);
+    const hipStream_t s = (hipStream_t)stream;
+    if (!p.wide) {
+        if (p.f32) hipLaunchKernelGGL(rope_pair_kernel<float>, grid, threads, 0, s, p);
+        else hipLaunchKernelGGL(rope_pair_kernel<uint16_t>, grid, threads, 0, s, p);
+    } else if (p.f32) {
+        if (p.interleaved) hipLaunchKernelGGL((rope_wide_kernel<float, true>), grid, threads, 0, s, p);
+        else hipLaunchKernelGGL((rope_wide_kernel<float, false>), grid, threads, 0, s, p);
+    } else {
+        if (p.interleaved) hipLaunchKernelGGL((rope_wide_kernel<uint16_t, true>), grid, threads, 0, s, p);
+        else hipLaunchKernelGGL((rope_wide_kernel<uint16_t, false>), grid, threads, 0, s, p);
+    }
+    return (int)hipGetLastError();
+}
+
+int launch_tree_accept(const AcceptLaunch &p, murmur_stream_t stream) {
+    const unsigned y = (unsigned)((2 * (int64_t)p.NL + kAcceptPlanes - 1) / kAcceptPlanes);
+    hipLaunchKernelGGL(tree_accept_kernel, dim3((unsigned)p.B, y), dim3(256), 0, (hipStream_t)stream, p);
+    return (int)hipGetLastError();
+}
+
+}  // namespace murmur

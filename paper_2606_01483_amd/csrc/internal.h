@@ -304,6 +304,70 @@ struct SharedAttnLaunch {
 };
 int launch_decode_attn_shared(const SharedAttnLaunch &a, murmur_stream_t stream);
 
+// ---- requests, rotary positions and trees of drafted tokens (draft.cpp; draft.hpp and tree_attn.hpp) ----
+
+constexpr int kReserveGroup = 16;  // sequences whose needs one workgroup counts, a wavefront each
+struct ReserveSums {               // of kReserveGroup sequences
+    int64_t tokens;
+    int32_t blocks, unused;
+};
+struct ReserveLaunch {
+    const int32_t *len, *fresh;
+    int32_t *bt, *ref, *stack, *top;
+    int32_t *start, *got, *slot, *pos, *seq;
+    int32_t *top0, *need;  // workspace: the stack's top before the call; blocks that a sequence needs, -1: refused
+    ReserveSums *sums;
+    int32_t B, max_blocks, log2_bs, n_blocks, per_seq, n_tokens;
+};
+int launch_paged_reserve(const ReserveLaunch &p, murmur_stream_t stream);
+
+struct RopeLaunch {
+    const void *q, *k, *v;
+    int64_t q_layer, q_token, kv_layer, kv_token;
+    const int32_t *pos, *slot, *seq;
+    const uint64_t *freq;
+    uint16_t *q_out, *k_cache, *v_cache;
+    int64_t s_layer, s_b, s_h, s_pos;
+    float gain;
+    int32_t rot, interleaved, f32, wide;  // wide: 16-byte loads, and rot is a multiple of 16
+    int32_t n_tokens, n_seqs, max_len, Hq, Hkv, NL;
+};
+int launch_rope_append(const RopeLaunch &p, murmur_stream_t stream);
+
+struct AcceptLaunch {
+    const int32_t *parent, *token, *next, *slot;
+    const uint16_t *k_tree, *v_tree;
+    uint16_t *k, *v;
+    int64_t s_layer, s_b, s_h, s_pos;
+    int32_t *path, *count, *last;
+    int32_t parent_per_seq, T, B, Hkv, NL, max_len;
+};
+int launch_tree_accept(const AcceptLaunch &p, murmur_stream_t stream);
+
+constexpr int kMaxNodes = 64;
+enum TreeShape : int32_t { kTree16, kTree32, kTree64, kTree128 };  // query rows of a workgroup
+struct TreePlan {
+    TreeShape shape;
+    int32_t n_split, row_sets;
+    int64_t units;  // (layer, sequence, KV head) groups times splits
+    size_t o_bytes, total;
+};
+TreePlan tree_plan(int32_t n_layers, int32_t B, int32_t Hq, int32_t Hkv, int32_t n_nodes, int32_t max_keep);
+struct TreeLaunch {
+    const int32_t *seg, *pol, *parent, *bt;
+    const uint16_t *q, *k, *v, *k_tree, *v_tree;
+    int64_t s_layer, s_b, s_h, s_pos;
+    void *out;
+    float *lse;
+    float *part_o;   // [groups][n_split][T * G][128]
+    float *part_ml;  // [groups][n_split][T * G][2]  (running max in log2 units, sum)
+    int32_t pol_mode, parent_per_seq, T, max_blocks, log2_bs, max_len, B, Hq, Hkv, G, NL, out_f32;
+    int32_t n_split, row_sets, units, shape;
+    uint32_t magic_g;  // ceil(2^16 / G): row / G is the high half of their product for rows up to 1024
+    float scale_log2;
+};
+int launch_decode_attn_tree(const TreeLaunch &a, murmur_stream_t stream);
+
 int read_and_clear_device_error(murmur_stream_t stream, int32_t *code);
 const char *hip_error_text(int err);
 

@@ -15,6 +15,8 @@
 //   paged cache (freeing behind the windows, appending the current token).
 //   pages.hpp, shared_attn.hpp (at the end): shared pages, and the attention over
 //   what a group of sequences shares.
+//   draft.hpp, tree_attn.hpp: requests into the pool, rotary positions, accepted
+//   paths, and the attention of trees of drafted tokens.
 //
 // Attention data flow per 64-wide wavefront and pass of 32 retained positions:
 //   K, V rows --global_load_lds_dwordx4--> LDS stage (XOR-swizzled 16 B chunks)
@@ -2356,3 +2358,5 @@ const char *hip_error_text(int err) { return hipGetErrorString((hipError_t)err);
 
 #include "pages.hpp"
 #include "shared_attn.hpp"
+#include "draft.hpp"
+#include "tree_attn.hpp"

@@ -1,4 +1,4 @@
-// Python entry to the per-step calls of libmurmur (include/murmur.h, include/murmur_shared.h): converts
+// Python entry to the per-step calls of libmurmur (include/murmur.h, murmur_shared.h, murmur_draft.h): converts
 // the arguments of one call in C and makes it.  murmur.py's ctypes calls did
 // the same in about 4.4 us for a decode step of 22 arguments, more than the
 // launch itself; this takes about 1.2 us.  Each function takes the C function's
@@ -11,13 +11,14 @@
 #include <tuple>
 #include <utility>
 
+#include "murmur_draft.h"
 #include "murmur_shared.h"
 
 namespace {
 
 PyObject *g_data_ptr;  // "data_ptr"
-// murmur.py's classes of the two structures (structures(), called once when it is imported)
-PyTypeObject *g_kv_type, *g_ring_type;
+// murmur.py's classes of the structures (structures(), called once when it is imported)
+PyTypeObject *g_kv_type, *g_ring_type, *g_rope_type, *g_qkv_type;
 
 // One argument: get() is false when the object is not taken (with or without
 // an exception set).
@@ -67,6 +68,10 @@ template <>
 struct Arg<const murmur_kv *> : StructArg<murmur_kv, g_kv_type> {};
 template <>
 struct Arg<const murmur_ring *> : StructArg<murmur_ring, g_ring_type> {};
+template <>
+struct Arg<const murmur_rope *> : StructArg<murmur_rope, g_rope_type> {};
+template <>
+struct Arg<const murmur_qkv *> : StructArg<murmur_qkv, g_qkv_type> {};
 
 template <>
 struct Arg<int32_t> {
@@ -142,18 +147,25 @@ ENTRY(paged_step_shared)
 ENTRY(paged_compact)
 ENTRY(shared_plan)
 ENTRY(decode_attn_shared)
+ENTRY(paged_reserve)
+ENTRY(rope_append)
+ENTRY(decode_attn_tree)
+ENTRY(tree_accept)
 
 PyObject *structures(PyObject *, PyObject *const *args, Py_ssize_t n) {
-    if (n != 2 || !PyType_Check(args[0]) || !PyType_Check(args[1])) {
-        PyErr_SetString(PyExc_TypeError, "structures: the classes of murmur_kv and murmur_ring");
+    PyTypeObject **const types[] = {&g_kv_type, &g_ring_type, &g_rope_type, &g_qkv_type};
+    constexpr Py_ssize_t count = sizeof(types) / sizeof(types[0]);
+    bool good = n == count;
+    for (Py_ssize_t i = 0; good && i < count; ++i) good = PyType_Check(args[i]);
+    if (!good) {
+        PyErr_SetString(PyExc_TypeError, "structures: the classes of murmur_kv, murmur_ring, murmur_rope and murmur_qkv");
         return nullptr;
     }
-    Py_INCREF(args[0]);
-    Py_INCREF(args[1]);
-    Py_XDECREF(g_kv_type);
-    Py_XDECREF(g_ring_type);
-    g_kv_type = reinterpret_cast<PyTypeObject *>(args[0]);
-    g_ring_type = reinterpret_cast<PyTypeObject *>(args[1]);
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        Py_INCREF(args[i]);
+        Py_XDECREF(*types[i]);
+        *types[i] = reinterpret_cast<PyTypeObject *>(args[i]);
+    }
     Py_RETURN_NONE;
 }
 
@@ -162,7 +174,8 @@ PyMethodDef g_methods[] = {METHOD(evict_compact),      METHOD(evict_compact_page
                            METHOD(decode_step),        METHOD(decode_step_static),  METHOD(decode_step_ring),
                            METHOD(paged_step),         METHOD(paged_fork),          METHOD(paged_step_shared),
                            METHOD(paged_compact),      METHOD(shared_plan),         METHOD(decode_attn_shared),
-                           METHOD(structures),         {nullptr, nullptr, 0, nullptr}};
+                           METHOD(paged_reserve),      METHOD(rope_append),         METHOD(decode_attn_tree),
+                           METHOD(tree_accept),        METHOD(structures),          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_pycall", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

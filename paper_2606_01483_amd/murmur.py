@@ -1,4 +1,4 @@
-"""ctypes binding of libmurmur.so (include/murmur.h, include/murmur_shared.h), one Python function per C entry point.
+"""ctypes binding of libmurmur.so (include/murmur.h, murmur_shared.h, murmur_draft.h), one Python function per C entry point.
 
 Argument marshalling only: every step of the decode path runs in the HIP
 kernels behind the C ABI.  Device buffers are torch tensors (or raw device
@@ -23,6 +23,8 @@ MURMUR_POL_PER_SEQ, MURMUR_POL_PER_LAYER = 1, 2
 MURMUR_DEVERR_BLOCK = 32
 MURMUR_DEVERR_POOL = 64
 MURMUR_DEVERR_PARENT, MURMUR_DEVERR_GROUP = 128, 256
+MURMUR_DEVERR_TREE = 512
+MURMUR_ROPE_PLAIN, MURMUR_ROPE_LINEAR, MURMUR_ROPE_BASE, MURMUR_ROPE_BANDS, MURMUR_ROPE_YARN = 0, 1, 2, 3, 4
 N_PIECES = 6
 SPLIT_UNIT = 128
 
@@ -50,6 +52,17 @@ class murmur_ring(ctypes.Structure):
     _fields_ = [("out_capacity", ctypes.c_int32), ("k_new", ctypes.c_void_p), ("v_new", ctypes.c_void_p)]
 
 
+class murmur_rope(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("gain", ctypes.c_float),
+                ("freq", ctypes.c_void_p)]
+
+
+class murmur_qkv(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("dtype", ctypes.c_int32),
+                ("q_layer", ctypes.c_int64), ("q_token", ctypes.c_int64), ("kv_layer", ctypes.c_int64),
+                ("kv_token", ctypes.c_int64)]
+
+
 class MurmurError(RuntimeError):
     def __init__(self, code: int, message: str):
         super().__init__(f"{_ERROR_NAMES.get(code, code)}: {message}")
@@ -63,10 +76,11 @@ _lib = None
 _PER_STEP = ("evict_compact", "evict_compact_paged", "decode_attn", "decode_step", "decode_step_static",
              "decode_step_ring", "paged_step")
 _PER_STEP_SHARED = ("paged_fork", "paged_step_shared", "paged_compact", "shared_plan", "decode_attn_shared")
+_PER_STEP_DRAFT = ("paged_reserve", "rope_append", "decode_attn_tree", "tree_accept")
 try:
     from . import _pycall
-    _pycall.structures(murmur_kv, murmur_ring)
-except (ImportError, AttributeError):  # not built, or a build of another version
+    _pycall.structures(murmur_kv, murmur_ring, murmur_rope, murmur_qkv)
+except (ImportError, AttributeError, TypeError):  # not built, or a build of another version
     _pycall = None
 
 
@@ -133,6 +147,25 @@ def _load():
     lib.murmur_decode_attn_shared.restype = ctypes.c_int
     lib.murmur_decode_attn_shared.argtypes = [vp, kvp, vp, vp, i32, i32, i32, i32, i32, i32, ctypes.c_float, vp, i32,
                                               vp, vp, sz, vp, sz, vp]
+    lib.murmur_paged_reserve_workspace.restype = ctypes.c_int
+    lib.murmur_paged_reserve_workspace.argtypes = [i32, szp]
+    lib.murmur_paged_reserve.restype = ctypes.c_int
+    lib.murmur_paged_reserve.argtypes = [vp, vp, i32, vp, i32, i32, vp, i32, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp,
+                                         sz, vp]
+    f64 = ctypes.c_double
+    lib.murmur_rope_freqs_host.restype = ctypes.c_int
+    lib.murmur_rope_freqs_host.argtypes = [i32, f64, i32, f64, f64, f64, f64, ctypes.POINTER(ctypes.c_uint64),
+                                           ctypes.POINTER(ctypes.c_float)]
+    lib.murmur_rope_append.restype = ctypes.c_int
+    lib.murmur_rope_append.argtypes = [ctypes.POINTER(murmur_rope), ctypes.POINTER(murmur_qkv), vp, vp, vp, i32, i32, i32,
+                                       i32, i32, vp, kvp, vp]
+    lib.murmur_decode_attn_tree_workspace.restype = ctypes.c_int
+    lib.murmur_decode_attn_tree_workspace.argtypes = [i32, i32, i32, i32, i32, i32, szp]
+    lib.murmur_decode_attn_tree.restype = ctypes.c_int
+    lib.murmur_decode_attn_tree.argtypes = [vp, vp, i32, vp, i32, i32, vp, kvp, vp, vp, vp, i32, i32, i32, i32, i32, i32,
+                                            i32, ctypes.c_float, vp, i32, vp, vp, sz, vp]
+    lib.murmur_tree_accept.restype = ctypes.c_int
+    lib.murmur_tree_accept.argtypes = [vp, i32, i32, vp, vp, vp, i32, vp, vp, kvp, i32, vp, vp, vp, vp]
     f64p = ctypes.POINTER(ctypes.c_double)
     lib.murmur_plan_chunks.restype = ctypes.c_int
     lib.murmur_plan_chunks.argtypes = [f64p, f64p, i32, ctypes.c_double, ctypes.c_double, ctypes.c_double, i32p,
@@ -145,7 +178,7 @@ def _load():
     lib.murmur_device_error.argtypes = [vp, i32p]
     # (C function, its address, the converter) of each per-step entry point
     lib.per_step = {n: (getattr(lib, "murmur_" + n), ctypes.cast(getattr(lib, "murmur_" + n), vp).value,
-                        getattr(_pycall, n, None)) for n in _PER_STEP + _PER_STEP_SHARED}
+                        getattr(_pycall, n, None)) for n in _PER_STEP + _PER_STEP_SHARED + _PER_STEP_DRAFT}
     _lib = lib
     return lib
 
@@ -418,6 +451,85 @@ def murmur_decode_attn_shared(q_dev, kv: murmur_kv, idx_dev, ranges_dev, max_kee
     """murmur_decode_attn, reading what the sequences of a group share once (see murmur_shared_plan)."""
     _call("decode_attn_shared", q_dev, kv, idx_dev, ranges_dev, max_keep, B, n_groups, Hq, Hkv, D, float(scale),
           out_dev, out_dtype, lse_dev, plan_dev, plan_bytes, ws_dev, ws_bytes, _stream(stream))
+
+
+def murmur_paged_reserve_workspace(B: int) -> int:
+    """Bytes of the workspace of murmur_paged_reserve."""
+    nbytes = ctypes.c_size_t(0)
+    _check(_load().murmur_paged_reserve_workspace(B, ctypes.byref(nbytes)))
+    return int(nbytes.value)
+
+
+def murmur_paged_reserve(len_dev, new_dev, B: int, block_table_dev, max_blocks: int, block_size: int, ref_dev,
+                         n_blocks: int, free_stack_dev, free_top_dev, capacity: int, per_seq: int, n_tokens: int,
+                         start_dev, got_dev, slot_dev, pos_dev, seq_dev, ws_dev, ws_bytes: int, stream=None) -> None:
+    """Blocks for new_dev[b] more tokens of every sequence, and the pool row, position and sequence of each token
+    (packed, or per_seq entries a sequence)."""
+    _call("paged_reserve", len_dev, new_dev, B, block_table_dev, max_blocks, block_size, ref_dev, n_blocks, free_stack_dev,
+          free_top_dev, capacity, per_seq, n_tokens, start_dev, got_dev, slot_dev, pos_dev, seq_dev, ws_dev, ws_bytes,
+          _stream(stream))
+
+
+def murmur_rope_freqs_host(rot_dim: int, base: float, kind: int = MURMUR_ROPE_PLAIN, factor: float = 1.0,
+                           original_len: float = 0.0, slow_turns: float = 1.0, fast_turns: float = 32.0):
+    """Host-only table of a rotation.  Returns (freq uint64 [rot_dim / 2], gain)."""
+    freq = np.zeros(max(int(rot_dim) // 2, 1), dtype=np.uint64)
+    gain = ctypes.c_float(0.0)
+    _check(_load().murmur_rope_freqs_host(int(rot_dim), float(base), int(kind), float(factor), float(original_len),
+                                          float(slow_turns), float(fast_turns),
+                                          freq.ctypes.data_as(ctypes.POINTER(ctypes.c_uint64)), ctypes.byref(gain)))
+    return freq, float(gain.value)
+
+
+def make_rope(rot_dim: int, interleaved: bool, freq_dev, gain: float = 1.0) -> murmur_rope:
+    """murmur_rope from a device table of murmur_rope_freqs_host (its tensor may be int64)."""
+    return murmur_rope(int(rot_dim), int(bool(interleaved)), float(gain), _addr(freq_dev))
+
+
+def make_qkv(q, k, v, dtype: int, q_layer: int, q_token: int, kv_layer: int, kv_token: int) -> murmur_qkv:
+    """murmur_qkv from device tensors (or addresses) and element strides of layers and tokens."""
+    return murmur_qkv(_addr(q), _addr(k), _addr(v), dtype, int(q_layer), int(q_token), int(kv_layer), int(kv_token))
+
+
+def qkv_from_tensors(q, k, v) -> murmur_qkv:
+    """murmur_qkv for bf16 or fp32 tensors shaped [NL, tokens, heads, D] whose heads are contiguous (k and v alike)."""
+    import torch
+    if q.dtype not in (torch.bfloat16, torch.float32) or k.dtype != q.dtype or v.dtype != q.dtype:
+        raise ValueError("q, k and v must all be bfloat16 or all be float32")
+    if k.shape != v.shape or k.stride() != v.stride() or any(x.stride()[2:] != (x.shape[3], 1) for x in (q, k)):
+        raise ValueError("k and v must share shape and strides, and heads be contiguous")
+    dtype = MURMUR_DTYPE_F32 if q.dtype == torch.float32 else MURMUR_DTYPE_BF16
+    return make_qkv(q, k, v, dtype, *q.stride()[:2], *k.stride()[:2])
+
+
+def murmur_rope_append(rope: murmur_rope, qkv: murmur_qkv, pos_dev, slot_dev, seq_dev, n_seqs: int, n_tokens: int, Hq: int,
+                       Hkv: int, D: int, q_out_dev, kv: murmur_kv, stream=None) -> None:
+    """q and k rotated to their positions, K and V written to the cache rows of the slot map, in one launch."""
+    _call("rope_append", rope, qkv, pos_dev, slot_dev, seq_dev, n_seqs, n_tokens, Hq, Hkv, D, q_out_dev, kv,
+          _stream(stream))
+
+
+def murmur_decode_attn_tree_workspace(n_layers: int, B: int, Hq: int, Hkv: int, n_nodes: int, max_keep: int) -> int:
+    nbytes = ctypes.c_size_t(0)
+    _check(_load().murmur_decode_attn_tree_workspace(n_layers, B, Hq, Hkv, n_nodes, max_keep, ctypes.byref(nbytes)))
+    return int(nbytes.value)
+
+
+def murmur_decode_attn_tree(seg_dev, pol_dev, pol_per_seq: int, parent_dev, parent_per_seq: int, n_nodes: int, q_dev,
+                            kv: murmur_kv, k_tree_dev, v_tree_dev, block_table_dev, max_blocks: int, block_size: int,
+                            max_keep: int, B: int, Hq: int, Hkv: int, D: int, scale: float, out_dev, out_dtype: int,
+                            lse_dev, ws_dev, ws_bytes: int, stream=None) -> None:
+    """Attention of every node of every sequence's tree over the retained cache, its ancestors and itself."""
+    _call("decode_attn_tree", seg_dev, pol_dev, pol_per_seq, parent_dev, parent_per_seq, n_nodes, q_dev, kv, k_tree_dev,
+          v_tree_dev, block_table_dev, max_blocks, block_size, max_keep, B, Hq, Hkv, D, float(scale), out_dev, out_dtype,
+          lse_dev, ws_dev, ws_bytes, _stream(stream))
+
+
+def murmur_tree_accept(parent_dev, parent_per_seq: int, n_nodes: int, token_dev, next_dev, slot_dev, B: int, k_tree_dev,
+                       v_tree_dev, kv: murmur_kv, Hkv: int, path_dev, count_dev, last_dev, stream=None) -> None:
+    """The path that the decoder agrees with, its K and V into the cache rows of slot_dev."""
+    _call("tree_accept", parent_dev, parent_per_seq, n_nodes, token_dev, next_dev, slot_dev, B, k_tree_dev, v_tree_dev, kv,
+          Hkv, path_dev, count_dev, last_dev, _stream(stream))
 
 
 def murmur_plan_chunks(seg_start, seg_end, audio_len: float, max_chunk: float = 300.0,
