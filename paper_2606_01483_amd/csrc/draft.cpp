@@ -75,18 +75,19 @@ int check_tree_sizes(int32_t n_layers, int32_t B, int32_t Hq, int32_t Hkv, int32
 
 }  // namespace
 
-// The rows of a workgroup are as many as the tree has, up to 128; where the (layer,
+// The rows of a workgroup are as many as the tree has, up to 256; where the (layer,
 // sequence, KV head) groups do not fill the chip, their lists are cut into splits.
 TreePlan tree_plan(int32_t n_layers, int32_t B, int32_t Hq, int32_t Hkv, int32_t n_nodes, int32_t max_keep) {
     TreePlan p{};
     const int64_t rows = (int64_t)n_nodes * (Hq / Hkv), groups = (int64_t)n_layers * B * Hkv;
-    const int per_wg = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
-    p.shape = rows <= 16 ? kTree16 : rows <= 32 ? kTree32 : rows <= 64 ? kTree64 : kTree128;
+    const int64_t passes = ((int64_t)max_keep + kWaveTile - 1) / kWaveTile;
+    p.shape = rows <= 16 ? kTreeFew : groups * ((rows + 255) / 256) > kRoundWorkgroups / 2 ? kTreePair : kTreeWide;
+    const int per_wg = p.shape == kTreeWide ? 256 : 128;
     p.row_sets = (int32_t)((rows + per_wg - 1) / per_wg);
-    const int64_t passes = ((int64_t)max_keep + kWaveTile - 1) / kWaveTile, wgs = groups * p.row_sets;
-    const int64_t want = std::max<int64_t>(1, 2 * kRoundWorkgroups / wgs);
-    const int64_t least = p.shape <= kTree32 ? 4 : p.shape == kTree64 ? 4 : 4;  // passes of a split
-    p.n_split = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, 64), passes / least));
+    const int64_t slots = p.shape == kTreePair ? 2 * kRoundWorkgroups : kRoundWorkgroups;
+    const int64_t want = std::max<int64_t>(1, slots / (groups * p.row_sets));
+    p.n_split = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, 64), passes / 4));
+    if (passes <= 8) p.n_split = 1;
     p.units = groups * p.n_split;
     if (p.n_split > 1) {
         p.o_bytes = (size_t)p.units * (size_t)rows * kHeadDim * sizeof(float);

@@ -345,7 +345,7 @@ struct AcceptLaunch {
 int launch_tree_accept(const AcceptLaunch &p, murmur_stream_t stream);
 
 constexpr int kMaxNodes = 64;
-enum TreeShape : int32_t { kTree16, kTree32, kTree64, kTree128 };  // query rows of a workgroup
+enum TreeShape : int32_t { kTreeFew, kTreeWide, kTreePair };  // workgroups of 8 wavefronts and 128 or 256 rows, of 4 and 128
 struct TreePlan {
     TreeShape shape;
     int32_t n_split, row_sets;

@@ -133,53 +133,67 @@ static __device__ __forceinline__ TreeList tree_list(const murmur_seg &s, const 
     return l;
 }
 
-// Whether rank r of the list is one that a row attends to.
-static __device__ __forceinline__ bool tree_allows(const TreeList &l, const TreeRule &x, int r) {
-    const int n = r - l.n0;
-    const uint32_t bits = n < 32 ? x.lo >> (n & 31) : x.hi >> (n & 31);
-    return r < l.count && (uint32_t)(r - l.a0) >= (uint32_t)x.a && (uint32_t)(l.b1 - 1 - r) >= (uint32_t)x.b &&
-           (uint32_t)(r - l.c0) >= (uint32_t)x.c && (n < 0 || (bits & 1u));
+// The ranks r0 .. r0 + 31 that a row attends to, a bit each.
+static __device__ __forceinline__ uint32_t tree_allows(const TreeList &l, const TreeRule &x, int r0) {
+    const auto below = [](int n) { return (uint32_t)((1ull << min(max(n, 0), 32)) - 1); };  // ranks before r0 + n
+    const auto stretch = [&](int from, int to) { return below(to - r0) & ~below(from - r0); };
+    const uint32_t out = stretch(l.a0, l.a0 + x.a) | stretch(l.b1 - x.b, l.b1) | stretch(l.c0, l.c0 + x.c);
+    const uint64_t nodes = (uint64_t)x.hi << 32 | x.lo;
+    const int n = r0 - l.n0;
+    // bits of nodes past the last are clear, which masks the list's end too
+    const uint32_t in = n >= 0 ? (n < 64 ? (uint32_t)(nodes >> n) : 0u) : (uint32_t)(nodes << min(-n, 63)) | below(-n);
+    return in & ~out;
 }
 
-// Where ranks lie: the cache rows of a (layer, KV head) of a sequence, and the nodes.
-// kRows rows of a pass for each lane; a row is one of the cache (>= 0) or ~node, and
-// ~0, the root's, wherever none is to be read.
-template <int kRows>
+// Rows of a pass for each lane: kTreeRows ranks four apart, as cache rows (>= 0) or
+// ~node; ~0, the root's, wherever none is to be read.
+constexpr int kTreeRows = 4;  // of a lane in a half pass of 16 rows
 struct TreeRows {
-    int32_t pos[kRows], entry[kRows];
+    int32_t pos[kTreeRows], entry[kTreeRows];
     // positions, and the block table's entries on their way
-    __device__ __forceinline__ void begin(const TreeList &l, const int32_t *bt_row, int32_t max_blocks, int32_t log2_bs,
-                                          int r0) {
+    __device__ __forceinline__ void begin(const TreeList &l, const TreeLaunch &a, const int32_t *bt_row, int r0, int c4) {
+        int p0;
+        if (r0 + 16 <= l.n0 && tab_run(l.tab, r0, 16, 0x7fffffff, p0)) {  // consecutive positions (uniform)
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const int r = r0 + 4 * i;
-            int piece;
-            const int p = tab_pos(l.tab, r, piece);
-            pos[i] = r < l.n0 ? p : (r < l.count ? ~(r - l.n0) : ~0);
-            if (bt_row) entry[i] = bt_row[pos[i] < 0 ? 0 : min(pos[i] >> log2_bs, max_blocks - 1)];  // uniform
+            for (int i = 0; i < kTreeRows; ++i) pos[i] = p0 + 4 * i + c4;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kTreeRows; ++i) {
+                const int r = r0 + 4 * i + c4;
+                int piece;
+                const int p = tab_pos(l.tab, r, piece);
+                pos[i] = r < l.n0 ? p : (r < l.count ? ~(r - l.n0) : ~0);
+            }
+        }
+        if (bt_row) {  // uniform
+#pragma unroll
+            for (int i = 0; i < kTreeRows; ++i) entry[i] = bt_row[min(max(pos[i], 0) >> a.log2_bs, a.max_blocks - 1)];
         }
     }
-    __device__ __forceinline__ void finish(const int32_t *bt_row, int32_t max_blocks, int32_t log2_bs, int32_t max_len,
-                                           int &err) {
+    // cache rows; a position that has none is an error and becomes the root's row
+    __device__ __forceinline__ void finish(const TreeLaunch &a, const int32_t *bt_row, int &err) {
+        const uint32_t last = (uint32_t)(a.max_len - 1), last_block = last >> a.log2_bs, in_block = (1u << a.log2_bs) - 1;
+        uint32_t row[kTreeRows];
+        bool wrong[kTreeRows], any = false;
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            if (pos[i] < 0) continue;
-            int64_t row = pos[i];
+        for (int i = 0; i < kTreeRows; ++i) {
+            row[i] = (uint32_t)pos[i];
+            wrong[i] = false;
             if (bt_row) {
-                const bool blocked = entry[i] < 0 || (pos[i] >> log2_bs) >= max_blocks;
-                row = ((int64_t)entry[i] << log2_bs) | (pos[i] & ((1 << log2_bs) - 1));
-                if (blocked) {
-                    err |= MURMUR_DEVERR_BLOCK;
-                    pos[i] = ~0;
-                    continue;
-                }
+                row[i] = (uint32_t)entry[i] << a.log2_bs | (row[i] & in_block);
+                wrong[i] = ((uint32_t)entry[i] > last_block) | (pos[i] >> a.log2_bs >= a.max_blocks);
             }
-            if (row >= max_len) {
-                err |= MURMUR_DEVERR_POSITION;
-                row = ~0;
-            }
-            pos[i] = (int32_t)row;
+            wrong[i] = (wrong[i] | (row[i] > last)) & (pos[i] >= 0);
+            any |= wrong[i];
         }
+        if (__builtin_expect(__ballot(any) != 0, 0)) {
+#pragma unroll
+            for (int i = 0; i < kTreeRows; ++i)
+                if (wrong[i])
+                    err |= bt_row && (entry[i] < 0 || pos[i] >> a.log2_bs >= a.max_blocks) ? MURMUR_DEVERR_BLOCK : MURMUR_DEVERR_POSITION;
+        }
+#pragma unroll
+        for (int i = 0; i < kTreeRows; ++i) pos[i] = wrong[i] ? ~0 : (pos[i] >= 0 ? (int32_t)row[i] : pos[i]);
     }
 };
 
@@ -188,8 +202,8 @@ struct TreeRows {
 // to the sums of the rows that attend to them, whose result is not finite there
 // whatever their weights, and taken out of the operands.
 template <int kTiles>
-static __device__ __forceinline__ void tree_keep_apart(u32x2 (&vf)[16], const uint8_t *tile, int r0, const TreeList &l,
-                                                       const TreeRule (&rule)[kTiles], WaveAcc (&w)[kTiles], int lane) {
+static __device__ __forceinline__ void tree_keep_apart(u32x2 (&vf)[16], const uint8_t *tile, const uint32_t (&allows)[kTiles],
+                                                       WaveAcc (&w)[kTiles], int lane) {
     const int c4 = lane >> 4;
     f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -208,7 +222,7 @@ static __device__ __forceinline__ void tree_keep_apart(u32x2 (&vf)[16], const ui
             for (int i = 0; i < 2; ++i) e[i] &= not_finite(e[i]);
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
-                const bool mine = tree_allows(l, rule[t], r0 + r);
+                const bool mine = allows[t] >> r & 1;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     w[t].acc[db][2 * i] += mine ? __builtin_bit_cast(float, e[i] << 16) : 0.f;
@@ -235,52 +249,51 @@ static __device__ __forceinline__ void tree_store(const TreeLaunch &a, int64_t r
 }
 
 // ---------------------------------------------------------------------------
-// Workgroup: kWays * kTiles * 16 query rows of one (layer, sequence, KV head) over one
-// split of the list.  Its four wavefronts are kWays ways by rows and 4 / kWays groups
-// by passes: the wavefronts of a group share the K and V rows of a pass, which they
-// load together into one of the group's two stages while they compute the other.
+// Workgroup: up to kWaves * kTiles * 16 query rows of one (layer, sequence, KV head)
+// over one split of the list.  Its wavefronts take the list kWaves / 2 passes (a round)
+// at a time: together they load a round's rows into one of two buffers while they
+// compute the other, and a split of two rounds is on its way as a whole from the
+// start.  They are `ways` ways by rows and the rest by passes, as the rows that are
+// there ask for; groups by passes are joined by way of LDS at the end.
 // ---------------------------------------------------------------------------
-constexpr int kTreeThreads = 256;
-template <int kWays>
+template <int kWaves>
 struct TreeLds {
-    static constexpr int kGroups = 4 / kWays;
-    uint8_t stages[kGroups][2][kStageBytes];
+    uint8_t stages[2][kWaves / 2][kStageBytes];
     TreeRule rule[64];
-    float ml[4][32][2];
+    float ml[kWaves][32][2];
     int err;
 };
 
-template <int kTerms, int kTiles, int kWays>
-__global__ __launch_bounds__(kTreeThreads, 2) void tree_attn_kernel(const TreeLaunch a) {
-    constexpr int kGroups = 4 / kWays, kRows = 8 / kWays, kAll = kWays * kTiles * 16;
-    __shared__ __attribute__((aligned(16))) TreeLds<kWays> lds;
+template <int kTerms, int kTiles, int kWaves>
+__global__ __launch_bounds__(kWaves * 64, 2) void tree_attn_kernel(const TreeLaunch a) {
+    constexpr int kAll = kWaves * kTiles * 16, kThreads = kWaves * 64, kRound = kWaves / 2;
+    static_assert(kTiles <= 2, "two tiles of LDS a wavefront");
+    __shared__ __attribute__((aligned(16))) TreeLds<kWaves> lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int way = wave % kWays, grp = wave / kWays, n16 = lane & 15, c4 = lane >> 4;
-    // the workgroups of one split's row sets follow each other on one XCD
-    const int x = blockIdx.x, set = (x >> 3) % a.row_sets, unit = (x >> 3) / a.row_sets * 8 + (x & 7);
+    const int n16 = lane & 15, c4 = lane >> 4;
+    // The workgroups of one split's row sets follow each other on one XCD.  An XCD's go to its shader engines in turn,
+    // so the sets start with another one for every split: otherwise (with as many sets as engines) one engine has every
+    // first set, and another every last one, where trees of few nodes have no rows.
+    const int x = blockIdx.x, eight = (x >> 3) / a.row_sets;
+    const int set = ((x >> 3) - eight * a.row_sets + eight) % a.row_sets, unit = eight * 8 + (x & 7);
     if (unit >= a.units) return;
     const int split = unit % a.n_split, group = unit / a.n_split;
     const int g = group % a.Hkv, lb = group / a.Hkv, b = lb % a.B, layer = lb / a.B;
     const murmur_seg s = reinterpret_cast<const murmur_seg *>(a.seg)[b];
-    if (layout_absent(s.prompt_pre, s.speech_len, s.prompt_mid, s.out_len)) return;
     const int rec = ((a.pol_mode & MURMUR_POL_PER_LAYER) ? layer * ((a.pol_mode & MURMUR_POL_PER_SEQ) ? a.B : 1) : 0) +
                     ((a.pol_mode & MURMUR_POL_PER_SEQ) ? b : 0);
     const murmur_policy p = reinterpret_cast<const murmur_policy *>(a.pol)[rec];
     TreeRule mine{};
     const TreeList l = tree_list(s, p, a.parent + (a.parent_per_seq ? (int64_t)b * a.T : 0), a.T, lane, mine);
-    const int row0 = set * kAll;
-    if (row0 >= l.live * a.G) return;
-    if (wave == 0) lds.rule[lane] = mine;
-    if (tid == 0) {
-        lds.err = l.err;
-        if (l.err) raise_device_error(l.err);
-    }
-    __syncthreads();
-
+    if (layout_absent(s.prompt_pre, s.speech_len, s.prompt_mid, s.out_len)) return;
+    const int row0 = set * kAll, rows_live = l.live * a.G;
+    if (row0 >= rows_live) return;
+    const int wanted = (min(rows_live - row0, kAll) + 16 * kTiles - 1) / (16 * kTiles);
+    const int ways = wanted <= 1 ? 1 : wanted <= 2 ? 2 : wanted <= 4 ? 4 : 8, groups = min(kWaves / ways, kRound);
+    const int way = wave & (ways - 1), grp = wave / ways;
     // the lane's row of every tile
     int node[kTiles], row[kTiles];
     u32x4 qf[kTiles][4];
-    float scale = 1.f;
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
         row[t] = row0 + (way * kTiles + t) * 16 + n16;
@@ -290,93 +303,100 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_attn_kernel(const TreeLa
 #pragma unroll
         for (int kc = 0; kc < 4; ++kc) qf[t][kc] = load16(q + 32 * kc);
     }
-    WaveAcc w[kTiles];
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-        scale = signed_scale(qf[t], a.scale_log2);
-        start_rows(w[t]);
-    }
     const int passes = l.err ? 0 : (l.count + kWaveTile - 1) / kWaveTile;
     const int p0 = (int)((int64_t)passes * split / a.n_split), p1 = (int)((int64_t)passes * (split + 1) / a.n_split);
-    const int rounds = (p1 - p0 + kGroups - 1) / kGroups;
+    const int rounds = (p1 - p0 + kRound - 1) / kRound;
     const int32_t *bt_row = a.bt ? a.bt + (int64_t)b * a.max_blocks : nullptr;
-    const uint16_t *kc = a.k + layer * a.s_layer + b * a.s_b + g * a.s_h, *vc = a.v + layer * a.s_layer + b * a.s_b + g * a.s_h;
+    const int64_t cache_at = layer * a.s_layer + b * a.s_b + g * a.s_h;
+    const uint16_t *kc = a.k + cache_at, *vc = a.v + cache_at;
     const int64_t tree_at = ((int64_t)lb * a.T * a.Hkv + g) * kHeadDim;
-    const int first = way * kRows;  // of the eight loads of a tile this wavefront has [first, first + kRows)
+    // this wavefront loads the half `wave & 1` of a round's pass `wave >> 1`
+    const int half = wave & 1, chunk = 8 * (n16 ^ c4);
     int err = 0;
-    TreeRows<kRows> rows;
-    const auto pass_of = [&](int it) { return p0 + it * kGroups + grp; };
-    const auto begin = [&](int it) {
-        rows.begin(l, bt_row, a.max_blocks, a.log2_bs, pass_of(it) * kWaveTile + 4 * first + c4);
-    };
-    const auto load = [&](int it) {
-        rows.finish(bt_row, a.max_blocks, a.log2_bs, a.max_len, err);
-        uint8_t *stage = lds.stages[grp][it & 1];
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const int j = first + i, c = n16 ^ ((4 * j + c4) & 15);
-            const bool is_node = rows.pos[i] < 0;
-            const int64_t at = (is_node ? tree_at + (int64_t)~rows.pos[i] * a.Hkv * kHeadDim : rows.pos[i] * a.s_pos) + 8 * c;
-            __builtin_amdgcn_global_load_lds((is_node ? a.k_tree : kc) + at, (lds_void_t *)(stage + j * 1024), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((is_node ? a.v_tree : vc) + at, (lds_void_t *)(stage + kTileBytes + j * 1024), 16, 0, 0);
-        }
-    };
-    if (rounds > 0) {
-        begin(0);
-        load(0);
-        begin(1);
+    TreeRows rows;
+    const auto mine_in = [&](int it) { return p0 + it * kRound + (wave >> 1) < p1; };
+    if (wave == 0) lds.rule[lane] = mine;
+    if (tid == 0) {
+        lds.err = l.err;
+        if (l.err) raise_device_error(l.err);
     }
+    float scale = 1.f;  // of the softmax, set with the queries' sign before the first pass
+    WaveAcc w[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) start_rows(w[t]);
+    const bool idle = grp >= groups || row0 + way * kTiles * 16 >= rows_live;  // uniform: a wavefront without rows
+    // Step `it` looks up the rows of round it + 2, loads round it + 1 and computes round it, so that there is one copy
+    // of each part's code: fetching it costs a short launch more than running it.
 #pragma unroll 1
-    for (int it = 0; it < rounds; ++it) {
-        wait_vm<0>();
-        __syncthreads();  // the group's rows are in, and its other stage is read
-        if (it + 1 < rounds) {
-            load(it + 1);
-            begin(it + 2);
+    for (int it = -2; it < rounds; ++it) {
+        if (it >= 0) {
+            wait_vm<0>();
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // the round's rows are in, and the other buffer is read
         }
-        const int r0 = pass_of(it) * kWaveTile;
-        if (pass_of(it) >= p1) continue;  // uniform: the last round of a group without one
-        const uint32_t kt = lds_addr(lds.stages[grp][it & 1]), vt = kt + kTileBytes;
-        u32x4 kf[8];
-        read_k_operands(kf, kt, n16, c4);
-        const int r1 = r0 + kWaveTile;
-        const bool ruled = r1 > l.n0 || (r1 > l.a0 && r0 < l.a0 + l.a_most) || (r1 > l.b1 - l.b_most && r0 < l.b1) ||
-                           (r1 > l.c0 && r0 < l.c0 + l.c_most);
-        u32x4 pr[kTiles][kTerms];
-        TreeRule rule[kTiles];
-        if (ruled) {
+        if (it >= -1 && mine_in(it + 1)) {
+            rows.finish(a, bt_row, err);
+            uint8_t *stage = lds.stages[(it + 1) & 1][wave >> 1] + 4096 * half;
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) rule[t] = lds.rule[node[t]];
-        }
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-            f32x4 sc[2];
-#pragma unroll
-            for (int blk = 0; blk < 2; ++blk) {
-                sc[blk] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int kk = 0; kk < 4; ++kk) sc[blk] = mfma16x16x32(kf[4 * blk + kk], qf[t][kk], sc[blk]);
+            for (int i = 0; i < kTreeRows; ++i) {
+                const bool node_row = rows.pos[i] < 0;
+                const int64_t at = (node_row ? tree_at + (int64_t)~rows.pos[i] * (a.Hkv * kHeadDim) : rows.pos[i] * a.s_pos) + (chunk ^ 32 * i);
+                __builtin_amdgcn_global_load_lds((node_row ? a.k_tree : kc) + at, (lds_void_t *)(stage + i * 1024), 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((node_row ? a.v_tree : vc) + at, (lds_void_t *)(stage + kTileBytes + i * 1024), 16, 0, 0);
             }
-            if (ruled) {
-                asm volatile("");  // a branch, which few passes take
-#pragma unroll
-                for (int blk = 0; blk < 2; ++blk)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        sc[blk][i] = tree_allows(l, rule[t], r0 + 16 * blk + 4 * c4 + i) ? sc[blk][i] : kNegInf;
-            }
-            softmax_pass<kTerms>(sc, kWaveTile, scale, w[t], c4, pr[t]);
         }
-        u32x2 vf[16];
-        read_v_operands(vf, vt, n16, c4);
-        if (ruled) tree_keep_apart<kTiles>(vf, lds.stages[grp][it & 1] + kTileBytes, r0, l, rule, w, lane);
+        if (mine_in(it + 2)) rows.begin(l, a, bt_row, (p0 + (it + 2) * kRound + (wave >> 1)) * kWaveTile + 16 * half, c4);
+        if (it < 0) continue;
+        if (it == 0) {
 #pragma unroll
-        for (int db = 0; db < 8; ++db) {
-            const u32x4 av = u32x4{vf[2 * db][0], vf[2 * db][1], vf[2 * db + 1][0], vf[2 * db + 1][1]};
+            for (int t = 0; t < kTiles; ++t) scale = signed_scale(qf[t], a.scale_log2);
+        }
+        if (idle) continue;
+#pragma unroll 1
+        for (int i = grp; i < kRound; i += groups) {
+            const int pass = p0 + it * kRound + i, r0 = pass * kWaveTile;
+            if (pass >= p1) break;
+            const uint8_t *stage = lds.stages[it & 1][i];
+            u32x4 kf[8];
+            read_k_operands(kf, lds_addr(stage), n16, c4);
+            const int r1 = r0 + kWaveTile;
+            const bool ruled = r1 > l.n0 || (r1 > l.a0 && r0 < l.a0 + l.a_most) || (r1 > l.b1 - l.b_most && r0 < l.b1) ||
+                               (r1 > l.c0 && r0 < l.c0 + l.c_most);
+            u32x4 pr[kTiles][kTerms];
+            uint32_t allows[kTiles];
+            f32x4 sc[kTiles][2];
 #pragma unroll
             for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-                for (int k = 0; k < kTerms; ++k) w[t].acc[db] = mfma16x16x32(av, pr[t][k], w[t].acc[db]);
+                for (int blk = 0; blk < 2; ++blk) {
+                    sc[t][blk] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk) sc[t][blk] = mfma16x16x32(kf[4 * blk + kk], qf[t][kk], sc[t][blk]);
+                }
+            if (ruled) {
+                asm volatile("");  // a branch, which few passes take
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+                    allows[t] = tree_allows(l, lds.rule[node[t]], r0);
+                    const uint32_t mine = allows[t] >> (4 * c4);
+#pragma unroll
+                    for (int blk = 0; blk < 2; ++blk)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sc[t][blk][e] = mine & (1u << (16 * blk + e)) ? sc[t][blk][e] : kNegInf;
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) softmax_pass<kTerms>(sc[t], kWaveTile, scale, w[t], c4, pr[t]);
+            u32x2 vf[16];
+            read_v_operands(vf, lds_addr(stage + kTileBytes), n16, c4);
+            if (ruled) tree_keep_apart<kTiles>(vf, stage + kTileBytes, allows, w, lane);
+#pragma unroll
+            for (int k = 0; k < kTerms; ++k)  // a sum's products apart, since each waits for the one before
+#pragma unroll
+                for (int db = 0; db < 8; ++db)
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t)
+                        w[t].acc[db] = mfma16x16x32(u32x4{vf[2 * db][0], vf[2 * db][1], vf[2 * db + 1][0], vf[2 * db + 1][1]},
+                                                    pr[t][k], w[t].acc[db]);
         }
     }
     if (__ballot(err != 0)) {
@@ -390,8 +410,11 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_attn_kernel(const TreeLa
 
     // Rows to the outputs, or to the split's partials
     const auto put = [&](int r, int c, f32x4 O, float M, float L) {
-        if (r >= l.live * a.G) return;
-        if (bad) L = __builtin_nanf("");
+        if (r >= rows_live) return;
+        if (bad) {
+            M = 0.f;
+            L = __builtin_nanf("");
+        }
         if (a.n_split > 1) {
             const int64_t at = ((int64_t)group * a.n_split + split) * (a.T * a.G) + r;
             *reinterpret_cast<f32x4 *>(a.part_o + at * kHeadDim + 4 * c) = O;
@@ -401,94 +424,142 @@ __global__ __launch_bounds__(kTreeThreads, 2) void tree_attn_kernel(const TreeLa
             if (l.there >> n & 1) tree_store(a, ((int64_t)lb * a.T + n) * a.Hq + g * a.G + r - n * a.G, c, O, M, L);
         }
     };
-    if constexpr (kGroups == 1) {
+    if (groups == 1) {
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
             const float sum = sum_over_c4(w[t].l_run);
 #pragma unroll
             for (int db = 0; db < 8; ++db) put(row[t], 4 * db + c4, w[t].acc[db], w[t].m_run * scale, sum);
         }
-    } else {
-        // the groups' states by way of LDS, two tiles of every wavefront at a time
-        float *o = reinterpret_cast<float *>(&lds.stages[0][0][0]) + wave * 32 * kHeadDim;
-        static_assert(sizeof(lds.stages) >= 4 * 32 * kHeadDim * sizeof(float), "two tiles of each wavefront");
+        return;
+    }
+    // the groups' states by way of the buffers
+    float *all = reinterpret_cast<float *>(&lds.stages[0][0][0]), *o = all + wave * kTiles * 16 * kHeadDim;
+    static_assert(sizeof(lds.stages) >= kWaves * 32 * kHeadDim * sizeof(float), "two tiles of each wavefront");
 #pragma unroll
-        for (int t0 = 0; t0 < kTiles; t0 += 2) {
-            if (t0 > 0) __syncthreads();
+    for (int t = 0; t < kTiles; ++t) {
+        const float sum = sum_over_c4(w[t].l_run);
+        const int r = 16 * t + n16;
+        if (c4 == 0) *reinterpret_cast<float2 *>(&lds.ml[wave][r][0]) = float2{w[t].m_run * scale, sum};
 #pragma unroll
-            for (int t = t0; t < t0 + 2 && t < kTiles; ++t) {
-                const float sum = sum_over_c4(w[t].l_run);
-                const int r = 16 * (t - t0) + n16;
-                if (c4 == 0) *reinterpret_cast<float2 *>(&lds.ml[wave][r][0]) = float2{w[t].m_run * scale, sum};
+        for (int db = 0; db < 8; ++db)
+            *reinterpret_cast<f32x4 *>(&o[r * kHeadDim + 4 * ((4 * db + c4) ^ (r & 7))]) = w[t].acc[db];
+    }
+    __syncthreads();
+    constexpr int kRows = 16 * kTiles;  // of a way
+#pragma unroll 1
+    for (int i = tid; i < ways * kRows * 32; i += kThreads) {
+        const int c = i & 31, wy = (i >> 5) / kRows, r = (i >> 5) % kRows;
+        if (row0 + wy * kRows + r >= rows_live) continue;
+        float m[kRound], sum[kRound];
+        f32x4 part[kRound];
 #pragma unroll
-                for (int db = 0; db < 8; ++db)
-                    *reinterpret_cast<f32x4 *>(&o[r * kHeadDim + 4 * ((4 * db + c4) ^ (r & 7))]) = w[t].acc[db];
-            }
-            __syncthreads();
-            const int n = min(2, kTiles - t0) * 16;  // rows of a way in this turn
-            for (int i = tid; i < kWays * n * 32; i += kTreeThreads) {
-                const int c = i & 31, wy = (i >> 5) / n, r = (i >> 5) % n;
-                float M = kNegInf, L = 0.f;
-#pragma unroll
-                for (int e = 0; e < kGroups; ++e) M = fmaxf(M, lds.ml[e * kWays + wy][r][0]);
-                f32x4 O = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int e = 0; e < kGroups; ++e) {
-                    const int wv = e * kWays + wy;
-                    const float m = lds.ml[wv][r][0], f = m == kNegInf ? 0.f : __builtin_amdgcn_exp2f(m - M);
-                    const f32x4 part = *reinterpret_cast<const f32x4 *>(
-                        reinterpret_cast<const float *>(&lds.stages[0][0][0]) + (wv * 32 + r) * kHeadDim + 4 * (c ^ (r & 7)));
-                    L += lds.ml[wv][r][1] * f;
-                    O += f * part;
-                }
-                put(row0 + (wy * kTiles + t0) * 16 + r, c, O, M, L);
-            }
+        for (int e = 0; e < kRound; ++e) {  // behind the last group: the first one again, which weighs nothing
+            const int wv = (e < groups ? e : 0) * ways + wy;
+            const float2 ml = *reinterpret_cast<const float2 *>(&lds.ml[wv][r][0]);
+            m[e] = ml.x;
+            sum[e] = ml.y;
+            part[e] = *reinterpret_cast<const f32x4 *>(all + (wv * kRows + r) * kHeadDim + 4 * (c ^ (r & 7)));
         }
+        float M = m[0], L = 0.f;
+#pragma unroll
+        for (int e = 1; e < kRound; ++e) M = fmaxf(M, m[e]);
+        f32x4 O = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < kRound; ++e) {
+            const float f = e >= groups || m[e] == kNegInf ? 0.f : __builtin_amdgcn_exp2f(m[e] - M);
+            L += e < groups ? sum[e] * f : 0.f;
+            O += e < groups ? f * part[e] : f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        put(row0 + wy * kRows + r, c, O, M, L);
     }
 }
 
-// A row by 32 threads, four head dims each.
+// A row by 32 threads, four head dims each, kParts times: each takes every kParts-th
+// split.
+template <int kParts>
 __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeLaunch a) {
-    const int rows = a.T * a.G;
-    const int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const int c = threadIdx.x & 31;
-    if (at >= (int64_t)a.NL * a.B * a.Hkv * rows) return;
+    constexpr int kRows = 8 / kParts, kBatch = 8;
+    __shared__ f32x4 s_o[kParts > 1 ? 8 : 1][32];
+    __shared__ float2 s_ml[8];
+    const int rows = a.T * a.G, slice = threadIdx.x >> 5, c = threadIdx.x & 31;
+    const int part = slice / kRows;
+    const int64_t at = (int64_t)blockIdx.x * kRows + slice % kRows;
     const int64_t group = at / rows;
     const int r = (int)(at - group * rows), n = (int)((uint32_t)r * a.magic_g >> 16);
     const int64_t lb = group / a.Hkv;
     const int g = (int)(group - lb * a.Hkv), b = (int)(lb % a.B);
-    const murmur_seg s = reinterpret_cast<const murmur_seg *>(a.seg)[b];
-    if (layout_absent(s.prompt_pre, s.speech_len, s.prompt_mid, s.out_len)) return;
-    if (a.parent[(a.parent_per_seq ? (int64_t)b * a.T : 0) + n] == -2) return;
-    const int64_t part0 = group * a.n_split * rows + r;
-    float M = kNegInf, L = 0.f;
-    for (int i = 0; i < a.n_split; ++i) M = fmaxf(M, a.part_ml[2 * (part0 + (int64_t)i * rows)]);
-    f32x4 O = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int i = 0; i < a.n_split; ++i) {
-        const int64_t p = part0 + (int64_t)i * rows;
-        const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * p);
-        const f32x4 part = *reinterpret_cast<const f32x4 *>(a.part_o + p * kHeadDim + 4 * c);
-        const float f = ml.x == kNegInf ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
-        L += ml.y * f;
-        O += f * part;
+    const bool in = at < (int64_t)a.NL * a.B * a.Hkv * rows;
+    bool there = false;
+    if (in) {
+        const murmur_seg s = reinterpret_cast<const murmur_seg *>(a.seg)[b];
+        there = !layout_absent(s.prompt_pre, s.speech_len, s.prompt_mid, s.out_len) &&
+                a.parent[(a.parent_per_seq ? (int64_t)b * a.T : 0) + n] != -2;
     }
-    tree_store(a, (lb * a.T + n) * a.Hq + g * a.G + r - n * a.G, c, O, M, L);
+    float M = kNegInf, L = 0.f;
+    f32x4 O = {0.f, 0.f, 0.f, 0.f};
+    if (there) {
+        const int64_t part0 = group * a.n_split * rows + r;
+        for (int i0 = part; i0 < a.n_split; i0 += kBatch * kParts) {
+            float2 ml[kBatch];
+            f32x4 o[kBatch];
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {  // behind the last split: the last one again, which weighs nothing
+                const int64_t p = part0 + (int64_t)min(i0 + j * kParts, a.n_split - 1) * rows;
+                ml[j] = *reinterpret_cast<const float2 *>(a.part_ml + 2 * p);
+                o[j] = *reinterpret_cast<const f32x4 *>(a.part_o + p * kHeadDim + 4 * c);
+            }
+            float m = M;
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) m = fmaxf(m, ml[j].x);
+            const float f0 = M == kNegInf ? 0.f : __builtin_amdgcn_exp2f(M - m);
+            L *= f0;
+            O *= f0;
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                const bool counts = i0 + j * kParts < a.n_split && ml[j].x != kNegInf;
+                const float f = counts ? __builtin_amdgcn_exp2f(ml[j].x - m) : 0.f;
+                L += counts ? ml[j].y * f : 0.f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) O[e] += counts ? o[j][e] * f : 0.f;
+            }
+            M = m;
+        }
+    }
+    if constexpr (kParts > 1) {
+        s_o[slice][c] = O;
+        if (c == 0) s_ml[slice] = float2{M, L};
+        __syncthreads();
+        if (part > 0) return;
+        float m = kNegInf;
+#pragma unroll
+        for (int e = 0; e < kParts; ++e) m = fmaxf(m, s_ml[e * kRows + slice].x);
+        L = 0.f;
+        O = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < kParts; ++e) {
+            const float2 ml = s_ml[e * kRows + slice];
+            const float f = ml.x == kNegInf ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
+            L += ml.y * f;
+            O += f * s_o[e * kRows + slice][c];
+        }
+        M = m;
+    }
+    if (there) tree_store(a, (lb * a.T + n) * a.Hq + g * a.G + r - n * a.G, c, O, M, L);
 }
 
-template <int kTerms, int kTiles, int kWays>
+template <int kTerms, int kTiles, int kWaves>
 static int launch_tree_as(const TreeLaunch &a, hipStream_t stream) {
     const unsigned grid = (unsigned)((a.units + 7) / 8 * 8 * a.row_sets);
-    hipLaunchKernelGGL((tree_attn_kernel<kTerms, kTiles, kWays>), dim3(grid), dim3(kTreeThreads), 0, stream, a);
+    hipLaunchKernelGGL((tree_attn_kernel<kTerms, kTiles, kWaves>), dim3(grid), dim3(kWaves * 64), 0, stream, a);
     return (int)hipGetLastError();
 }
 
 template <int kTerms>
 static int launch_tree(const TreeLaunch &a, hipStream_t stream) {
     switch (a.shape) {
-        case kTree16: return launch_tree_as<kTerms, 1, 1>(a, stream);
-        case kTree32: return launch_tree_as<kTerms, 2, 1>(a, stream);
-        case kTree64: return launch_tree_as<kTerms, 2, 2>(a, stream);
+        case kTreeFew: return launch_tree_as<kTerms, 1, 8>(a, stream);
+        case kTreeWide: return launch_tree_as<kTerms, 2, 8>(a, stream);
         default: return launch_tree_as<kTerms, 2, 4>(a, stream);
     }
 }
@@ -497,7 +568,10 @@ int launch_decode_attn_tree(const TreeLaunch &a, murmur_stream_t stream) {
     const int e = a.out_f32 ? launch_tree<3>(a, (hipStream_t)stream) : launch_tree<2>(a, (hipStream_t)stream);
     if (e != 0 || a.n_split == 1) return e;
     const int64_t rows = (int64_t)a.NL * a.B * a.Hkv * a.T * a.G;
-    hipLaunchKernelGGL(tree_merge_kernel, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, (hipStream_t)stream, a);
+    if (a.n_split <= 8)
+        hipLaunchKernelGGL(tree_merge_kernel<1>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, (hipStream_t)stream, a);
+    else
+        hipLaunchKernelGGL(tree_merge_kernel<4>, dim3((unsigned)((rows + 1) / 2)), dim3(256), 0, (hipStream_t)stream, a);
     return (int)hipGetLastError();
 }
 
