@@ -237,6 +237,52 @@ static __device__ __forceinline__ void tree_keep_apart(u32x2 (&vf)[16], const ui
         for (int x = 0; x < 2; ++x) vf[i][x] &= ~not_finite(vf[i][x]);
 }
 
+// Softmax update of a pass for all row tiles, as softmax_pass, but the running max of
+// a row follows only where a logit exceeds it by more than kTreeLag (in log2 units of
+// the weight): weights are then at most 2^kTreeLag, which costs their sums in fp32 and
+// their bf16 parts nothing, and after a list's first passes next to no pass rescales.
+constexpr float kTreeLag = 8.f;
+template <int kTerms, int kTiles>
+static __device__ __forceinline__ void tree_softmax(const f32x4 (&s)[kTiles][2], float scale, WaveAcc (&w)[kTiles],
+                                                    u32x4 (&p)[kTiles][kTerms]) {
+    float top[kTiles];
+    bool rises = false;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        top[t] = fmaxf(fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][0][2], s[t][0][3])),
+                       fmaxf(fmaxf(s[t][1][0], s[t][1][1]), fmaxf(s[t][1][2], s[t][1][3])));
+        rises |= (top[t] - w[t].m_run) * scale > kTreeLag;
+    }
+    if (__ballot(rises)) {
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+            const float m_new = fmaxf(w[t].m_run, max_over_c4(top[t]));
+            const float alpha = __builtin_amdgcn_exp2f((w[t].m_run - m_new) * scale);  // 0 while the state is empty
+            w[t].l_run *= alpha;
+#pragma unroll
+            for (int db = 0; db < 8; ++db) w[t].acc[db] *= alpha;
+            w[t].m_run = m_new;
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        float pr[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) pr[i] = __builtin_amdgcn_exp2f((s[t][i >> 2][i & 3] - w[t].m_run) * scale);
+        w[t].l_run += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
+#pragma unroll
+        for (int wd = 0; wd < 4; ++wd) {
+            float e0 = pr[2 * wd], e1 = pr[2 * wd + 1];
+#pragma unroll
+            for (int k = 0; k < kTerms; ++k) {
+                p[t][k][wd] = pack_bf16(e0, e1);
+                e0 -= __builtin_bit_cast(float, p[t][k][wd] << 16);
+                e1 -= __builtin_bit_cast(float, p[t][k][wd] & 0xffff0000u);
+            }
+        }
+    }
+}
+
 // Normalised output of four head dims of a row, and the lse (c == 0).
 static __device__ __forceinline__ void tree_store(const TreeLaunch &a, int64_t row, int c, f32x4 O, float M, float L) {
     const float inv = 1.f / L;
@@ -384,8 +430,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_attn_kernel(const TreeLau
                         for (int e = 0; e < 4; ++e) sc[t][blk][e] = mine & (1u << (16 * blk + e)) ? sc[t][blk][e] : kNegInf;
                 }
             }
-#pragma unroll
-            for (int t = 0; t < kTiles; ++t) softmax_pass<kTerms>(sc[t], kWaveTile, scale, w[t], c4, pr[t]);
+            tree_softmax<kTerms, kTiles>(sc, scale, w, pr);
             u32x2 vf[16];
             read_v_operands(vf, lds_addr(stage + kTileBytes), n16, c4);
             if (ruled) tree_keep_apart<kTiles>(vf, stage + kTileBytes, allows, w, lane);
