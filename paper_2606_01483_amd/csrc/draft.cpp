@@ -343,6 +343,10 @@ MURMUR_EXPORT int murmur_decode_attn_tree(const murmur_seg *seg_dev, const murmu
     a.row_sets = plan.row_sets;
     a.units = (int32_t)plan.units;
     a.shape = plan.shape;
+    a.max_pos = block_table_dev ? (int32_t)std::min<int64_t>((int64_t)max_blocks << log2_bs, 0x7fffffff) : kv->max_len;
+    const uint64_t row_bytes = (uint64_t)kv->stride_pos * 2;
+    a.near_rows = row_bytes < (1 << 24) && kv->max_len <= (1 << 24) &&
+                  (uint64_t)(kv->max_len - 1) * row_bytes + 2 * kHeadDim < ((uint64_t)1 << 32);
     a.magic_g = (65536u + (uint32_t)a.G - 1) / (uint32_t)a.G;
     a.scale_log2 = scale * 1.4426950408889634f;
     const int e = launch_decode_attn_tree(a, stream);

@@ -363,6 +363,8 @@ struct TreeLaunch {
     float *part_ml;  // [groups][n_split][T * G][2]  (running max in log2 units, sum)
     int32_t pol_mode, parent_per_seq, T, max_blocks, log2_bs, max_len, B, Hq, Hkv, G, NL, out_f32;
     int32_t n_split, row_sets, units, shape;
+    int32_t max_pos;    // positions below it have an entry in the table (a row of the cache without one)
+    int32_t near_rows;  // rows and their bytes are below 2^24, and every offset in a KV head's plane below 2^32
     uint32_t magic_g;  // ceil(2^16 / G): row / G is the high half of their product for rows up to 1024
     float scale_log2;
 };

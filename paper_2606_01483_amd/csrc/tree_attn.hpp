@@ -150,10 +150,12 @@ static __device__ __forceinline__ uint32_t tree_allows(const TreeList &l, const 
 constexpr int kTreeRows = 4;  // of a lane in a half pass of 16 rows
 struct TreeRows {
     int32_t pos[kTreeRows], entry[kTreeRows];
+    bool plain;  // uniform: consecutive cached positions, all within the table
     // positions, and the block table's entries on their way
     __device__ __forceinline__ void begin(const TreeList &l, const TreeLaunch &a, const int32_t *bt_row, int r0, int c4) {
         int p0;
-        if (r0 + 16 <= l.n0 && tab_run(l.tab, r0, 16, 0x7fffffff, p0)) {  // consecutive positions (uniform)
+        plain = r0 + 16 <= l.n0 && tab_run(l.tab, r0, 16, a.max_pos, p0);
+        if (plain) {
 #pragma unroll
             for (int i = 0; i < kTreeRows; ++i) pos[i] = p0 + 4 * i + c4;
         } else {
@@ -167,11 +169,13 @@ struct TreeRows {
         }
         if (bt_row) {  // uniform
 #pragma unroll
-            for (int i = 0; i < kTreeRows; ++i) entry[i] = bt_row[min(max(pos[i], 0) >> a.log2_bs, a.max_blocks - 1)];
+            for (int i = 0; i < kTreeRows; ++i)
+                entry[i] = bt_row[plain ? pos[i] >> a.log2_bs : min(max(pos[i], 0) >> a.log2_bs, a.max_blocks - 1)];
         }
     }
     // cache rows; a position that has none is an error and becomes the root's row
     __device__ __forceinline__ void finish(const TreeLaunch &a, const int32_t *bt_row, int &err) {
+        if (plain && !bt_row) return;
         const uint32_t last = (uint32_t)(a.max_len - 1), last_block = last >> a.log2_bs, in_block = (1u << a.log2_bs) - 1;
         uint32_t row[kTreeRows];
         bool wrong[kTreeRows], any = false;
@@ -181,19 +185,23 @@ struct TreeRows {
             wrong[i] = false;
             if (bt_row) {
                 row[i] = (uint32_t)entry[i] << a.log2_bs | (row[i] & in_block);
-                wrong[i] = ((uint32_t)entry[i] > last_block) | (pos[i] >> a.log2_bs >= a.max_blocks);
+                wrong[i] = ((uint32_t)entry[i] > last_block) | (!plain & (pos[i] >> a.log2_bs >= a.max_blocks));
             }
-            wrong[i] = (wrong[i] | (row[i] > last)) & (pos[i] >= 0);
+            wrong[i] = (wrong[i] | (row[i] > last)) & (plain | (pos[i] >= 0));
             any |= wrong[i];
         }
-        if (__builtin_expect(__ballot(any) != 0, 0)) {
+        if (plain && __builtin_expect(__ballot(any) == 0, 1)) {
 #pragma unroll
-            for (int i = 0; i < kTreeRows; ++i)
-                if (wrong[i])
-                    err |= bt_row && (entry[i] < 0 || pos[i] >> a.log2_bs >= a.max_blocks) ? MURMUR_DEVERR_BLOCK : MURMUR_DEVERR_POSITION;
+            for (int i = 0; i < kTreeRows; ++i) pos[i] = (int32_t)row[i];
+            return;
         }
+        plain = false;
 #pragma unroll
-        for (int i = 0; i < kTreeRows; ++i) pos[i] = wrong[i] ? ~0 : (pos[i] >= 0 ? (int32_t)row[i] : pos[i]);
+        for (int i = 0; i < kTreeRows; ++i) {
+            if (wrong[i])
+                err |= bt_row && (entry[i] < 0 || pos[i] >> a.log2_bs >= a.max_blocks) ? MURMUR_DEVERR_BLOCK : MURMUR_DEVERR_POSITION;
+            pos[i] = wrong[i] ? ~0 : (pos[i] >= 0 ? (int32_t)row[i] : pos[i]);
+        }
     }
 };
 
@@ -357,7 +365,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_attn_kernel(const TreeLau
     const uint16_t *kc = a.k + cache_at, *vc = a.v + cache_at;
     const int64_t tree_at = ((int64_t)lb * a.T * a.Hkv + g) * kHeadDim;
     // this wavefront loads the half `wave & 1` of a round's pass `wave >> 1`
-    const int half = wave & 1, chunk = 8 * (n16 ^ c4);
+    const int half = wave & 1, chunk = 16 * (n16 ^ c4);
+    const uint32_t row_bytes = (uint32_t)a.s_pos * 2u;
     int err = 0;
     TreeRows rows;
     const auto mine_in = [&](int it) { return p0 + it * kRound + (wave >> 1) < p1; };
@@ -382,12 +391,28 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_attn_kernel(const TreeLau
         if (it >= -1 && mine_in(it + 1)) {
             rows.finish(a, bt_row, err);
             uint8_t *stage = lds.stages[(it + 1) & 1][wave >> 1] + 4096 * half;
+            if (rows.plain && a.near_rows) {  // uniform: offsets of 32 bits, the same for K and V, from scalar bases
+                uint32_t at[kTreeRows];
 #pragma unroll
-            for (int i = 0; i < kTreeRows; ++i) {
-                const bool node_row = rows.pos[i] < 0;
-                const int64_t at = (node_row ? tree_at + (int64_t)~rows.pos[i] * (a.Hkv * kHeadDim) : rows.pos[i] * a.s_pos) + (chunk ^ 32 * i);
-                __builtin_amdgcn_global_load_lds((node_row ? a.k_tree : kc) + at, (lds_void_t *)(stage + i * 1024), 16, 0, 0);
-                __builtin_amdgcn_global_load_lds((node_row ? a.v_tree : vc) + at, (lds_void_t *)(stage + kTileBytes + i * 1024), 16, 0, 0);
+                for (int i = 0; i < kTreeRows; ++i)
+                    at[i] = __umul24((uint32_t)rows.pos[i], row_bytes) + (uint32_t)(chunk ^ 64 * i);
+#pragma unroll
+                for (int i = 0; i < kTreeRows; ++i) {
+                    __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint8_t *>(kc) + at[i], (lds_void_t *)(stage + i * 1024), 16, 0, 0);
+                    __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint8_t *>(vc) + at[i],
+                                                     (lds_void_t *)(stage + kTileBytes + i * 1024), 16, 0, 0);
+                }
+                asm volatile("" ::: "memory");  // the two paths' last loads are not one load of a 64-bit address
+            } else {
+#pragma unroll
+                for (int i = 0; i < kTreeRows; ++i) {
+                    const bool node_row = rows.pos[i] < 0;
+                    const int64_t at = (node_row ? tree_at + (int64_t)~rows.pos[i] * (a.Hkv * kHeadDim) : rows.pos[i] * a.s_pos) +
+                                       (chunk ^ 64 * i) / 2;
+                    __builtin_amdgcn_global_load_lds((node_row ? a.k_tree : kc) + at, (lds_void_t *)(stage + i * 1024), 16, 0, 0);
+                    __builtin_amdgcn_global_load_lds((node_row ? a.v_tree : vc) + at, (lds_void_t *)(stage + kTileBytes + i * 1024),
+                                                     16, 0, 0);
+                }
             }
         }
         if (mine_in(it + 2)) rows.begin(l, a, bt_row, (p0 + (it + 2) * kRound + (wave >> 1)) * kWaveTile + 16 * half, c4);
