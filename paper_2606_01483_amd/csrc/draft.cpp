@@ -75,19 +75,40 @@ int check_tree_sizes(int32_t n_layers, int32_t B, int32_t Hq, int32_t Hkv, int32
 
 }  // namespace
 
-// The rows of a workgroup are as many as the tree has, up to 256; where the (layer,
-// sequence, KV head) groups do not fill the chip, their lists are cut into splits.
+// A workgroup has up to 128 rows, of eight wavefronts with a compute unit to itself or
+// of four and two on one.  The list is cut into the splits that the following estimate
+// (us, fitted to batches of 1 to 128 trees of 2 to 64 nodes over 200 to 20 000 rows)
+// finds best, among those that fill the chip once, twice or three times: 7 for the way
+// to the first pass and from the last one; a pass of 128 rows 1.3, or 1.9 where
+// another workgroup shares the unit, of which 0.55 and 1.25 are the rows of K and V;
+// and for a merge 4 and its partials at 4 TB/s, written and read.  (12 trees of 32
+// nodes over 4000 rows: two splits on eight wavefronts 80, five on four 71; 32 trees
+// of 32 over 900 rows: 42 and 53.)
+// Eight wavefronts take one row tile each where a split is short: less is left to join
+// at its end, but every tile then reads the rows from LDS again (12 trees of 16 nodes,
+// 900 rows: 22.9 and 24.0 with two tiles; 4000 rows: 48.5 and 46.2).
 TreePlan tree_plan(int32_t n_layers, int32_t B, int32_t Hq, int32_t Hkv, int32_t n_nodes, int32_t max_keep) {
     TreePlan p{};
     const int64_t rows = (int64_t)n_nodes * (Hq / Hkv), groups = (int64_t)n_layers * B * Hkv;
-    const int64_t passes = ((int64_t)max_keep + kWaveTile - 1) / kWaveTile;
-    p.shape = rows <= 16 ? kTreeFew : groups * ((rows + 255) / 256) > kRoundWorkgroups / 2 ? kTreePair : kTreeWide;
-    const int per_wg = p.shape == kTreeWide ? 256 : 128;
-    p.row_sets = (int32_t)((rows + per_wg - 1) / per_wg);
-    const int64_t slots = p.shape == kTreePair ? 2 * kRoundWorkgroups : kRoundWorkgroups;
-    const int64_t want = std::max<int64_t>(1, slots / (groups * p.row_sets));
-    p.n_split = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, 64), passes / 4));
-    if (passes <= 8) p.n_split = 1;
+    const int64_t passes = ((int64_t)max_keep + kWaveTile - 1) / kWaveTile, most = std::min<int64_t>(kMaxTreeSplits, passes / 4);
+    p.row_sets = (int32_t)((rows + kTreeRowSet - 1) / kTreeRowSet);
+    const int64_t sets = groups * p.row_sets;
+    const double full = (double)std::min<int64_t>(rows, kTreeRowSet) / kTreeRowSet;
+    double best = 0.0;
+    for (int pair = 0; pair < 2; ++pair) {
+        const int64_t slots = (pair + 1) * kRoundWorkgroups;
+        const double pass_us = pair ? 1.25 + 0.65 * full : 0.55 + 0.75 * full;
+        for (int fill = 0; fill <= 3; ++fill) {
+            const int64_t s = std::max<int64_t>(1, std::min(fill * slots / sets, most));
+            const double merge_us = s > 1 ? 4.0 + (double)(groups * s * rows) * 2 * (kHeadDim + 2) * sizeof(float) / 4e6 : 0.0;
+            const double us = 7.0 + (double)((sets * s + slots - 1) / slots) * (double)((passes + s - 1) / s) * pass_us + merge_us;
+            if (best == 0.0 || us < best) {
+                best = us;
+                p.n_split = (int32_t)s;
+                p.shape = pair ? kTreePair : rows <= 64 || passes <= 12 * s ? kTreeFew : kTreeWide;
+            }
+        }
+    }
     p.units = groups * p.n_split;
     if (p.n_split > 1) {
         p.o_bytes = (size_t)p.units * (size_t)rows * kHeadDim * sizeof(float);
@@ -343,6 +364,13 @@ MURMUR_EXPORT int murmur_decode_attn_tree(const murmur_seg *seg_dev, const murmu
     a.row_sets = plan.row_sets;
     a.units = (int32_t)plan.units;
     a.shape = plan.shape;
+    const int merge_rows = plan.n_split <= kTreeMergeWhole ? 8 : 2;
+    a.merge_sets = (n_nodes * a.G + merge_rows - 1) / merge_rows;
+    a.by_sets = DivideBy::of((uint32_t)a.row_sets);
+    a.by_split = DivideBy::of((uint32_t)a.n_split);
+    a.by_heads = DivideBy::of((uint32_t)Hkv);
+    a.by_batch = DivideBy::of((uint32_t)B);
+    a.by_merge = DivideBy::of((uint32_t)a.merge_sets);
     a.max_pos = block_table_dev ? (int32_t)std::min<int64_t>((int64_t)max_blocks << log2_bs, 0x7fffffff) : kv->max_len;
     const uint64_t row_bytes = (uint64_t)kv->stride_pos * 2;
     a.near_rows = row_bytes < (1 << 24) && kv->max_len <= (1 << 24) &&

@@ -345,7 +345,24 @@ struct AcceptLaunch {
 int launch_tree_accept(const AcceptLaunch &p, murmur_stream_t stream);
 
 constexpr int kMaxNodes = 64;
-enum TreeShape : int32_t { kTreeFew, kTreeWide, kTreePair };  // workgroups of 8 wavefronts and 128 or 256 rows, of 4 and 128
+// x / d for x below 2^31 and d in [1, 2^31): the product with ceil(2^(31 + s) / d), where
+// 2^s >= d, is off by less than x / 2^31 of a d-th.
+struct DivideBy {
+    uint32_t mul, shift;
+    static DivideBy of(uint32_t d) {
+        uint32_t s = 0;
+        while (((uint64_t)1 << s) < d) ++s;
+        return DivideBy{(uint32_t)((((uint64_t)1 << (31 + s)) + d - 1) / d), 31 + s};
+    }
+#if defined(__HIPCC__)
+    __host__ __device__
+#endif
+    int operator()(int x) const { return (int)((uint64_t)(uint32_t)x * mul >> shift); }
+};
+enum TreeShape : int32_t { kTreeFew, kTreeWide, kTreePair };  // workgroups of 8 wavefronts (one or two row tiles each), of 4 (two)
+constexpr int kTreeRowSet = 128;     // rows of a workgroup
+constexpr int kMaxTreeSplits = 64;
+constexpr int kTreeMergeWhole = 8;   // splits up to which one thread joins four head dims of a row
 struct TreePlan {
     TreeShape shape;
     int32_t n_split, row_sets;
@@ -363,6 +380,8 @@ struct TreeLaunch {
     float *part_ml;  // [groups][n_split][T * G][2]  (running max in log2 units, sum)
     int32_t pol_mode, parent_per_seq, T, max_blocks, log2_bs, max_len, B, Hq, Hkv, G, NL, out_f32;
     int32_t n_split, row_sets, units, shape;
+    int32_t merge_sets;  // workgroups of the merge for each group
+    DivideBy by_sets, by_split, by_heads, by_batch, by_merge;
     int32_t max_pos;    // positions below it have an entry in the table (a row of the cache without one)
     int32_t near_rows;  // rows and their bytes are below 2^24, and every offset in a KV head's plane below 2^32
     uint32_t magic_g;  // ceil(2^16 / G): row / G is the high half of their product for rows up to 1024

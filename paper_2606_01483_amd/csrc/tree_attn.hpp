@@ -47,8 +47,7 @@ static __device__ __forceinline__ TreeList tree_list(const murmur_seg &s, const 
     // ancestors and itself, twice as far up in every round
     uint64_t up = 1ull << lane;
     int hop = ok && par >= 0 ? par : lane;
-#pragma unroll
-    for (int round = 0; round < 6; ++round) {
+    for (int reach = 1; reach < T; reach *= 2) {
         const uint32_t lo = __shfl((uint32_t)up, hop), hi = __shfl((uint32_t)(up >> 32), hop);
         up |= (uint64_t)hi << 32 | lo;
         hop = __shfl(hop, hop);
@@ -87,6 +86,8 @@ static __device__ __forceinline__ TreeList tree_list(const murmur_seg &s, const 
         }
         rule.a = max(start(depth), from) - from;
         rule.b = max(ns, most + ws) - max(ns, start(depth) + ws);
+        l.a_most = max(most, from) - from;  // the deepest node's
+        l.b_most = max(ns, most + ws) - max(ns, l0 + ws);  // the root's
     } else {
         rule.a = rule.b = 0;
     }
@@ -106,6 +107,7 @@ static __device__ __forceinline__ TreeList tree_list(const murmur_seg &s, const 
             rg[11] = c - base;
         }
         rule.c = max(0, min(j + depth - wo, c) - base);
+        l.c_most = max(0, min(j + deepest - wo, c) - base);
         if (wo <= deepest) {  // ancestors that the output window has left, unless they are sinks
             uint64_t near = 1ull << lane;
             const int to = par >= 0 ? par : lane;
@@ -126,10 +128,6 @@ static __device__ __forceinline__ TreeList tree_list(const murmur_seg &s, const 
     l.c0 = l.b1 + mid + sinks;
     l.n0 = l.b1 + mid + rg[9] + rg[11];
     l.count = l.n0 + l.live;
-    const bool is = par != -2;
-    l.a_most = wave_max(is ? rule.a : 0);
-    l.b_most = wave_max(is ? rule.b : 0);
-    l.c_most = wave_max(is ? rule.c : 0);
     return l;
 }
 
@@ -303,8 +301,8 @@ static __device__ __forceinline__ void tree_store(const TreeLaunch &a, int64_t r
 }
 
 // ---------------------------------------------------------------------------
-// Workgroup: up to kWaves * kTiles * 16 query rows of one (layer, sequence, KV head)
-// over one split of the list.  Its wavefronts take the list kWaves / 2 passes (a round)
+// Workgroup: up to 128 query rows of one (layer, sequence, KV head) over one split of
+// the list.  Its wavefronts take the list kWaves / 2 passes (a round)
 // at a time: together they load a round's rows into one of two buffers while they
 // compute the other, and a split of two rounds is on its way as a whole from the
 // start.  They are `ways` ways by rows and the rest by passes, as the rows that are
@@ -314,25 +312,25 @@ template <int kWaves>
 struct TreeLds {
     uint8_t stages[2][kWaves / 2][kStageBytes];
     TreeRule rule[64];
-    float ml[kWaves][32][2];
+    float2 ml[kWaves][2][64];
     int err;
 };
 
 template <int kTerms, int kTiles, int kWaves>
 __global__ __launch_bounds__(kWaves * 64, 2) void tree_attn_kernel(const TreeLaunch a) {
-    constexpr int kAll = kWaves * kTiles * 16, kThreads = kWaves * 64, kRound = kWaves / 2;
-    static_assert(kTiles <= 2, "two tiles of LDS a wavefront");
+    constexpr int kAll = 128, kThreads = kWaves * 64, kRound = kWaves / 2;
+    static_assert(kAll <= kWaves * kTiles * 16, "a wavefront's tiles for all rows");
     __shared__ __attribute__((aligned(16))) TreeLds<kWaves> lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n16 = lane & 15, c4 = lane >> 4;
     // The workgroups of one split's row sets follow each other on one XCD.  An XCD's go to its shader engines in turn,
     // so the sets start with another one for every split: otherwise (with as many sets as engines) one engine has every
     // first set, and another every last one, where trees of few nodes have no rows.
-    const int x = blockIdx.x, eight = (x >> 3) / a.row_sets;
-    const int set = ((x >> 3) - eight * a.row_sets + eight) % a.row_sets, unit = eight * 8 + (x & 7);
+    const int x = blockIdx.x, eight = a.by_sets(x >> 3), turned = (x >> 3) - eight * a.row_sets + eight;
+    const int set = turned - a.by_sets(turned) * a.row_sets, unit = eight * 8 + (x & 7);
     if (unit >= a.units) return;
-    const int split = unit % a.n_split, group = unit / a.n_split;
-    const int g = group % a.Hkv, lb = group / a.Hkv, b = lb % a.B, layer = lb / a.B;
+    const int group = a.by_split(unit), split = unit - group * a.n_split;
+    const int lb = a.by_heads(group), g = group - lb * a.Hkv, layer = a.by_batch(lb), b = lb - layer * a.B;
     const murmur_seg s = reinterpret_cast<const murmur_seg *>(a.seg)[b];
     const int rec = ((a.pol_mode & MURMUR_POL_PER_LAYER) ? layer * ((a.pol_mode & MURMUR_POL_PER_SEQ) ? a.B : 1) : 0) +
                     ((a.pol_mode & MURMUR_POL_PER_SEQ) ? b : 0);
@@ -478,70 +476,62 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_attn_kernel(const TreeLau
     __syncthreads();
     const bool bad = lds.err != 0;
 
-    // Rows to the outputs, or to the split's partials
-    const auto put = [&](int r, int c, f32x4 O, float M, float L) {
-        if (r >= rows_live) return;
+    // The groups' states by way of the buffers, register by register: a lane's share of a row's sum, its part of O and
+    // the row's max stand in the same lane of every group.
+    const int groups_here = min(groups, p1 - p0);  // those that had a pass
+    if (groups_here > 1) {
+        constexpr int kWords = 8 * kTiles;
+        f32x4 *o = reinterpret_cast<f32x4 *>(&lds.stages[0][0][0]);
+        static_assert(sizeof(lds.stages) >= kWaves * kWords * 64 * sizeof(f32x4), "the sums of every wavefront");
+        if (grp > 0 && grp < groups_here) {
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+                lds.ml[wave][t][lane] = float2{w[t].m_run, w[t].l_run};
+#pragma unroll
+                for (int db = 0; db < 8; ++db) o[(wave * kWords + 8 * t + db) * 64 + lane] = w[t].acc[db];
+            }
+        }
+        __syncthreads();
+        if (grp == 0) {
+#pragma unroll 1
+            for (int e = 1; e < groups_here; ++e) {
+                const int wv = e * ways + way;
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+                    const float2 ml = lds.ml[wv][t][lane];
+                    const float m = fmaxf(w[t].m_run, ml.x);
+                    const float f0 = __builtin_amdgcn_exp2f((w[t].m_run - m) * scale), f1 = __builtin_amdgcn_exp2f((ml.x - m) * scale);
+                    w[t].l_run = w[t].l_run * f0 + ml.y * f1;
+#pragma unroll
+                    for (int db = 0; db < 8; ++db)
+                        w[t].acc[db] = w[t].acc[db] * f0 + o[(wv * kWords + 8 * t + db) * 64 + lane] * f1;
+                    w[t].m_run = m;
+                }
+            }
+        }
+    }
+    if (grp > 0) return;
+    // rows to the outputs, or to the split's partials
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        float M = w[t].m_run * scale, L = sum_over_c4(w[t].l_run);
         if (bad) {
             M = 0.f;
             L = __builtin_nanf("");
         }
+        const bool there = row[t] < rows_live && (l.there >> node[t] & 1);
+        if (!there) continue;
         if (a.n_split > 1) {
-            const int64_t at = ((int64_t)group * a.n_split + split) * (a.T * a.G) + r;
-            *reinterpret_cast<f32x4 *>(a.part_o + at * kHeadDim + 4 * c) = O;
-            if (c == 0) *reinterpret_cast<float2 *>(a.part_ml + 2 * at) = float2{M, L};
+            const int64_t at = ((int64_t)group * a.n_split + split) * (a.T * a.G) + row[t];
+#pragma unroll
+            for (int db = 0; db < 8; ++db)
+                *reinterpret_cast<f32x4 *>(a.part_o + at * kHeadDim + 16 * db + 4 * c4) = w[t].acc[db];
+            if (c4 == 0) *reinterpret_cast<float2 *>(a.part_ml + 2 * at) = float2{M, L};
         } else {
-            const int n = (int)((uint32_t)r * a.magic_g >> 16);
-            if (l.there >> n & 1) tree_store(a, ((int64_t)lb * a.T + n) * a.Hq + g * a.G + r - n * a.G, c, O, M, L);
+            const int64_t at = ((int64_t)lb * a.T + node[t]) * a.Hq + g * a.G + row[t] - node[t] * a.G;
+#pragma unroll
+            for (int db = 0; db < 8; ++db) tree_store(a, at, 4 * db + c4, w[t].acc[db], M, L);
         }
-    };
-    if (groups == 1) {
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-            const float sum = sum_over_c4(w[t].l_run);
-#pragma unroll
-            for (int db = 0; db < 8; ++db) put(row[t], 4 * db + c4, w[t].acc[db], w[t].m_run * scale, sum);
-        }
-        return;
-    }
-    // the groups' states by way of the buffers
-    float *all = reinterpret_cast<float *>(&lds.stages[0][0][0]), *o = all + wave * kTiles * 16 * kHeadDim;
-    static_assert(sizeof(lds.stages) >= kWaves * 32 * kHeadDim * sizeof(float), "two tiles of each wavefront");
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-        const float sum = sum_over_c4(w[t].l_run);
-        const int r = 16 * t + n16;
-        if (c4 == 0) *reinterpret_cast<float2 *>(&lds.ml[wave][r][0]) = float2{w[t].m_run * scale, sum};
-#pragma unroll
-        for (int db = 0; db < 8; ++db)
-            *reinterpret_cast<f32x4 *>(&o[r * kHeadDim + 4 * ((4 * db + c4) ^ (r & 7))]) = w[t].acc[db];
-    }
-    __syncthreads();
-    constexpr int kRows = 16 * kTiles;  // of a way
-#pragma unroll 1
-    for (int i = tid; i < ways * kRows * 32; i += kThreads) {
-        const int c = i & 31, wy = (i >> 5) / kRows, r = (i >> 5) % kRows;
-        if (row0 + wy * kRows + r >= rows_live) continue;
-        float m[kRound], sum[kRound];
-        f32x4 part[kRound];
-#pragma unroll
-        for (int e = 0; e < kRound; ++e) {  // behind the last group: the first one again, which weighs nothing
-            const int wv = (e < groups ? e : 0) * ways + wy;
-            const float2 ml = *reinterpret_cast<const float2 *>(&lds.ml[wv][r][0]);
-            m[e] = ml.x;
-            sum[e] = ml.y;
-            part[e] = *reinterpret_cast<const f32x4 *>(all + (wv * kRows + r) * kHeadDim + 4 * (c ^ (r & 7)));
-        }
-        float M = m[0], L = 0.f;
-#pragma unroll
-        for (int e = 1; e < kRound; ++e) M = fmaxf(M, m[e]);
-        f32x4 O = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int e = 0; e < kRound; ++e) {
-            const float f = e >= groups || m[e] == kNegInf ? 0.f : __builtin_amdgcn_exp2f(m[e] - M);
-            L += e < groups ? sum[e] * f : 0.f;
-            O += e < groups ? f * part[e] : f32x4{0.f, 0.f, 0.f, 0.f};
-        }
-        put(row0 + wy * kRows + r, c, O, M, L);
     }
 }
 
@@ -552,24 +542,16 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeLaunch a) {
     constexpr int kRows = 8 / kParts, kBatch = 8;
     __shared__ f32x4 s_o[kParts > 1 ? 8 : 1][32];
     __shared__ float2 s_ml[8];
-    const int rows = a.T * a.G, slice = threadIdx.x >> 5, c = threadIdx.x & 31;
-    const int part = slice / kRows;
-    const int64_t at = (int64_t)blockIdx.x * kRows + slice % kRows;
-    const int64_t group = at / rows;
-    const int r = (int)(at - group * rows), n = (int)((uint32_t)r * a.magic_g >> 16);
-    const int64_t lb = group / a.Hkv;
-    const int g = (int)(group - lb * a.Hkv), b = (int)(lb % a.B);
-    const bool in = at < (int64_t)a.NL * a.B * a.Hkv * rows;
-    bool there = false;
-    if (in) {
-        const murmur_seg s = reinterpret_cast<const murmur_seg *>(a.seg)[b];
-        there = !layout_absent(s.prompt_pre, s.speech_len, s.prompt_mid, s.out_len) &&
-                a.parent[(a.parent_per_seq ? (int64_t)b * a.T : 0) + n] != -2;
-    }
+    const int rows = a.T * a.G, slice = threadIdx.x >> 5, c = threadIdx.x & 31, part = slice / kRows;
+    const int group = a.by_merge(blockIdx.x), r0 = ((int)blockIdx.x - group * a.merge_sets) * kRows;
+    const int lb = a.by_heads(group), g = group - lb * a.Hkv, b = lb - a.by_batch(lb) * a.B;
+    const int r = min(r0 + slice % kRows, rows - 1), n = (int)((uint32_t)r * a.magic_g >> 16);
+    const murmur_seg s = reinterpret_cast<const murmur_seg *>(a.seg)[b];
+    const int32_t parent = a.parent[(a.parent_per_seq ? (int64_t)b * a.T : 0) + n];
     float M = kNegInf, L = 0.f;
     f32x4 O = {0.f, 0.f, 0.f, 0.f};
-    if (there) {
-        const int64_t part0 = group * a.n_split * rows + r;
+    {  // of rows that are not there too: whatever the workspace holds is not stored
+        const int64_t part0 = (int64_t)group * a.n_split * rows + r;
         for (int i0 = part; i0 < a.n_split; i0 += kBatch * kParts) {
             float2 ml[kBatch];
             f32x4 o[kBatch];
@@ -615,7 +597,8 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeLaunch a) {
         }
         M = m;
     }
-    if (there) tree_store(a, (lb * a.T + n) * a.Hq + g * a.G + r - n * a.G, c, O, M, L);
+    const bool there = parent != -2 && !layout_absent(s.prompt_pre, s.speech_len, s.prompt_mid, s.out_len);
+    if (there && r0 + slice % kRows < rows) tree_store(a, ((int64_t)lb * a.T + n) * a.Hq + g * a.G + r - n * a.G, c, O, M, L);
 }
 
 template <int kTerms, int kTiles, int kWaves>
@@ -637,11 +620,11 @@ static int launch_tree(const TreeLaunch &a, hipStream_t stream) {
 int launch_decode_attn_tree(const TreeLaunch &a, murmur_stream_t stream) {
     const int e = a.out_f32 ? launch_tree<3>(a, (hipStream_t)stream) : launch_tree<2>(a, (hipStream_t)stream);
     if (e != 0 || a.n_split == 1) return e;
-    const int64_t rows = (int64_t)a.NL * a.B * a.Hkv * a.T * a.G;
-    if (a.n_split <= 8)
-        hipLaunchKernelGGL(tree_merge_kernel<1>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, (hipStream_t)stream, a);
+    const unsigned grid = (unsigned)(a.units / a.n_split) * (unsigned)a.merge_sets;
+    if (a.n_split <= kTreeMergeWhole)
+        hipLaunchKernelGGL(tree_merge_kernel<1>, dim3(grid), dim3(256), 0, (hipStream_t)stream, a);
     else
-        hipLaunchKernelGGL(tree_merge_kernel<4>, dim3((unsigned)((rows + 1) / 2)), dim3(256), 0, (hipStream_t)stream, a);
+        hipLaunchKernelGGL(tree_merge_kernel<4>, dim3(grid), dim3(256), 0, (hipStream_t)stream, a);
     return (int)hipGetLastError();
 }
 
