@@ -1,7 +1,8 @@
 // Device code of requests into a paged pool, rotary positions and accepted paths
 // (included by kernels.hip).
 //
-//   reserve_count_kernel, reserve_take_kernel  blocks and slot maps for new tokens
+//   reserve_group_kernel, reserve_count_kernel, reserve_long_kernel
+//                                              blocks and slot maps for new tokens
 //   rope_wide_kernel, rope_pair_kernel         q and k rotated, K and V into the cache
 //   tree_accept_kernel                         the accepted path into the cache
 #pragma once
@@ -10,12 +11,14 @@ namespace murmur {
 
 // ---------------------------------------------------------------------------
 // reserve.  Sequences are served in order, so a sequence's blocks are found from the
-// number that those before it need: the first launch counts (a wavefront per sequence,
-// and sums over kReserveGroup of them), the second pops and writes the maps, a
-// workgroup per sequence.  A sequence is refused where its blocks end behind the
-// stack, or its tokens behind the maps; then so is every later one that needs a block,
-// so those that are served pop without holes and the top is the minimum of what they
-// leave (an integer atomic, whose order does not matter).
+// number that those before it need.  Up to kReserveGroup sequences are one workgroup's
+// work, a wavefront each; more take two launches: the first counts (a wavefront per
+// sequence, and sums over kReserveGroup of them), the second pops and writes the maps,
+// a wavefront per sequence or (long prompts) a workgroup.  A sequence is refused where
+// its blocks end behind the stack, or its tokens behind the maps; then so is every
+// later one that needs a block, so those that are served pop without holes and the top
+// is the minimum of what they leave (an integer atomic, whose order does not matter).
+// Bound by round trips to memory: lengths, entries, stack, maps.
 // ---------------------------------------------------------------------------
 constexpr int kReserveThreads = 64 * kReserveGroup;
 
@@ -25,40 +28,152 @@ static __device__ __forceinline__ int64_t wave_sum64(int64_t x) {
     return x;
 }
 
+// What sequence b asks for, by a wavefront: its blocks, or -1 and the device error.
+struct ReserveAsk {
+    int32_t len, fresh;  // fresh: 0 where either is negative
+    int32_t need, err;
+    int32_t entry;  // the lane's of the first 64 columns
+};
+static __device__ __forceinline__ ReserveAsk reserve_ask(const ReserveLaunch &p, int b, int lane) {
+    ReserveAsk a{p.len[b], p.fresh[b], 0, 0, 0};
+    if (a.len < 0 || a.fresh < 0) {
+        a.err = MURMUR_DEVERR_COUNT;
+        a.fresh = 0;
+    } else if (a.fresh > 0) {
+        const int64_t last = ((int64_t)a.len + a.fresh - 1) >> p.log2_bs;
+        if (last >= p.max_blocks) a.err = MURMUR_DEVERR_BLOCK;
+        else if (p.per_seq > 0 && a.fresh > p.per_seq) a.err = MURMUR_DEVERR_OVERFLOW;
+        else {
+            const int32_t *row = p.bt + (int64_t)b * p.max_blocks;
+            for (int c0 = a.len >> p.log2_bs; c0 <= (int)last; c0 += 64) {
+                const bool in = c0 + lane <= (int)last;
+                const int32_t x = in ? row[c0 + lane] : 0;
+                if (c0 == a.len >> p.log2_bs) a.entry = x;
+                a.need += __popcll(__ballot(in && x < 0));
+                const bool wrong = in && (x >= p.n_blocks || (p.ref && x >= 0 && p.ref[x] > 1));
+                if (__ballot(wrong)) a.err = MURMUR_DEVERR_BLOCK;
+            }
+        }
+    }
+    if (a.err) a.need = -1;
+    return a;
+}
+
+// Takes the blocks of sequence b and writes its maps, by kThreads threads (a wavefront,
+// or a workgroup with s_scan and s_bad).  tokens, blocks: of the sequences before it;
+// all: tokens of all of them.  Returns the top that it leaves, or INT32_MAX.
+template <int kThreads>
+static __device__ __forceinline__ int32_t reserve_take(const ReserveLaunch &p, int b, const ReserveAsk &ask, int32_t top, int64_t tokens,
+                                                    int blocks, int64_t all, int tid, int *s_scan, int *s_bad) {
+    const auto start_at = [&](int64_t packed, int q) {
+        return (int32_t)min(p.per_seq > 0 ? (int64_t)q * p.per_seq : packed, (int64_t)0x7fffffff);
+    };
+    const int32_t len = ask.len, fresh = ask.fresh, need = ask.need;
+    const int64_t at = p.per_seq > 0 ? (int64_t)b * p.per_seq : tokens;
+    int err = 0;
+    bool served = need >= 0;
+    if (served && at + fresh > p.n_tokens) {
+        served = false;
+        err |= MURMUR_DEVERR_OVERFLOW;
+    } else if (served && need > 0 && (int64_t)blocks + need > top) {
+        served = false;
+        err |= MURMUR_DEVERR_POOL;
+    }
+    int32_t *row = p.bt + (int64_t)b * p.max_blocks;
+    const int first = len >> p.log2_bs, last = fresh > 0 ? (int)(((int64_t)len + fresh - 1) >> p.log2_bs) : first;
+    const bool held = kThreads == 64 && last - first < 64;  // every entry stands in a lane
+    int32_t entry = ask.entry, left = 0x7fffffff;
+    // the blocks: the k-th that is missing is the k-th from the top behind those of the sequences before
+    if (served && need > 0) {
+        int k = top - 1 - blocks;
+        left = k + 1 - need;
+        bool bad = false;
+        for (int c0 = first; c0 <= last; c0 += kThreads) {
+            const int c = c0 + tid;
+            const bool missing = c <= last && (held ? entry : row[c]) < 0;
+            int total, off;
+            if constexpr (kThreads == 64) {
+                const uint64_t those = __ballot(missing);
+                total = __popcll(those);
+                off = __popcll(those & ((1ull << tid) - 1));
+            } else {
+                off = wg_exclusive_scan<kThreads>(missing, s_scan, tid, total);
+            }
+            if (missing) {
+                const int32_t x = p.stack[k - off];
+                if (x >= 0 && x < p.n_blocks) {
+                    row[c] = x;
+                    if (p.ref) p.ref[x] = 1;
+                    entry = x;
+                } else {
+                    bad = true;
+                }
+            }
+            k -= total;
+        }
+        if constexpr (kThreads == 64) {
+            if (!held) wait_vmem();  // the entries before they are read again
+            bad = __ballot(bad) != 0;
+        } else {
+            if (bad) *s_bad = 1;
+            __syncthreads();
+            bad = *s_bad;
+        }
+        if (bad) {
+            served = false;
+            err |= MURMUR_DEVERR_POOL;
+        }
+    }
+    // the maps, kBatch entries of a thread at a time
+    constexpr int kBatch = 4;
+    const int64_t end = min(p.per_seq > 0 ? at + p.per_seq : at + fresh, (int64_t)p.n_tokens);
+    for (int64_t i0 = at; i0 < end; i0 += kBatch * kThreads) {
+        int32_t block[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const int64_t i = i0 + j * kThreads + tid, of = min(i - at, max((int64_t)fresh - 1, (int64_t)0));
+            const int c = (int)((len + of) >> p.log2_bs);
+            if (held) block[j] = __shfl(entry, c - first);
+            else block[j] = served && fresh > 0 && i < end ? row[c] : 0;
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const int64_t i = i0 + j * kThreads + tid, pos = len + (i - at);
+            if (i >= end) break;
+            const bool there = i - at < fresh;
+            p.slot[i] = there && served ? (block[j] << p.log2_bs) | (int32_t)(pos & ((1 << p.log2_bs) - 1)) : -1;
+            if (p.pos) p.pos[i] = there ? (int32_t)min(pos, (int64_t)0x7fffffff) : -1;
+            if (p.seq) p.seq[i] = there ? b : -1;
+        }
+    }
+    // the entries that no sequence has, between all of them
+    for (int64_t i = (p.per_seq > 0 ? (int64_t)p.B * p.per_seq : all) + (int64_t)b * kThreads + tid; i < p.n_tokens;
+         i += (int64_t)p.B * kThreads) {
+        p.slot[i] = -1;
+        if (p.pos) p.pos[i] = -1;
+        if (p.seq) p.seq[i] = -1;
+    }
+    if (tid == 0) {
+        p.got[b] = served ? fresh : -1;
+        p.start[b] = start_at(tokens, b);
+        if (b == p.B - 1) p.start[p.B] = start_at(all, p.B);
+        if (err | ask.err) raise_device_error(err | ask.err);
+    }
+    return left;
+}
+
+static __device__ __forceinline__ int32_t reserve_top(const ReserveLaunch &p, int32_t top) { return min(max(top, 0), p.n_blocks); }
+
 __global__ __launch_bounds__(kReserveThreads) void reserve_count_kernel(const ReserveLaunch p) {
     __shared__ ReserveSums s_sums[kReserveGroup];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int b = blockIdx.x * kReserveGroup + wave;
-    int need = 0, err = 0;
-    int32_t n = 0;
-    if (b < p.B) {
-        const int32_t len = p.len[b];
-        n = p.fresh[b];
-        const int64_t end = (int64_t)len + n;
-        if (len < 0 || n < 0) {
-            err = MURMUR_DEVERR_COUNT;
-            n = 0;
-        } else if (n > 0) {
-            const int64_t last = (end - 1) >> p.log2_bs;
-            if (last >= p.max_blocks) err = MURMUR_DEVERR_BLOCK;
-            else if (p.per_seq > 0 && n > p.per_seq) err = MURMUR_DEVERR_OVERFLOW;
-            else {
-                const int32_t *row = p.bt + (int64_t)b * p.max_blocks;
-                for (int c0 = len >> p.log2_bs; c0 <= (int)last; c0 += 64) {
-                    const int32_t x = c0 + lane <= (int)last ? row[c0 + lane] : 0;
-                    const bool in = c0 + lane <= (int)last;
-                    need += __popcll(__ballot(in && x < 0));
-                    const bool wrong = in && (x >= p.n_blocks || (p.ref && x >= 0 && p.ref[x] > 1));
-                    if (__ballot(wrong)) err = MURMUR_DEVERR_BLOCK;
-                }
-            }
-        }
-        if (lane == 0) p.need[b] = err ? -1 : need;
-        if (err) need = 0;
-    }
+    ReserveAsk ask{0, 0, 0, 0, 0};
+    if (b < p.B) ask = reserve_ask(p, b, lane);
     if (lane == 0) {
-        s_sums[wave] = ReserveSums{n, need, 0};
-        if (err) raise_device_error(err);
+        s_sums[wave] = ReserveSums{ask.fresh, max(ask.need, 0), 0};
+        if (b < p.B) p.need[b] = ask.need;
+        if (ask.err) raise_device_error(ask.err);
     }
     __syncthreads();
     if (tid == 0) {
@@ -72,28 +187,82 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_count_kernel(const Re
     }
 }
 
-template <int kThreads>
-__global__ __launch_bounds__(kThreads) void reserve_take_kernel(const ReserveLaunch p) {
-    __shared__ int64_t s_tokens[2][kThreads / 64];
-    __shared__ int s_blocks[kThreads / 64];
+// kReserveGroup sequences, a wavefront each; all there are, or (kMany) those of one
+// workgroup behind reserve_count_kernel.
+template <bool kMany>
+__global__ __launch_bounds__(kReserveThreads) void reserve_group_kernel(const ReserveLaunch p) {
+    __shared__ int s_need[kReserveGroup], s_fresh[kReserveGroup], s_blocks[kReserveGroup];
+    __shared__ int64_t s_tokens[2][kReserveGroup];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int b = blockIdx.x * kReserveGroup + wave;
+    const int32_t top = reserve_top(p, kMany ? *p.top0 : *p.top);
+    ReserveAsk ask{0, 0, 0, 0, 0};
+    if (b < p.B) ask = reserve_ask(p, b, lane);
+    ask.err = kMany ? 0 : ask.err;  // reported
+    int64_t tokens = 0, all = 0;
+    int blocks = 0;
+    if (kMany) {
+        for (int i = tid; i < (int)gridDim.x; i += kReserveThreads) {
+            const ReserveSums t = p.sums[i];
+            tokens += i < (int)blockIdx.x ? t.tokens : 0;
+            blocks += i < (int)blockIdx.x ? t.blocks : 0;
+            all += t.tokens;
+        }
+        tokens = wave_sum64(tokens);
+        all = wave_sum64(all);
+        blocks = wave_sum(blocks);
+    }
+    if (lane == 0) {
+        s_need[wave] = max(ask.need, 0);
+        s_fresh[wave] = ask.fresh;
+        s_tokens[0][wave] = tokens;
+        s_tokens[1][wave] = all;
+        s_blocks[wave] = blocks;
+    }
+    __syncthreads();
+    const int w = lane & (kReserveGroup - 1);
+    const bool one = lane < kReserveGroup, before = one && w < wave;
+    const int64_t fresh = s_fresh[w];
+    tokens = wave_sum64((one ? s_tokens[0][w] : 0) + (before ? fresh : 0));
+    blocks = wave_sum((one ? s_blocks[w] : 0) + (before ? s_need[w] : 0));
+    all = wave_sum64(one ? (kMany ? s_tokens[1][w] : fresh) : 0);
+    int32_t left = 0x7fffffff;
+    if (b < p.B) left = reserve_take<64>(p, b, ask, top, tokens, blocks, all, lane, nullptr, nullptr);
+    __syncthreads();  // the sums are read, and so is the top
+    if (lane == 0) s_need[wave] = left;
+    __syncthreads();
+    if (tid == 0) {
+#pragma unroll
+        for (int i = 0; i < kReserveGroup; ++i) left = min(left, s_need[i]);
+        if (left != 0x7fffffff) __hip_atomic_fetch_min(p.top, left, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+}
+
+// Long prompts: a workgroup per sequence, behind reserve_count_kernel.
+__global__ __launch_bounds__(kReserveThreads) void reserve_long_kernel(const ReserveLaunch p) {
+    constexpr int kWaves = kReserveThreads / 64;
+    __shared__ int64_t s_tokens[2][kWaves];
+    __shared__ int s_blocks[kWaves];
     __shared__ int s_bad;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = blockIdx.x;
     const int groups = (p.B + kReserveGroup - 1) / kReserveGroup, mine = b / kReserveGroup;
+    ReserveAsk ask{p.len[b], p.fresh[b], p.need[b], 0, 0};
+    if (ask.len < 0 || ask.fresh < 0) ask.fresh = 0;
+    const int32_t top = reserve_top(p, *p.top0);
     if (tid == 0) s_bad = 0;
     // tokens and blocks of the sequences before this one, and all tokens
     int64_t tokens = 0, all = 0;
     int blocks = 0;
-    for (int i = tid; i < groups; i += kThreads) {
+    if (tid < b - mine * kReserveGroup) {
+        const int o = mine * kReserveGroup + tid;
+        blocks = max(p.need[o], 0);
+        tokens = p.len[o] >= 0 ? max(p.fresh[o], 0) : 0;
+    }
+    for (int i = tid; i < groups; i += kReserveThreads) {
         const ReserveSums t = p.sums[i];
         tokens += i < mine ? t.tokens : 0;
         blocks += i < mine ? t.blocks : 0;
         all += t.tokens;
-    }
-    if (tid < b - mine * kReserveGroup) {
-        const int o = mine * kReserveGroup + tid;
-        const int32_t n = p.need[o];
-        blocks += max(n, 0);
-        tokens += p.len[o] >= 0 ? max(p.fresh[o], 0) : 0;
     }
     tokens = wave_sum64(tokens);
     all = wave_sum64(all);
@@ -106,79 +275,14 @@ __global__ __launch_bounds__(kThreads) void reserve_take_kernel(const ReserveLau
     __syncthreads();
     tokens = all = blocks = 0;
 #pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) {
+    for (int w = 0; w < kWaves; ++w) {
         tokens += s_tokens[0][w];
         all += s_tokens[1][w];
         blocks += s_blocks[w];
     }
-    const auto start_at = [&](int64_t packed, int q) {
-        return (int32_t)min(p.per_seq > 0 ? (int64_t)q * p.per_seq : packed, (int64_t)0x7fffffff);
-    };
-    const int32_t len = p.len[b], fresh = len >= 0 ? max(p.fresh[b], 0) : 0, need = p.need[b];
-    const int64_t at = p.per_seq > 0 ? (int64_t)b * p.per_seq : tokens;
-    const int32_t top = min(max(*p.top0, 0), p.n_blocks);
-    int err = 0;
-    bool served = need >= 0;
-    if (served && at + fresh > p.n_tokens) {
-        served = false;
-        err |= MURMUR_DEVERR_OVERFLOW;
-    } else if (served && need > 0 && (int64_t)blocks + need > top) {
-        served = false;
-        err |= MURMUR_DEVERR_POOL;
-    }
-    const int first = served && fresh > 0 ? len >> p.log2_bs : 0;
-    const int last = served && fresh > 0 ? (int)(((int64_t)len + fresh - 1) >> p.log2_bs) : -1;
-    int32_t *row = p.bt + (int64_t)b * p.max_blocks;
-    // the blocks: the k-th that is missing is the k-th from the top behind those of the sequences before
-    if (served && need > 0) {
-        int k = top - 1 - blocks;
-        for (int c0 = first; c0 <= last; c0 += kThreads) {
-            const int c = c0 + tid;
-            const bool missing = c <= last && row[c] < 0;
-            int total;
-            const int off = wg_exclusive_scan<kThreads>(missing, s_blocks, tid, total);
-            if (missing) {
-                const int32_t x = p.stack[k - off];
-                if (x >= 0 && x < p.n_blocks) {
-                    row[c] = x;
-                    if (p.ref) p.ref[x] = 1;
-                } else {
-                    s_bad = 1;
-                }
-            }
-            k -= total;
-        }
-        if (tid == 0)
-            __hip_atomic_fetch_min(p.top, top - blocks - need, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
     __syncthreads();
-    if (s_bad) {
-        served = false;
-        err |= MURMUR_DEVERR_POOL;
-    }
-    // the maps
-    const int64_t end = p.per_seq > 0 ? min(at + p.per_seq, (int64_t)p.n_tokens) : min(at + fresh, (int64_t)p.n_tokens);
-    for (int64_t i = at + tid; i < end; i += kThreads) {
-        const int64_t pos = len + (i - at);
-        const bool there = i - at < fresh;
-        int32_t slot = -1;
-        if (there && served) slot = (row[pos >> p.log2_bs] << p.log2_bs) | (int32_t)(pos & ((1 << p.log2_bs) - 1));
-        p.slot[i] = slot;
-        if (p.pos) p.pos[i] = there ? (int32_t)min(pos, (int64_t)0x7fffffff) : -1;
-        if (p.seq) p.seq[i] = there ? b : -1;
-    }
-    for (int64_t i = (p.per_seq > 0 ? (int64_t)p.B * p.per_seq : all) + (int64_t)b * kThreads + tid; i < p.n_tokens;
-         i += (int64_t)p.B * kThreads) {
-        p.slot[i] = -1;
-        if (p.pos) p.pos[i] = -1;
-        if (p.seq) p.seq[i] = -1;
-    }
-    if (tid == 0) {
-        p.got[b] = served ? fresh : -1;
-        p.start[b] = start_at(tokens, b);
-        if (b == p.B - 1) p.start[p.B] = start_at(all, p.B);
-        if (err) raise_device_error(err);
-    }
+    const int32_t left = reserve_take<kReserveThreads>(p, b, ask, top, tokens, blocks, all, tid, s_blocks, &s_bad);
+    if (tid == 0 && left != 0x7fffffff) __hip_atomic_fetch_min(p.top, left, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 // ---------------------------------------------------------------------------
@@ -392,14 +496,19 @@ __global__ __launch_bounds__(256) void tree_accept_kernel(const AcceptLaunch p) 
 // ---- launchers ----
 
 int launch_paged_reserve(const ReserveLaunch &p, murmur_stream_t stream) {
-    hipLaunchKernelGGL(reserve_count_kernel, dim3((unsigned)((p.B + kReserveGroup - 1) / kReserveGroup)), dim3(kReserveThreads),
-                       0, (hipStream_t)stream, p);
+    const hipStream_t s = (hipStream_t)stream;
+    const dim3 groups((unsigned)((p.B + kReserveGroup - 1) / kReserveGroup)), threads(kReserveThreads);
+    // 12 prompts of 2283 tokens: 6.1 us behind the count's 3.3; in one launch, a wavefront each, 14.2
+    const bool few = p.n_tokens / p.B <= 256;
+    if (few && groups.x == 1) {
+        hipLaunchKernelGGL(reserve_group_kernel<false>, groups, threads, 0, s, p);
+        return (int)hipGetLastError();
+    }
+    hipLaunchKernelGGL(reserve_count_kernel, groups, threads, 0, s, p);
     const int e = (int)hipGetLastError();
     if (e != 0) return e;
-    if (p.n_tokens / p.B <= 256)
-        hipLaunchKernelGGL(reserve_take_kernel<64>, dim3((unsigned)p.B), dim3(64), 0, (hipStream_t)stream, p);
-    else
-        hipLaunchKernelGGL(reserve_take_kernel<1024>, dim3((unsigned)p.B), dim3(1024), 0, (hipStream_t)stream, p);
+    if (few) hipLaunchKernelGGL(reserve_group_kernel<true>, groups, threads, 0, s, p);
+    else hipLaunchKernelGGL(reserve_long_kernel, dim3((unsigned)p.B), threads, 0, s, p);
     return (int)hipGetLastError();
 }
 
