@@ -122,7 +122,7 @@ typedef struct murmur_qkv {
  * into the cache rows of a slot map, all in one launch.  The turns are exact (see
  * murmur_rope_freqs_host), sines and products fp32; bf16 results are rounded once.
  *   pos_dev:   device int32 [n_tokens]: rotary positions; a token of a negative one is
- *              not there: nothing is read or written for it;
+ *              not there: nothing is written for it;
  *   slot_dev:  device int32 [n_tokens]: the row of K and V, as a position of sequence
  *              seq[t] of the cache; -1: K and V are not kept.  No two tokens have the
  *              same row;

@@ -330,6 +330,7 @@ struct RopeLaunch {
     int64_t s_layer, s_b, s_h, s_pos;
     float gain;
     int32_t rot, interleaved, f32, wide;  // wide: 16-byte loads, and rot is a multiple of 16
+    int32_t parts;  // wavefronts of a token
     int32_t n_tokens, n_seqs, max_len, Hq, Hkv, NL;
 };
 int launch_rope_append(const RopeLaunch &p, murmur_stream_t stream);
