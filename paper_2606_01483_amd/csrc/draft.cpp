@@ -66,8 +66,9 @@ int check_tree_sizes(int32_t n_layers, int32_t B, int32_t Hq, int32_t Hkv, int32
     if (Hq / Hkv > kMaxGroup)
         return fail(MURMUR_EUNSUPPORTED, "query heads per KV head %d exceeds %d", Hq / Hkv, kMaxGroup);
     if (max_keep > kMaxKeep) return fail(MURMUR_EUNSUPPORTED, "max_keep %d exceeds %d", max_keep, kMaxKeep);
-    // workgroups, and rows of the merge, in 31 bits
-    if ((double)n_layers * B * Hkv * n_nodes * (Hq / Hkv) > 1073741824.0)
+    // 512 threads for each of the row sets of every (layer, sequence, KV head), in 32 bits
+    const double groups = (double)n_layers * B * Hkv;
+    if (groups * ((n_nodes * (Hq / Hkv) + kTreeRowSet - 1) / kTreeRowSet) > 4194304.0)
         return fail(MURMUR_EINVAL, "problem too large for one launch (n_layers = %d, B = %d, Hq = %d, n_nodes = %d)", n_layers, B,
                     Hq, n_nodes);
     return MURMUR_OK;
@@ -241,8 +242,8 @@ MURMUR_EXPORT int murmur_rope_append(const murmur_rope *rope, const murmur_qkv *
     if (D != kHeadDim) return fail(MURMUR_EUNSUPPORTED, "head_dim %d is not supported (only %d)", D, kHeadDim);
     const int rc = check_cache(kv);
     if (rc != MURMUR_OK) return rc;
-    if ((int64_t)kv->n_layers * n_tokens > ((int64_t)1 << 31))
-        return fail(MURMUR_EINVAL, "n_layers * n_tokens must be at most 2^31");
+    if ((int64_t)kv->n_layers * n_tokens > (1 << 25))
+        return fail(MURMUR_EINVAL, "n_layers * n_tokens must be at most 2^25");
     if (!aligned(pos_dev, 4) || !aligned(slot_dev, 4) || !aligned(seq_dev, 4))
         return fail(MURMUR_EINVAL, "device pointers must be 4-byte aligned");
     if (!aligned(q_out_dev, 16)) return fail(MURMUR_EINVAL, "q_out_dev must be 16-byte aligned");

@@ -664,3 +664,98 @@ class BeamBatch:
         M.murmur_decode_attn_shared(q, self.kv, self.idx, None, self.max_keep, self.B, self.groups, self.Hq, self.Hkv,
                                     self.D, self.wl.scale, self.out, self.out_dtype, self.lse, self.plan,
                                     self.plan_bytes, self.ws, self.ws_bytes, stream)
+
+
+class TreeBatch:
+    """Rounds of speculative decoding on a paged pool, from unrotated projections: prefill() places the prompts of new
+    requests (murmur_paged_reserve, murmur_rope_append); a round is attend(), in which every node of every sequence's
+    tree of drafted tokens attends to the retained cache, its ancestors and itself (reserve for the longest path, rotary
+    positions, murmur_decode_attn_tree), and accept(), which takes over the path that the decoder agrees with
+    (murmur_tree_accept), moves the layouts on and returns the blocks behind the windows (murmur_paged_step_shared).  No
+    host work, so a round can be captured into one HIP graph.
+
+    Memory plumbing only: the pool [NL][n_blocks * block_size][Hkv][D], the block table, counts and free stack, the
+    trees' K and V [NL][B][T][Hkv][D], slot maps, layouts and outputs.  seg [B, 4] are the layouts of the prompts with out_len 1 (the
+    first token, which the prefill gives, is the first root); a row of zeros is a sequence that is not there.  Layouts
+    live on the device (`seg`) and grow with accept()."""
+
+    def __init__(self, seg: np.ndarray, policy: np.ndarray, n_nodes: int, rope: M.murmur_rope, n_layers: int, hq: int, hkv: int,
+                 block_size: int, n_blocks: int, max_len: int, max_keep: int, scale: float, device: str = "cuda",
+                 out_dtype: int = M.MURMUR_DTYPE_F32):
+        self.B, self.T, self.NL, self.Hq, self.Hkv, self.D = len(seg), int(n_nodes), int(n_layers), int(hq), int(hkv), 128
+        self.bs, self.n_blocks, self.max_keep, self.scale, self.out_dtype = int(block_size), int(n_blocks), int(max_keep), float(scale), out_dtype
+        self.rows, self.max_blocks, self.rope = self.n_blocks * self.bs, -(-int(max_len) // self.bs), rope
+        B, T, NL, D, dev = self.B, self.T, self.NL, self.D, torch.device(device)
+
+        def i32(x):
+            return torch.from_numpy(np.ascontiguousarray(x, dtype=np.int32)).to(dev)
+
+        self.seg, self.pol = i32(seg), i32(np.asarray(policy).reshape(-1, 5))
+        self.pol_mode = M.MURMUR_POL_PER_SEQ if self.pol.shape[0] > 1 else 0
+        self.k = torch.zeros((NL, self.rows, hkv, D), dtype=torch.bfloat16, device=dev)
+        self.v = torch.zeros_like(self.k)
+        self.kv = M.make_kv(self.k, self.v, NL, self.rows, (self.rows * hkv * D, 0, D, hkv * D))
+        self.k_tree = torch.zeros((NL, B, T, hkv, D), dtype=torch.bfloat16, device=dev)
+        self.v_tree = torch.zeros_like(self.k_tree)
+        self.tree = M.make_kv(self.k_tree, self.v_tree, NL, B * T, (B * T * hkv * D, 0, D, hkv * D))
+        self.bt = i32(np.full((B, self.max_blocks), -1))
+        self.stack, self.top = i32(np.arange(self.n_blocks)), i32([self.n_blocks])
+        self.ref, self.copied = i32(np.zeros(self.n_blocks)), i32(np.zeros(B))
+        self.q = torch.zeros((NL, B, T, hq, D), dtype=torch.bfloat16, device=dev)
+        self.out = torch.zeros((NL, B, T, hq, D), dtype=torch.bfloat16 if out_dtype == M.MURMUR_DTYPE_BF16 else torch.float32, device=dev)
+        self.lse = torch.zeros((NL, B, T, hq), dtype=torch.float32, device=dev)
+        self.start, self.got = i32(np.zeros(B + 1)), i32(np.zeros(B))
+        self.slot, self.node_slot = i32(np.zeros((B, T))), i32(np.arange(B * T))
+        self.path, self.count, self.last = i32(np.zeros((B, T))), i32(np.zeros(B)), i32(np.zeros(B))
+        self.reserve_bytes = M.murmur_paged_reserve_workspace(B)
+        self.reserve_ws = torch.zeros(self.reserve_bytes // 4, dtype=torch.int32, device=dev)
+        self.ws_bytes = M.murmur_decode_attn_tree_workspace(NL, B, hq, hkv, T, self.max_keep)
+        self.ws = torch.zeros(max(self.ws_bytes, 256) // 4, dtype=torch.int32, device=dev)
+
+    def _root(self):
+        """Positions of the roots, -1 for a sequence that is not there."""
+        s = self.seg
+        return torch.where(s[:, 3] > 0, s[:, 0] + s[:, 1] + s[:, 2] + s[:, 3] - 1, -1)
+
+    def _reserve(self, length, new, per_seq, n_tokens, slot, pos, stream) -> None:
+        M.murmur_paged_reserve(length, new, self.B, self.bt, self.max_blocks, self.bs, self.ref, self.n_blocks, self.stack, self.top,
+                               self.n_blocks, per_seq, n_tokens, self.start, self.got, slot, pos, None, self.reserve_ws,
+                               self.reserve_bytes, stream)
+
+    def prefill(self, q, k, v, q_out, stream=None):
+        """Places the prompts: q, k, v [NL, tokens, heads, D], packed in sequence order; q_out [NL, tokens, Hq, D] takes
+        the rotated queries.  Returns the positions [tokens]."""
+        n = q.shape[1]
+        with BeamBatch._on(stream):
+            new = self._root().clamp_(min=0)
+            length = torch.zeros_like(new)
+            slot, pos = torch.empty(n, dtype=torch.int32, device=new.device), torch.empty(n, dtype=torch.int32, device=new.device)
+        self._reserve(length, new, 0, n, slot, pos, stream)
+        M.murmur_rope_append(self.rope, M.qkv_from_tensors(q, k, v), pos, slot, None, 1, n, self.Hq, self.Hkv, self.D, q_out, self.kv,
+                             stream)
+        return pos
+
+    def attend(self, parent, depth, q, k, v, stream=None) -> None:
+        """parent, depth int32 [B, T] (depth -1 where there is no node); q, k, v [NL, B * T, heads, D]."""
+        with BeamBatch._on(stream):
+            root = self._root()
+            there = (root >= 0).int()
+            pos = torch.where((depth >= 0) & (root >= 0)[:, None], root[:, None] + depth, -1).int()
+            new, length = there * self.T, root.clamp(min=0)
+        self._reserve(length, new, self.T, self.B * self.T, self.slot, None, stream)
+        M.murmur_rope_append(self.rope, M.qkv_from_tensors(q, k, v), pos, self.node_slot, None, 1, self.B * self.T, self.Hq, self.Hkv,
+                             self.D, self.q, self.tree, stream)
+        M.murmur_decode_attn_tree(self.seg, self.pol, self.pol_mode, parent, 1, self.T, self.q, self.kv, self.k_tree, self.v_tree,
+                                  self.bt, self.max_blocks, self.bs, self.max_keep, self.B, self.Hq, self.Hkv, self.D, self.scale,
+                                  self.out, self.out_dtype, self.lse, self.ws, self.ws_bytes, stream)
+
+    def accept(self, parent, token, said, stream=None) -> None:
+        """token, said int32 [B, T]: the nodes' tokens and those that the decoder gives after each.  Leaves path, count and
+        last (the next roots); frees what no step from the new roots on retains."""
+        M.murmur_tree_accept(parent, 1, self.T, token, said, self.slot, self.B, self.k_tree, self.v_tree, self.kv, self.Hkv,
+                             self.path, self.count, self.last, stream)
+        with BeamBatch._on(stream):
+            self.seg[:, 3] += self.count
+        M.murmur_paged_step_shared(self.seg, self.pol, int(self.pol_mode != 0), self.B, self.bt, self.max_blocks, self.bs, self.ref,
+                                   self.n_blocks, self.stack, self.top, self.n_blocks, True, self.copied, None, 0, None, None,
+                                   stream)
