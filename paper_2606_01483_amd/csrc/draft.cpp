@@ -271,11 +271,11 @@ MURMUR_EXPORT int murmur_rope_append(const murmur_rope *rope, const murmur_qkv *
     p.interleaved = rope->interleaved;
     p.f32 = in->dtype == MURMUR_DTYPE_F32;
     const int64_t wide = 16 / (int64_t)size;
-    p.wide = rope->rot_dim % 16 == 0 && aligned(in->q, 16) && aligned(in->k, 16) && aligned(in->v, 16) &&
+    p.wide = aligned(in->q, 16) && aligned(in->k, 16) && aligned(in->v, 16) &&
              in->q_layer % wide == 0 && in->q_token % wide == 0 && in->kv_layer % wide == 0 && in->kv_token % wide == 0;
     // a token's heads to several wavefronts where the tokens leave most of the chip's 8192 without work
     const int64_t items = (int64_t)kv->n_layers * n_tokens;
-    p.parts = p.wide && items <= 1024 ? (Hq + 2 * Hkv + 7) / 8 : 1;
+    p.parts = p.wide && items <= 1024 && (rope->interleaved || rope->rot_dim % 16 == 0) ? (Hq + 2 * Hkv + 7) / 8 : 1;
     p.n_tokens = n_tokens;
     p.n_seqs = n_seqs;
     p.max_len = kv->max_len;

@@ -3,7 +3,8 @@
 //
 //   reserve_group_kernel, reserve_count_kernel, reserve_long_kernel
 //                                              blocks and slot maps for new tokens
-//   rope_wide_kernel, rope_pair_kernel         q and k rotated, K and V into the cache
+//   rope_wide_kernel, rope_mixed_kernel, rope_pair_kernel
+//                                              q and k rotated, K and V into the cache
 //   tree_accept_kernel                         the accepted path into the cache
 #pragma once
 
@@ -374,7 +375,7 @@ __global__ __launch_bounds__(256) void rope_wide_kernel(const RopeLaunch p) {
     if (item >= (int64_t)p.NL * p.n_tokens) return;
     const int part = (int)(task - item * p.parts);
     const int h0 = part * kRopeHeads, h_end = p.parts > 1 ? min(h0 + kRopeHeads, heads) : heads;
-    const bool turns = 16 * u < p.rot;
+    const int turns = kInterleaved ? min(max(p.rot / 2 - 8 * u, 0), 8) : (16 * u < p.rot ? 8 : 0);  // pairs that do
     const int at0 = kInterleaved || !turns ? 16 * u : 8 * u, at1 = kInterleaved || !turns ? 16 * u + 8 : p.rot / 2 + 8 * u;
     RopeToken x;
     x.layer = (int)(item / p.n_tokens);
@@ -390,7 +391,7 @@ __global__ __launch_bounds__(256) void rope_wide_kernel(const RopeLaunch p) {
     };
     uint64_t freq[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) freq[i] = turns ? p.freq[8 * u + i] : 0;
+    for (int i = 0; i < 8; ++i) freq[i] = i < turns ? p.freq[8 * u + i] : 0;
     const int first = h0 + (lane >> 3);
     if (p.parts > 1) load(first);  // before it is known whether the token is there: one round trip fewer
     if (!rope_token(p, part == 0 && lane == 0, x)) return;
@@ -409,9 +410,9 @@ __global__ __launch_bounds__(256) void rope_wide_kernel(const RopeLaunch p) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         float &e = i < 4 ? a[j][2 * i] : b[j][2 * i - 8], &o = i < 4 ? a[j][2 * i + 1] : b[j][2 * i - 7];
-                        const float y = fmaf(e, cos[i], -(o * sin[i]));
-                        o = fmaf(e, sin[i], o * cos[i]);
-                        e = y;
+                        const float y = fmaf(e, cos[i], -(o * sin[i])), z = fmaf(e, sin[i], o * cos[i]);
+                        e = i < turns ? y : e;
+                        o = i < turns ? z : o;
                     }
                 } else {
 #pragma unroll
@@ -425,6 +426,57 @@ __global__ __launch_bounds__(256) void rope_wide_kernel(const RopeLaunch p) {
             store8(to + at0, a[j]);
             store8(to + at1, b[j]);
         }
+    }
+}
+
+// The half layout where the pairs' second elements do not start at a 16-byte chunk: a
+// lane loads, turns and stores the eight elements of a chunk and finds the other one of
+// each pair in LDS.  Lane i computes pair i's sines for the wavefront.  (26 880 tokens
+// of 36 heads, 50 of 128 elements rotated: 98 us, 143 by pairs.)
+template <typename T>
+__global__ __launch_bounds__(256) void rope_mixed_kernel(const RopeLaunch p) {
+    __shared__ float s_head[4][4][kHeadDim];  // four heads a wavefront
+    __shared__ float2 s_turn[4][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int heads = p.Hq + 2 * p.Hkv, half = p.rot / 2, mine = lane >> 4, c0 = 8 * (lane & 15);
+    const int64_t item = (int64_t)blockIdx.x * 4 + wave;
+    if (item >= (int64_t)p.NL * p.n_tokens) return;
+    RopeToken x;
+    x.layer = (int)(item / p.n_tokens);
+    x.t = (int)(item - (int64_t)x.layer * p.n_tokens);
+    if (!rope_token(p, lane == 0, x)) return;
+    // LDS between the lanes of one wavefront, whose accesses are done in order
+    const auto ordered = [] { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
+    if (lane < half) turn_of(p.freq[lane], x.pos, p.gain, s_turn[wave][lane].x, s_turn[wave][lane].y);
+    ordered();
+    float2 turn[8];  // cosine, and the sine that the other element takes
+    int other[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int e = c0 + i;
+        other[i] = e < half ? e + half : e - half;
+        if (e >= p.rot) other[i] = e;
+        turn[i] = e < p.rot ? s_turn[wave][min(e, other[i])] : float2{1.f, 0.f};
+        if (e < half) turn[i].y = -turn[i].y;
+    }
+    for (int h0 = 0; h0 < heads; h0 += 4) {
+        const int h = h0 + mine;
+        float a[8];
+        load8(rope_source<T>(p, x, min(h, heads - 1)) + c0, a);
+        float *head = s_head[wave][mine];
+        *reinterpret_cast<f32x4 *>(head + c0) = f32x4{a[0], a[1], a[2], a[3]};
+        *reinterpret_cast<f32x4 *>(head + c0 + 4) = f32x4{a[4], a[5], a[6], a[7]};
+        ordered();
+        if (h < p.Hq + p.Hkv) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float y = fmaf(a[i], turn[i].x, head[other[i]] * turn[i].y);
+                a[i] = c0 + i < p.rot ? y : a[i];
+            }
+        }
+        ordered();
+        uint16_t *to = h < heads ? rope_target(p, x, h) : nullptr;
+        if (to) store8(to + c0, a);
     }
 }
 
@@ -538,7 +590,10 @@ int launch_paged_reserve(const ReserveLaunch &p, murmur_stream_t stream) {
 int launch_rope_append(const RopeLaunch &p, murmur_stream_t stream) {
     const dim3 grid((unsigned)(((int64_t)p.NL * p.n_tokens * p.parts + 3) / 4)), threads(256);
     const hipStream_t s = (hipStream_t)stream;
-    if (!p.wide) {
+    if (p.wide && !p.interleaved && p.rot % 16 != 0) {
+        if (p.f32) hipLaunchKernelGGL(rope_mixed_kernel<float>, grid, threads, 0, s, p);
+        else hipLaunchKernelGGL(rope_mixed_kernel<uint16_t>, grid, threads, 0, s, p);
+    } else if (!p.wide) {
         if (p.f32) hipLaunchKernelGGL(rope_pair_kernel<float>, grid, threads, 0, s, p);
         else hipLaunchKernelGGL(rope_pair_kernel<uint16_t>, grid, threads, 0, s, p);
     } else if (p.f32) {

@@ -329,7 +329,7 @@ struct RopeLaunch {
     uint16_t *q_out, *k_cache, *v_cache;
     int64_t s_layer, s_b, s_h, s_pos;
     float gain;
-    int32_t rot, interleaved, f32, wide;  // wide: 16-byte loads, and rot is a multiple of 16
+    int32_t rot, interleaved, f32, wide;  // wide: 16-byte loads
     int32_t parts;  // wavefronts of a token
     int32_t n_tokens, n_seqs, max_len, Hq, Hkv, NL;
 };

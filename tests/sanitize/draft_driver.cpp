@@ -34,7 +34,7 @@ int launch_paged_reserve(const ReserveLaunch &p, murmur_stream_t) {
 int launch_rope_append(const RopeLaunch &p, murmur_stream_t) {
     check(((int64_t)p.NL * p.n_tokens * p.parts + 3) / 4 * 256 < (int64_t)1 << 32, "rope: threads");
     check(p.parts >= 1 && (p.parts == 1 || p.parts * 8 >= p.Hq + 2 * p.Hkv), "rope: heads");
-    check(!p.wide || p.rot % 16 == 0, "rope: wide");
+    check(p.parts == 1 || (p.wide && (p.interleaved || p.rot % 16 == 0)), "rope: parts");
     return 0;
 }
 int launch_decode_attn_tree(const TreeLaunch &a, murmur_stream_t) {

@@ -314,22 +314,23 @@ def test_rope_tokens_that_are_not_there_or_not_kept():
 def test_rope_in_place():
     """q_out may be q itself."""
     announce("rope in place")
-    for rot in (128, 50):
-        case = Rope(11, 21, fused=False, rot=rot)
+    for rot, interleaved in ((128, False), (50, False), (50, True), (16, True)):
+        case = Rope(11, 21, fused=False, rot=rot, interleaved=interleaved)
         before = case.q.clone()
         case.out = case.q
         case.run().check(q=before)
 
 
-def test_rope_values_that_are_not_finite():
+@pytest.mark.parametrize("rot,skew", [(64, 0), (50, 0), (50, 1)])
+def test_rope_values_that_are_not_finite(rot, skew):
     """An infinity or a NaN stays in its pair; V and the part that is not rotated pass as they are."""
-    announce("rope not finite")
-    case = Rope(12, 3, rot=64)
+    announce(f"rope not finite, rot {rot} skew {skew}")
+    case = Rope(12, 3, rot=rot, skew=skew)
     case.q[0, 1, 2, 3], case.k[0, 1, 0, 100], case.v[0, 2, 1, 7] = float("nan"), float("inf"), float("-inf")
     case.run()
     out = case.out.cpu()
     bad = torch.zeros_like(out, dtype=torch.bool)
-    bad[0, 1, 2, [3, 35]] = True
+    bad[0, 1, 2, [3, 3 + rot // 2]] = True
     assert torch.equal(~torch.isfinite(out), bad)
     assert float(case.kc[0, 0, case.slot_np[1], 0, 100]) == float("inf") and int((~torch.isfinite(case.kc)).sum()) == 1
     assert float(case.vc[0, 0, case.slot_np[2], 1, 7]) == float("-inf") and int((~torch.isfinite(case.vc)).sum()) == 1
