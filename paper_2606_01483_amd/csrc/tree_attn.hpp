@@ -302,11 +302,20 @@ static __device__ __forceinline__ void tree_store(const TreeLaunch &a, int64_t r
 
 // ---------------------------------------------------------------------------
 // Workgroup: up to 128 query rows of one (layer, sequence, KV head) over one split of
-// the list.  Its wavefronts take the list kWaves / 2 passes (a round)
-// at a time: together they load a round's rows into one of two buffers while they
-// compute the other, and a split of two rounds is on its way as a whole from the
-// start.  They are `ways` ways by rows and the rest by passes, as the rows that are
+// the list.  Its wavefronts take the list kWaves / 2 passes (a round) at a time:
+// together they load a round's rows into one of two buffers while they compute the
+// other.  They are `ways` ways by rows and the rest by passes, as the rows that are
 // there ask for; groups by passes are joined by way of LDS at the end.
+// Large trees are bound by the vector and matrix units: 64 trees of 64 nodes over 2000
+// rows, two layers, 490 us, 480 TFLOP/s (an 8192^3 product reaches 1102), where a pass
+// of two row tiles is 212 vector and 48 matrix instructions, a third of these for the
+// weights' second part.  One tile a wavefront reads K and V from LDS twice as often (64
+// chunks of 64 nodes 807 us, 612 with two); three, at two wavefronts a SIMD, do not fit
+// the registers.  Small ones are bound by latency: of 10 us (16 nodes, 160 rows) 3.4
+// pass before the first rows are on their way (layout, policy and tree; the table's
+// entries; code that is fetched), 0.8 before they are there, 4.5 in six passes, 0.9 in
+// the outputs.  The table's row in LDS, loaded at the start, changed nothing, nor did
+// loads that pass the L2s by.
 // ---------------------------------------------------------------------------
 template <int kWaves>
 struct TreeLds {
@@ -457,6 +466,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_attn_kernel(const TreeLau
             u32x2 vf[16];
             read_v_operands(vf, lds_addr(stage + kTileBytes), n16, c4);
             if (ruled) tree_keep_apart<kTiles>(vf, stage + kTileBytes, allows, w, lane);
+            // ahead of the other wavefront's vector instructions: 31 nodes over 35 000 rows 220 us for four layers, not 230
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int k = 0; k < kTerms; ++k)  // a sum's products apart, since each waits for the one before
 #pragma unroll
@@ -465,6 +476,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_attn_kernel(const TreeLau
                     for (int t = 0; t < kTiles; ++t)
                         w[t].acc[db] = mfma16x16x32(u32x4{vf[2 * db][0], vf[2 * db][1], vf[2 * db + 1][0], vf[2 * db + 1][1]},
                                                     pr[t][k], w[t].acc[db]);
+            __builtin_amdgcn_s_setprio(0);
         }
     }
     if (__ballot(err != 0)) {
@@ -536,7 +548,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_attn_kernel(const TreeLau
 }
 
 // A row by 32 threads, four head dims each, kParts times: each takes every kParts-th
-// split.
+// split.  868 rows of 64 splits 6.9 us (29 MB of partials, the launch), 1344 of five 4.2.
 template <int kParts>
 __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeLaunch a) {
     constexpr int kRows = 8 / kParts, kBatch = 8;

@@ -181,10 +181,11 @@ def test_rows_of_minus_infinity():
     assert torch.isnan(case.out).all() and (case.lse == float("-inf")).all()
 
 
-def test_far_rows():
-    """A pool of more than 2^32 bytes a plane: rows behind 2^31 elements."""
-    announce("far rows")
-    rows, hkv, T = 6_000_000, 4, 3
+@pytest.mark.parametrize("rows", [3_500_000, 6_000_000])
+def test_far_rows(rows):
+    """Pools of more than 2^31 and 2^32 bytes a plane."""
+    announce(f"far rows {rows}")
+    hkv, T = 4, 3
     rng = np.random.default_rng(15)
     case = TreeCase(15, [[2, 60, 0, 5]], [30, 2, 0, OFF, 0], random_tree(rng, T)[None], block=16)
     k = torch.empty((1, rows, hkv, D), dtype=torch.bfloat16, device="cuda")
