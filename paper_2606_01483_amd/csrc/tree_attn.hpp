@@ -307,15 +307,17 @@ static __device__ __forceinline__ void tree_store(const TreeLaunch &a, int64_t r
 // other.  They are `ways` ways by rows and the rest by passes, as the rows that are
 // there ask for; groups by passes are joined by way of LDS at the end.
 // Large trees are bound by the vector and matrix units: 64 trees of 64 nodes over 2000
-// rows, two layers, 490 us, 480 TFLOP/s (an 8192^3 product reaches 1102), where a pass
+// rows, two layers, 486 to 516 us, 491 to 463 TFLOP/s (an 8192^3 product reaches 1102), where a pass
 // of two row tiles is 212 vector and 48 matrix instructions, a third of these for the
 // weights' second part.  One tile a wavefront reads K and V from LDS twice as often (64
 // chunks of 64 nodes 807 us, 612 with two); three, at two wavefronts a SIMD, do not fit
-// the registers.  Small ones are bound by latency: of 10 us (16 nodes, 160 rows) 3.4
-// pass before the first rows are on their way (layout, policy and tree; the table's
-// entries; code that is fetched), 0.8 before they are there, 4.5 in six passes, 0.9 in
-// the outputs.  The table's row in LDS, loaded at the start, changed nothing, nor did
-// loads that pass the L2s by.
+// the registers.  Small ones are bound by latency: of 10 us (16 nodes, 160 rows,
+// clocked in an earlier form) 3.4 pass before the first rows are on their way (layout,
+// policy and tree; the table's entries; code that is fetched), 0.8 before they are
+// there, 4.5 in six passes, 0.9 in the outputs.  The table's row in LDS, loaded at the
+// start, gained nothing, and loads that pass the L2s by cost 7 to 9 % of the 64 chunks
+// of 64 nodes.  A raised wavefront priority around the values' products: 31 nodes over
+// 35 000 rows 2 % faster, the others 0.5 to 2 % slower.
 // ---------------------------------------------------------------------------
 template <int kWaves>
 struct TreeLds {
@@ -466,8 +468,6 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_attn_kernel(const TreeLau
             u32x2 vf[16];
             read_v_operands(vf, lds_addr(stage + kTileBytes), n16, c4);
             if (ruled) tree_keep_apart<kTiles>(vf, stage + kTileBytes, allows, w, lane);
-            // ahead of the other wavefront's vector instructions: 31 nodes over 35 000 rows 220 us for four layers, not 230
-            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int k = 0; k < kTerms; ++k)  // a sum's products apart, since each waits for the one before
 #pragma unroll
@@ -476,7 +476,6 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_attn_kernel(const TreeLau
                     for (int t = 0; t < kTiles; ++t)
                         w[t].acc[db] = mfma16x16x32(u32x4{vf[2 * db][0], vf[2 * db][1], vf[2 * db + 1][0], vf[2 * db + 1][1]},
                                                     pr[t][k], w[t].acc[db]);
-            __builtin_amdgcn_s_setprio(0);
         }
     }
     if (__ballot(err != 0)) {
@@ -548,7 +547,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void tree_attn_kernel(const TreeLau
 }
 
 // A row by 32 threads, four head dims each, kParts times: each takes every kParts-th
-// split.  868 rows of 64 splits 6.9 us (29 MB of partials, the launch), 1344 of five 4.2.
+// split.  868 rows of 64 splits 7.6 us (29 MB of partials, the launch), 5376 of five 5.1.
 template <int kParts>
 __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeLaunch a) {
     constexpr int kRows = 8 / kParts, kBatch = 8;
