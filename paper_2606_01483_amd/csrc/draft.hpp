@@ -364,7 +364,7 @@ static __device__ __forceinline__ void store8(uint16_t *to, const float (&x)[8])
 // 12 sequences 4.0 us, 5.0 with a wavefront each.  A head is eight units
 // of two 16-byte (bf16) chunks, a lane has one of them in every eighth head: eight
 // pairs that turn alike in all heads, so the sines are computed once.  Bound by memory:
-// 27 396 tokens of 36 heads, 505 MB, 95 us, 5.3 TB/s (a plain copy of 4 GiB reaches 4.7).
+// 27 396 tokens of 36 heads, 505 MB, 98 us, 5.2 TB/s (a plain copy of 4 GiB reaches 4.7).
 constexpr int kRopeHeads = 8;
 template <typename T, bool kInterleaved>
 __global__ __launch_bounds__(256) void rope_wide_kernel(const RopeLaunch p) {
