@@ -674,6 +674,9 @@ class TreeBatch:
     (murmur_tree_accept), moves the layouts on and returns the blocks behind the windows (murmur_paged_step_shared).  No
     host work, so a round can be captured into one HIP graph.
 
+    A sequence that reserve refuses in a round (got -1: a pool without room, a table that ends) sits it out: its nodes'
+    outputs are right, but nothing is accepted (count 0), its layout stays and last is its root again.
+
     Memory plumbing only: the pool [NL][n_blocks * block_size][Hkv][D], the block table, counts and free stack, the
     trees' K and V [NL][B][T][Hkv][D], slot maps, layouts and outputs.  seg [B, 4] are the layouts of the prompts with out_len 1 (the
     first token, which the prefill gives, is the first root); a row of zeros is a sequence that is not there.  Layouts
@@ -752,10 +755,14 @@ class TreeBatch:
     def accept(self, parent, token, said, stream=None) -> None:
         """token, said int32 [B, T]: the nodes' tokens and those that the decoder gives after each.  Leaves path, count and
         last (the next roots); frees what no step from the new roots on retains."""
-        M.murmur_tree_accept(parent, 1, self.T, token, said, self.slot, self.B, self.k_tree, self.v_tree, self.kv, self.Hkv,
+        with BeamBatch._on(stream):
+            refused = self.got < 0
+            mine = torch.where(refused[:, None], -1, token)  # a root without a token: no path, no row written
+        M.murmur_tree_accept(parent, 1, self.T, mine, said, self.slot, self.B, self.k_tree, self.v_tree, self.kv, self.Hkv,
                              self.path, self.count, self.last, stream)
         with BeamBatch._on(stream):
             self.seg[:, 3] += self.count
+            self.last.copy_(torch.where(refused, token[:, 0], self.last))
         M.murmur_paged_step_shared(self.seg, self.pol, int(self.pol_mode != 0), self.B, self.bt, self.max_blocks, self.bs, self.ref,
                                    self.n_blocks, self.stack, self.top, self.n_blocks, True, self.copied, None, 0, None, None,
                                    stream)

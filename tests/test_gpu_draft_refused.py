@@ -1,0 +1,134 @@
+"""Rounds of decode.TreeBatch in which murmur_paged_reserve refuses sequences: a pool that runs out and recovers.  A
+sequence that is refused sits the round out (nothing accepted, the same root again) and goes on as if the round had not been."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import draft as OD
+from paper_2606_01483_amd import murmur as M
+from _draft import OFF, i32
+from test_gpu_draft_rounds import SEG, Run, announce, follows
+
+pytestmark = pytest.mark.gpu
+ALL = [OFF, 0, 0, OFF, 0]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    M.lib()
+    yield
+    torch.cuda.synchronize()
+    assert M.murmur_device_error() == 0
+
+
+def empty(batch):
+    """Takes every free block out of the pool; returns them."""
+    held = batch.stack[:int(batch.top)].clone()
+    batch.top.zero_()
+    return held
+
+
+def refill(batch, held):
+    free = torch.cat([held, batch.stack[:int(batch.top)]])
+    batch.stack[:len(free)] = free
+    batch.top.fill_(len(free))
+
+
+def said_of(token):
+    return np.where(token >= 0, follows(token), -1)
+
+
+def check_took(run, parent, token, said, got):
+    """Counts, paths, next roots and layouts; returns the nodes that each live sequence took."""
+    batch, taken = run.batch, {}
+    for b in range(len(run.seg)):
+        live, refused = b in run.live, b in run.live and got[b] < 0
+        path, last = OD.accept(parent[b], token[b], said[b]) if live and not refused else ([], token[b, 0] if refused else -1)
+        assert int(batch.count[b]) == len(path) and int(batch.last[b]) == last, (b, got[b])
+        assert batch.path[b].tolist() == path + [-1] * (run.T - len(path))
+        if live:
+            run.tokens[b] += [int(token[b, t]) for t in path[1:]] + [int(last)] * (len(path) > 0)
+            taken[b] = len(path)
+            assert int(batch.seg[b].sum()) == len(run.tokens[b]), (b, got[b])
+        else:
+            assert int(batch.seg[b].abs().sum()) == 0
+    return taken
+
+
+def one_round(run):
+    """A round against the oracle; what was refused, and the nodes that each live sequence took."""
+    parent, depth, token = run.draft()
+    run.batch.attend(i32(parent), i32(depth), *run.decoder(np.maximum(token, 0)))
+    torch.cuda.synchronize()
+    errors, got = M.murmur_device_error(), run.batch.got.tolist()
+    short = [b for b in run.live if got[b] < 0]
+    assert errors == (M.MURMUR_DEVERR_POOL if short else 0)
+    run.check_outputs(parent, token)  # the cache of a refused sequence is whole, and so are its nodes
+    run.batch.accept(i32(parent), i32(token), i32(said_of(token)))
+    torch.cuda.synchronize()
+    M.murmur_device_error()  # no block for the next root: its next reserve says so
+    return short, check_took(run, parent, token, said_of(token), got)
+
+
+@pytest.mark.parametrize("pol", [ALL, [30, 5, 3, 9, 2]])
+def test_a_pool_that_runs_out_and_recovers(pol):
+    announce(f"a pool that runs out, policy {pol}")
+    run = Run(5, SEG, pol, T=9)
+    refused, out_of = 0, None
+    for turn in range(11):
+        if turn in (2, 7):
+            out_of = empty(run.batch)
+        short, taken = one_round(run)
+        assert out_of is not None or not short
+        refused += len(short)
+        if turn in (5, 8):
+            refill(run.batch, out_of)
+            out_of = None
+        if out_of is None:
+            run.check_cache()
+    assert refused > 2 and min(taken.values()) > 0
+
+
+def test_in_a_graph():
+    """Refusals are the device's to find: the rounds of a captured graph sit them out too."""
+    announce("refused rounds in a graph")
+    seg, T = [s for s in SEG if any(s)], 7
+    eager, graph = Run(6, seg, ALL, T=T), Run(6, seg, ALL, T=T)
+    B = len(seg)
+    parent, depth, token, said = (i32(np.full((B, T), -2)) for _ in range(4))
+    q, k, v = (x.clone() for x in graph.decoder(np.zeros(B * T)))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        graph.batch.attend(parent, depth, q, k, v, side)
+        graph.batch.accept(parent, token, said, side)
+    torch.cuda.synchronize()
+    refused = 0
+    for turn in range(7):
+        if turn == 2:
+            out_of = empty(eager.batch)
+            empty(graph.batch)
+        p, d, t = eager.draft()
+        s, x = said_of(t), eager.decoder(np.maximum(t, 0))
+        eager.batch.attend(i32(p), i32(d), *x)
+        eager.batch.accept(i32(p), i32(t), i32(s))
+        for to, value in ((parent, i32(p)), (depth, i32(d)), (token, i32(t)), (said, i32(s)), (q, x[0]), (k, x[1]), (v, x[2])):
+            to.copy_(value)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        got = eager.batch.got.tolist()
+        refused += sum(x < 0 for x in got)
+        check_took(eager, p, t, s, got)
+        check_took(graph, p, t, s, got)
+        for name in ("out", "lse", "got", "seg", "bt", "ref", "top", "path", "count", "last", "k", "v"):
+            assert torch.equal(getattr(eager.batch, name), getattr(graph.batch, name)), (turn, name)
+        if turn == 4:
+            for x in (eager, graph):
+                refill(x.batch, out_of)
+    assert M.murmur_device_error() == M.MURMUR_DEVERR_POOL and refused > 0
+    eager.check_cache()
