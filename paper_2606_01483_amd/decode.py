@@ -680,7 +680,7 @@ class TreeBatch:
     Memory plumbing only: the pool [NL][n_blocks * block_size][Hkv][D], the block table, counts and free stack, the
     trees' K and V [NL][B][T][Hkv][D], slot maps, layouts and outputs.  seg [B, 4] are the layouts of the prompts with out_len 1 (the
     first token, which the prefill gives, is the first root); a row of zeros is a sequence that is not there.  Layouts
-    live on the device (`seg`) and grow with accept()."""
+    live on the device (`seg`) and grow with accept(); trees and tokens of a row of zeros are not looked at."""
 
     def __init__(self, seg: np.ndarray, policy: np.ndarray, n_nodes: int, rope: M.murmur_rope, n_layers: int, hq: int, hkv: int,
                  block_size: int, n_blocks: int, max_len: int, max_keep: int, scale: float, device: str = "cuda",
@@ -757,7 +757,8 @@ class TreeBatch:
         last (the next roots); frees what no step from the new roots on retains."""
         with BeamBatch._on(stream):
             refused = self.got < 0
-            mine = torch.where(refused[:, None], -1, token)  # a root without a token: no path, no row written
+            out = refused | (self.seg[:, 3] <= 0)
+            mine = torch.where(out[:, None], -1, token)  # a root without a token: no path, no row written
         M.murmur_tree_accept(parent, 1, self.T, mine, said, self.slot, self.B, self.k_tree, self.v_tree, self.kv, self.Hkv,
                              self.path, self.count, self.last, stream)
         with BeamBatch._on(stream):

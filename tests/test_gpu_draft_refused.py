@@ -1,12 +1,13 @@
-"""Rounds of decode.TreeBatch in which murmur_paged_reserve refuses sequences: a pool that runs out and recovers.  A
-sequence that is refused sits the round out (nothing accepted, the same root again) and goes on as if the round had not been."""
+"""Rounds of decode.TreeBatch in which murmur_paged_reserve refuses sequences: a pool that runs out and recovers; rows of
+sequences that are not there.  A sequence that is refused sits the round out (nothing accepted, the same root again) and goes
+on as if the round had not been."""
 import numpy as np
 import pytest
 import torch
 
 from oracle import draft as OD
 from paper_2606_01483_amd import murmur as M
-from _draft import OFF, i32
+from _draft import OFF, i32, random_tree
 from test_gpu_draft_rounds import SEG, Run, announce, follows
 
 pytestmark = pytest.mark.gpu
@@ -132,3 +133,21 @@ def test_in_a_graph():
                 refill(x.batch, out_of)
     assert M.murmur_device_error() == M.MURMUR_DEVERR_POOL and refused > 0
     eager.check_cache()
+
+
+def test_a_row_of_zeros_stays_one():
+    """Trees and tokens of a sequence that is not there are not looked at."""
+    announce("trees of absent sequences")
+    run = Run(10, SEG, ALL, T=6)
+    rng = np.random.default_rng(10)
+    for turn in range(3):
+        parent, depth, token = run.draft()
+        parent[1], depth[1], token[1] = random_tree(rng, 6, wide=1), np.arange(6), follows(5)
+        for t in range(6):
+            token[1, t] = follows(token[1, t - 1]) if t else 5
+        run.batch.attend(i32(parent), i32(depth), *run.decoder(np.maximum(token, 0)))
+        run.batch.accept(i32(parent), i32(token), i32(said_of(token)))
+        torch.cuda.synchronize()
+        assert M.murmur_device_error() == 0
+        check_took(run, parent, token, said_of(token), run.batch.got.tolist())
+        run.check_cache()
