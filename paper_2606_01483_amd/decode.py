@@ -727,13 +727,16 @@ class TreeBatch:
 
     def prefill(self, q, k, v, q_out, stream=None):
         """Places the prompts: q, k, v [NL, tokens, heads, D], packed in sequence order; q_out [NL, tokens, Hq, D] takes
-        the rotated queries.  Returns the positions [tokens]."""
+        the rotated queries.  Returns the positions [tokens].  A sequence whose prompt is refused (got -1) is not there from
+        then on: its layout becomes zeros."""
         n = q.shape[1]
         with BeamBatch._on(stream):
             new = self._root().clamp_(min=0)
             length = torch.zeros_like(new)
             slot, pos = torch.empty(n, dtype=torch.int32, device=new.device), torch.empty(n, dtype=torch.int32, device=new.device)
         self._reserve(length, new, 0, n, slot, pos, stream)
+        with BeamBatch._on(stream):
+            self.seg.mul_((self.got >= 0).int()[:, None])
         M.murmur_rope_append(self.rope, M.qkv_from_tensors(q, k, v), pos, slot, None, 1, n, self.Hq, self.Hkv, self.D, q_out, self.kv,
                              stream)
         return pos

@@ -1,6 +1,6 @@
-"""Rounds of decode.TreeBatch in which murmur_paged_reserve refuses sequences: a pool that runs out and recovers; rows of
-sequences that are not there.  A sequence that is refused sits the round out (nothing accepted, the same root again) and goes
-on as if the round had not been."""
+"""Rounds of decode.TreeBatch in which murmur_paged_reserve refuses sequences: a pool that runs out and recovers, prompts
+that find no room; rows of sequences that are not there.  A sequence that is refused sits the round out (nothing accepted, the
+same root again) and goes on as if the round had not been."""
 import numpy as np
 import pytest
 import torch
@@ -133,6 +133,21 @@ def test_in_a_graph():
                 refill(x.batch, out_of)
     assert M.murmur_device_error() == M.MURMUR_DEVERR_POOL and refused > 0
     eager.check_cache()
+
+
+def test_prompts_without_room():
+    """A prompt that is refused is not there in the rounds that follow; the others are as if it had never been."""
+    announce("a refused prompt")
+    run = Run(9, SEG, ALL, T=6, n_blocks=20)  # nine for the first; the third needs twelve
+    torch.cuda.synchronize()
+    # the fourth needs seven, so it is refused with the third
+    assert M.murmur_device_error() == M.MURMUR_DEVERR_POOL and run.batch.got.tolist() == [67, 0, -1, -1]
+    assert run.batch.seg.tolist() == [SEG[0], [0] * 4, [0] * 4, [0] * 4]
+    run.live = [0]
+    for turn in range(4):
+        short, taken = one_round(run)
+        assert not short and taken[0] > 0
+        run.check_cache()
 
 
 def test_a_row_of_zeros_stays_one():
