@@ -669,7 +669,7 @@ class BeamBatch:
 class TreeBatch:
     """Rounds of speculative decoding on a paged pool, from unrotated projections: prefill() places the prompts of new
     requests (murmur_paged_reserve, murmur_rope_append); a round is attend(), in which every node of every sequence's
-    tree of drafted tokens attends to the retained cache, its ancestors and itself (reserve for the longest path, rotary
+    tree of drafted tokens attends to the retained cache, its ancestors and itself (reserve for the deepest path, rotary
     positions, murmur_decode_attn_tree), and accept(), which takes over the path that the decoder agrees with
     (murmur_tree_accept), moves the layouts on and returns the blocks behind the windows (murmur_paged_step_shared).  No
     host work, so a round can be captured into one HIP graph.
@@ -742,12 +742,12 @@ class TreeBatch:
         return pos
 
     def attend(self, parent, depth, q, k, v, stream=None) -> None:
-        """parent, depth int32 [B, T] (depth -1 where there is no node); q, k, v [NL, B * T, heads, D]."""
+        """parent, depth int32 [B, T] (depth: nodes above a node, -1 where there is none); q, k, v [NL, B * T, heads, D]."""
         with BeamBatch._on(stream):
             root = self._root()
-            there = (root >= 0).int()
             pos = torch.where((depth >= 0) & (root >= 0)[:, None], root[:, None] + depth, -1).int()
-            new, length = there * self.T, root.clamp(min=0)
+            new = torch.where(root >= 0, depth.amax(1) + 1, 0).int()
+            length = root.clamp(min=0)
         self._reserve(length, new, self.T, self.B * self.T, self.slot, None, stream)
         M.murmur_rope_append(self.rope, M.qkv_from_tensors(q, k, v), pos, self.node_slot, None, 1, self.B * self.T, self.Hq, self.Hkv,
                              self.D, self.q, self.tree, stream)

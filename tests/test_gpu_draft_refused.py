@@ -1,12 +1,14 @@
-"""Rounds of decode.TreeBatch in which murmur_paged_reserve refuses sequences: a pool that runs out and recovers, prompts
-that find no room; rows of sequences that are not there.  A sequence that is refused sits the round out (nothing accepted, the
-same root again) and goes on as if the round had not been."""
+"""Rounds of decode.TreeBatch in which murmur_paged_reserve refuses sequences: a pool that runs out and recovers, a table
+that ends, prompts that find no room, rows of sequences that are not there.  A sequence that is refused sits the round out
+(nothing accepted, the same root again) and goes on as if the round had not been."""
 import numpy as np
 import pytest
 import torch
 
+import test_gpu_draft_rounds as rounds
 from oracle import draft as OD
 from paper_2606_01483_amd import murmur as M
+from paper_2606_01483_amd.decode import TreeBatch
 from _draft import OFF, i32, random_tree
 from test_gpu_draft_rounds import SEG, Run, announce, follows
 
@@ -133,6 +135,72 @@ def test_in_a_graph():
                 refill(x.batch, out_of)
     assert M.murmur_device_error() == M.MURMUR_DEVERR_POOL and refused > 0
     eager.check_cache()
+
+
+def bush(T, deep):
+    """A chain of `deep` nodes behind the root, the rest children of the root."""
+    parent = np.zeros(T, dtype=np.int32)
+    parent[0] = -1
+    parent[1:deep + 1] = np.arange(deep)
+    depth = np.ones(T, dtype=np.int32)
+    depth[:deep + 1] = np.arange(deep + 1)
+    return parent, depth
+
+
+@pytest.mark.parametrize("deep", [0, 1, 4])
+def test_a_round_asks_for_its_deepest_path(deep):
+    """Blocks are taken for the deepest path's positions, not for every node; the last positions of a table are used."""
+    announce(f"deepest path {deep}")
+    seg, T, block = [[0, 60, 2, 1], [3, 0, 0, 1]], 16, 4
+    run = Run(7, seg, ALL, T=T, block=block)
+    if deep == 0:
+        parent, depth = np.full((2, T), -2, dtype=np.int32), np.full((2, T), -1, dtype=np.int32)
+        parent[:, 0], depth[:, 0] = -1, 0
+    else:
+        parent, depth = (np.stack([x, x]) for x in bush(T, deep))
+    for turn in range(3):
+        token = np.full((2, T), 1)
+        token[:, 0] = [x[-1] for x in run.tokens]
+        for t in range(1, deep + 1):
+            token[:, t] = follows(token[:, t - 1])
+        before = [len(x) for x in run.tokens]
+        run.batch.attend(i32(parent), i32(depth), *run.decoder(np.maximum(token, 0)))
+        torch.cuda.synchronize()
+        assert run.batch.got.tolist() == [deep + 1] * 2 and M.murmur_device_error() == 0
+        table = run.batch.bt.cpu().numpy()
+        for b in range(2):
+            assert (table[b] >= 0).sum() == -(-(before[b] + deep) // block)
+        run.check_outputs(parent, token)
+        run.batch.accept(i32(parent), i32(token), i32(said_of(token)))
+        torch.cuda.synchronize()
+        assert M.murmur_device_error() == 0
+        assert min(check_took(run, parent, token, said_of(token), [T, T]).values()) == deep + 1
+        run.check_cache()
+
+
+def test_the_end_of_the_table(monkeypatch):
+    """A path that ends in the table's last position is served; a longer one is refused, and a shorter one goes on."""
+    announce("end of the table")
+    T, limit = 8, 48
+    monkeypatch.setattr(rounds, "TreeBatch", lambda *a, max_len, **kw: TreeBatch(*a, max_len=limit, **kw))
+    run = Run(8, [[4, 36, 2, 1]], ALL, T=T)  # the root at 42; 42 .. 47 are left
+    for deep, served in ((7, False), (3, True), (4, False), (1, True)):  # the root then at 46 and 48
+        parent, depth = (x[None] for x in bush(T, deep))
+        token = np.full((1, T), 1)
+        token[0, 0] = run.tokens[0][-1]
+        for t in range(1, deep + 1):
+            token[:, t] = follows(token[:, t - 1])
+        run.batch.attend(i32(parent), i32(depth), *run.decoder(token))
+        torch.cuda.synchronize()
+        assert M.murmur_device_error() == (0 if served else M.MURMUR_DEVERR_BLOCK)
+        got = run.batch.got.tolist()
+        assert got == [deep + 1 if served else -1]
+        run.check_outputs(parent, token)
+        run.batch.accept(i32(parent), i32(token), i32(said_of(token)))
+        torch.cuda.synchronize()
+        assert M.murmur_device_error() == (M.MURMUR_DEVERR_BLOCK if run.batch.seg.sum() > limit else 0)  # no row for the next root
+        assert check_took(run, parent, token, said_of(token), got)[0] == (deep + 1 if served else 0)
+    assert len(run.tokens[0]) == limit + 1
 
 
 def test_prompts_without_room():
