@@ -689,6 +689,8 @@ class TreeBatch:
         self.bs, self.n_blocks, self.max_keep, self.scale, self.out_dtype = int(block_size), int(n_blocks), int(max_keep), float(scale), out_dtype
         self.rows, self.max_blocks, self.rope = self.n_blocks * self.bs, -(-int(max_len) // self.bs), rope
         B, T, NL, D, dev = self.B, self.T, self.NL, self.D, torch.device(device)
+        if np.shape(policy) not in ((5,), (1, 5), (B, 5)):  # freed blocks are gone in every layer
+            raise ValueError("policy must be one record or one per sequence")
 
         def i32(x):
             return torch.from_numpy(np.ascontiguousarray(x, dtype=np.int32)).to(dev)

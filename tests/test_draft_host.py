@@ -217,3 +217,16 @@ def test_projections_from_tensors():
     for q, k, v in ((x.float(), x, x), (x, x, x[:, :, :6]), (x.half(), x.half(), x.half()), (x.transpose(1, 2), x, x), (x[..., ::2], x, x)):
         with pytest.raises(ValueError):
             M.qkv_from_tensors(q, k, v)
+
+
+@pytest.mark.parametrize("shape", [(2, 5), (4, 5), (2, 3, 5), (15,), (3, 4), (0, 5)])
+def test_policies_of_a_batch_of_trees(shape):
+    """Records for another number of sequences would be read past their end, those of layers for sequences."""
+    from paper_2606_01483_amd.decode import TreeBatch
+    seg = np.array([[4, 30, 0, 1]] * 3)
+    rest = dict(n_nodes=4, rope=rope(), n_layers=2, hq=8, hkv=2, block_size=8, n_blocks=16, max_len=64, max_keep=40, scale=1.0,
+                device="cpu")
+    with pytest.raises(ValueError):
+        TreeBatch(seg, np.full(shape, -1), **rest)
+    for good in ((5,), (1, 5), (3, 5)):
+        assert TreeBatch(seg, np.full(good, -1), **rest).pol.shape[0] == (3 if good == (3, 5) else 1)
