@@ -151,8 +151,9 @@ int murmur_rope_append(const murmur_rope *rope, const murmur_qkv *in, const int3
  * Another tree is invalid (MURMUR_DEVERR_TREE for its sequence). */
 
 /* Workspace bytes of murmur_decode_attn_tree (may be 0): 256-byte aligned, not
- * initialised.  The sizes grow with B, n_nodes and max_keep; calls that run at the same
- * time need workspaces of their own. */
+ * initialised; a larger one is fine.  The sizes grow with n_layers, B, n_nodes and
+ * max_keep, up to 98 MiB, so the workspace of the largest call serves every smaller one
+ * of the same heads.  Calls that run at the same time need workspaces of their own. */
 int murmur_decode_attn_tree_workspace(int32_t n_layers, int32_t B, int32_t Hq, int32_t Hkv, int32_t n_nodes,
                                       int32_t max_keep, size_t *bytes);
 

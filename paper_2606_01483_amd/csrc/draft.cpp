@@ -99,7 +99,7 @@ TreePlan tree_plan(int32_t n_layers, int32_t B, int32_t Hq, int32_t Hkv, int32_t
     for (int pair = 0; pair < 2; ++pair) {
         const int64_t slots = (pair + 1) * kRoundWorkgroups;
         const double pass_us = pair ? 1.25 + 0.65 * full : 0.55 + 0.75 * full;
-        for (int fill = 0; fill <= 3; ++fill) {
+        for (int fill = 0; fill <= kTreeFills; ++fill) {
             const int64_t s = std::max<int64_t>(1, std::min(fill * slots / sets, most));
             const double merge_us = s > 1 ? 4.0 + (double)(groups * s * rows) * 2 * (kHeadDim + 2) * sizeof(float) / 4e6 : 0.0;
             const double us = 7.0 + (double)((sets * s + slots - 1) / slots) * (double)((passes + s - 1) / s) * pass_us + merge_us;
@@ -110,6 +110,11 @@ TreePlan tree_plan(int32_t n_layers, int32_t B, int32_t Hq, int32_t Hkv, int32_t
             }
         }
     }
+    // The bytes of calls of these sizes and smaller ones: the estimate may cut the lists of a smaller batch where it leaves
+    // those of a larger one whole, so the largest number of partial rows is bounded by what does grow.  A list is cut into
+    // at most `most` parts, and only while the parts of all row sets fill the chip's slots at most kTreeFills times.
+    const int64_t parts = std::min(groups * rows * std::max<int64_t>(most, 1), kTreeFills * 2 * kRoundWorkgroups * (int64_t)kTreeRowSet);
+    p.serves = most > 1 ? round_up((size_t)parts * (kHeadDim + 2) * sizeof(float), 256) : 0;
     p.units = groups * p.n_split;
     if (p.n_split > 1) {
         p.o_bytes = (size_t)p.units * (size_t)rows * kHeadDim * sizeof(float);
@@ -292,7 +297,7 @@ MURMUR_EXPORT int murmur_decode_attn_tree_workspace(int32_t n_layers, int32_t B,
     if (!bytes) return fail(MURMUR_EINVAL, "bytes must not be NULL");
     const int rc = check_tree_sizes(n_layers, B, Hq, Hkv, n_nodes, max_keep);
     if (rc != MURMUR_OK) return rc;
-    *bytes = tree_plan(n_layers, B, Hq, Hkv, n_nodes, max_keep).total;
+    *bytes = tree_plan(n_layers, B, Hq, Hkv, n_nodes, max_keep).serves;
     return ok();
 }
 

@@ -363,12 +363,14 @@ struct DivideBy {
 enum TreeShape : int32_t { kTreeFew, kTreeWide, kTreePair };  // workgroups of 8 wavefronts (one or two row tiles each), of 4 (two)
 constexpr int kTreeRowSet = 128;     // rows of a workgroup
 constexpr int kMaxTreeSplits = 64;
+constexpr int kTreeFills = 3;        // times that the splits of all row sets fill the chip at most
 constexpr int kTreeMergeWhole = 8;   // splits up to which one thread joins four head dims of a row
 struct TreePlan {
     TreeShape shape;
     int32_t n_split, row_sets;
     int64_t units;  // (layer, sequence, KV head) groups times splits
     size_t o_bytes, total;
+    size_t serves;  // bytes that serve every call of at most these sizes
 };
 TreePlan tree_plan(int32_t n_layers, int32_t B, int32_t Hq, int32_t Hkv, int32_t n_nodes, int32_t max_keep);
 struct TreeLaunch {

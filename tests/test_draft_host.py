@@ -165,6 +165,27 @@ def test_workspaces():
             M.murmur_decode_attn_tree_workspace(*args)
 
 
+def test_the_largest_workspace_serves_smaller_calls(route):
+    """Sizes grow with the layers, the batch, the nodes and the lists: what a caller allocates once is enough for each call."""
+    at = lambda nl, B, T, keep, hq=28, hkv=4: M.murmur_decode_attn_tree_workspace(nl, B, hq, hkv, T, keep)  # noqa: E731
+    for sizes in ([(1, B, 16, 900) for B in range(1, 130)], [(1, 12, T, 2000) for T in range(1, 65)], [(nl, 3, 9, 700) for nl in range(1, 99)],
+                  [(1, 12, 16, keep) for keep in range(1, 5000, 7)], [(1, 1, 31, 1 << i) for i in range(29)]):
+        got = [at(*x) for x in sizes]
+        assert got == sorted(got), sizes[0]
+    rng = np.random.default_rng(3)
+    for _ in range(3000):
+        hkv = int(rng.integers(1, 9))
+        hq = hkv * int(rng.integers(1, 17))
+        large = [int(np.exp2(rng.uniform(0, top))) for top in (5, 8, 6, 17)]
+        small = [int(rng.integers(1, x + 1)) for x in large]
+        most = at(*large, hq, hkv)
+        assert at(*small, hq, hkv) <= most <= 98 << 20, (small, large, hq, hkv)
+        nl, B, T, keep = small
+        got = outcome("murmur_decode_attn_tree", kv=kv(n_layers=nl), B=B, n_nodes=T, max_keep=keep, Hq=hq, Hkv=hkv, ws_dev=FAKE if most else None,
+                      ws_bytes=most)
+        assert got[0] == M.MURMUR_EHIP, (small, large, hq, hkv, got)
+
+
 # ---- the rotation's table ------------------------------------------------------------------------------------------
 
 def as_turns(freq):
