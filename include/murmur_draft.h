@@ -78,9 +78,11 @@ enum {
     MURMUR_ROPE_YARN = 4,   /* the same, and a gain of 1 + 0.1 ln(factor) on the rotated part of q and of k */
 };
 
-/* Host only: the table of a rotation.  freq[i] is f_i as a fraction of 2^64, rounded to
- * nearest, so that position p's turn is the fraction p * freq[i] mod 2^64, exact in
- * integers: far positions lose nothing.
+/* Host only: the table of a rotation.  freq[i] is f_i as a fraction of 2^64, within two
+ * steps of it, and position p's turn is the fraction p * freq[i] mod 2^64, an exact
+ * integer product: at position 2^31 it is within 2^-32 of a turn.  (The bands are linear
+ * in the turns n_i, as Peng et al. give them; a ramp over the pair's index is a table of
+ * the caller's own.)
  *   rot_dim: even, in [2, 128]; base > 1; factor >= 1 (ignored by MURMUR_ROPE_PLAIN);
  *   original_len, slow_turns, fast_turns: of MURMUR_ROPE_BANDS and MURMUR_ROPE_YARN,
  *            0 < original_len, 0 <= slow_turns < fast_turns (ignored by the others);
@@ -119,8 +121,9 @@ typedef struct murmur_qkv {
 } murmur_qkv;
 
 /* Rotates q and k of every token to its position, in every layer, and writes K and V
- * into the cache rows of a slot map, all in one launch.  The turns are exact (see
- * murmur_rope_freqs_host), sines and products fp32; bf16 results are rounded once.
+ * into the cache rows of a slot map, all in one launch.  The turns are the table's, cut to
+ * 2^-32 of one (see murmur_rope_freqs_host), sines and products fp32; bf16 results are
+ * rounded once.
  *   pos_dev:   device int32 [n_tokens]: rotary positions; a token of a negative one is
  *              not there: nothing is written for it;
  *   slot_dev:  device int32 [n_tokens]: the row of K and V, as a position of sequence

@@ -1,6 +1,7 @@
 // C ABI of requests into a paged pool, rotary positions and trees of drafted tokens
 // (include/murmur_draft.h): argument checks, buffer sizes and dispatch.  As in api.cpp,
 // every check runs before the first HIP call.
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -205,17 +206,19 @@ MURMUR_EXPORT int murmur_rope_freqs_host(int32_t rot_dim, double base, int32_t k
         return fail(MURMUR_EINVAL, "original_len must be finite and positive");
     if (bands && (!(slow_turns >= 0.0) || !(fast_turns > slow_turns) || !isfinite(fast_turns)))
         return fail(MURMUR_EINVAL, "slow_turns must be at least 0 and fast_turns finite and above it");
-    const double two_pi = 6.283185307179586476925;
-    if (kind == MURMUR_ROPE_BASE && rot_dim > 2) base *= pow(factor, rot_dim / (rot_dim - 2.0));
-    if (!isfinite(base)) return fail(MURMUR_EINVAL, "base and factor are too large");
+    // In long double, whose 64 bits keep a turn of up to 1 / (2 pi) to a fraction of the table's step.
+    const long double two_pi = 6.283185307179586476925286766559L;
+    long double b = base;
+    if (kind == MURMUR_ROPE_BASE && rot_dim > 2) b *= powl(factor, rot_dim / (rot_dim - 2.0L));
+    if (!(b <= DBL_MAX)) return fail(MURMUR_EINVAL, "base and factor are too large");
     for (int i = 0; i < rot_dim / 2; ++i) {
-        double f = pow(base, -2.0 * i / rot_dim) / two_pi;
+        long double f = powl(b, -2.0L * i / rot_dim) / two_pi;
         if (kind == MURMUR_ROPE_LINEAR) f /= factor;
         if (bands) {
-            const double keep = std::min(1.0, std::max(0.0, (original_len * f - slow_turns) / (fast_turns - slow_turns)));
-            f = f * keep + f / factor * (1.0 - keep);
+            const long double keep = std::min(1.0L, std::max(0.0L, (original_len * f - slow_turns) / ((long double)fast_turns - slow_turns)));
+            f = f * keep + f / factor * (1.0L - keep);
         }
-        freq[i] = (uint64_t)nearbyint(ldexp(f, 64));  // f <= 1 / (2 pi)
+        freq[i] = (uint64_t)nearbyintl(ldexpl(f, 64));  // f <= 1 / (2 pi)
     }
     *gain = kind == MURMUR_ROPE_YARN ? (float)(1.0 + 0.1 * log(factor)) : 1.f;
     return ok();

@@ -4,6 +4,7 @@ import ctypes
 import math
 import os
 import re
+from decimal import Decimal, localcontext
 
 import numpy as np
 import pytest
@@ -213,6 +214,39 @@ def test_frequencies(rot, base):
     close(M.MURMUR_ROPE_YARN, plain * (keep + (1 - keep) / 8), gain=1 + 0.1 * math.log(8))
     keep = np.clip((4096 * plain - 0.5) / 3.5, 0, 1)
     close(M.MURMUR_ROPE_BANDS, plain * (keep + (1 - keep) / 8), slow_turns=0.5, fast_turns=4.0)
+
+
+def in_60_digits(rot, base, kind, factor=1.0, original=0.0, slow=1.0, fast=32.0):
+    """The table's entries in steps of 2^-64, unrounded."""
+    with localcontext() as c:
+        c.prec = 60
+        pi = Decimal("3.14159265358979323846264338327950288419716939937510582097494")
+        b, factor, slow, fast = Decimal(base), Decimal(factor), Decimal(slow), Decimal(fast)
+        if kind == M.MURMUR_ROPE_BASE and rot > 2:
+            b *= (factor.ln() * rot / (rot - 2)).exp()
+        got = []
+        for i in range(rot // 2):
+            f = (b.ln() * -2 * i / rot).exp() / (2 * pi)
+            if kind == M.MURMUR_ROPE_LINEAR:
+                f /= factor
+            if kind in (M.MURMUR_ROPE_BANDS, M.MURMUR_ROPE_YARN):
+                keep = min(Decimal(1), max(Decimal(0), (Decimal(original) * f - slow) / (fast - slow)))
+                f = f * keep + f / factor * (1 - keep)
+            got.append(f * 2 ** 64)
+        return got
+
+
+@pytest.mark.parametrize("kind", [M.MURMUR_ROPE_PLAIN, M.MURMUR_ROPE_LINEAR, M.MURMUR_ROPE_BASE, M.MURMUR_ROPE_BANDS, M.MURMUR_ROPE_YARN])
+@pytest.mark.parametrize("rot", [2, 50, 64, 128])
+@pytest.mark.parametrize("base", [1.5, 1e4, 5e5, 1e6])
+def test_frequencies_to_two_steps(rot, base, kind):
+    """Within two steps of 2^-64, so that position 2^31 is turned to 2^-32 of a turn.  A value of at most 2^61.4 steps takes
+    roundings of 2^-64 of it, 0.16 steps each: the power (an ulp, two of them), its argument (ln(base) x base^-x / (2 pi) of
+    them, at most 0.06 steps; three times that where the base is a product of a power), two divisions; in the bands a share's
+    six, of frequencies below 32 / 4096, and three more; the last rounding half a step.  0.5 + 0.32 + 0.18 + 0.32 + 0.48."""
+    f, _ = M.murmur_rope_freqs_host(rot, base, kind, 8.0, 4096.0)
+    off = [abs(int(x) - want) for x, want in zip(f, in_60_digits(rot, base, kind, 8.0, 4096.0))]
+    assert max(off) <= 2, float(max(off))
 
 
 def test_the_slowest_pair_takes_the_factor():
