@@ -203,7 +203,8 @@ int murmur_decode_attn_tree(const murmur_seg *seg_dev, const murmur_policy *pol_
  *   next_dev:  device int32 [B][n_nodes]: the token that the decoder gives after each;
  *   slot_dev:  device int32 [B][n_nodes]: the cache rows of the path's first, second,
  *              ... node, as positions of sequence b of the cache, all different; -1: not
- *              kept;
+ *              kept, but counted (the root of a sequence that murmur_paged_reserve has
+ *              refused is therefore given a negative token: it sits the round out);
  *   kv:        the cache, written (n_layers of it), as murmur_rope_append;
  *   path_dev:  device int32 [B][n_nodes], output: the path's nodes, then -1;
  *   count_dev, last_dev: device int32 [B], outputs: nodes of the path, and the token

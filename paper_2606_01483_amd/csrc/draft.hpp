@@ -361,7 +361,8 @@ static __device__ __forceinline__ void store8(uint16_t *to, const float (&x)[8])
 
 // A wavefront per (layer, token), or kRopeHeads heads of one (p.parts of them), which
 // takes fewer round trips to memory where there are few tokens: the current token of
-// 12 sequences 4.0 us, 5.0 with a wavefront each.  A head is eight units
+// 12 sequences 4.0 us, 5.0 with a wavefront each (of bf16 a lane then loads a second
+// head, which is another wavefront's to store).  A head is eight units
 // of two 16-byte (bf16) chunks, a lane has one of them in every eighth head: eight
 // pairs that turn alike in all heads, so the sines are computed once.  Bound by memory:
 // 27 396 tokens of 36 heads, 505 MB, 98 us, 5.2 TB/s (a plain copy of 4 GiB reaches 4.7).
@@ -519,7 +520,9 @@ __global__ __launch_bounds__(256) void rope_pair_kernel(const RopeLaunch p) {
 
 // ---------------------------------------------------------------------------
 // accept.  A wavefront follows the path from the root, a step a ballot; every
-// workgroup of a sequence does so for itself, then they copy the path's rows.
+// workgroup of a sequence does so for itself, then they copy the path's rows.  Bound by
+// round trips: a workgroup's planes one after the other, since a store may be to what
+// the next load reads (64 sequences, 56 planes, 3.3 rows each: 10.0 us, 2.4 TB/s).
 // ---------------------------------------------------------------------------
 constexpr int kAcceptPlanes = 4;  // (layer, K or V) planes of a workgroup
 
@@ -573,7 +576,9 @@ __global__ __launch_bounds__(256) void tree_accept_kernel(const AcceptLaunch p) 
 int launch_paged_reserve(const ReserveLaunch &p, murmur_stream_t stream) {
     const hipStream_t s = (hipStream_t)stream;
     const dim3 groups((unsigned)((p.B + kReserveGroup - 1) / kReserveGroup)), threads(kReserveThreads);
-    // 12 prompts of 2283 tokens: 6.1 us behind the count's 3.3; in one launch, a wavefront each, 14.2
+    // 12 prompts of 2283 tokens: 6.1 us behind the count's 3.3; in one launch, a wavefront each, 14.2.  The map's length
+    // stands for the sequences', which only the device knows: a long prompt among short requests is one wavefront's work
+    // (27 000 tokens and 127 single ones 98 us, and 8 single ones, a workgroup each, 20).
     const bool few = p.n_tokens / p.B <= 256;
     if (few && groups.x == 1) {
         hipLaunchKernelGGL(reserve_group_kernel<false>, groups, threads, 0, s, p);

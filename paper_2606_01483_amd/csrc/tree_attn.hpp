@@ -307,7 +307,7 @@ static __device__ __forceinline__ void tree_store(const TreeLaunch &a, int64_t r
 // other.  They are `ways` ways by rows and the rest by passes, as the rows that are
 // there ask for; groups by passes are joined by way of LDS at the end.
 // Large trees are bound by the vector and matrix units: 64 trees of 64 nodes over 2000
-// rows, two layers, 486 to 500 us, 491 to 477 TFLOP/s (an 8192^3 product reaches 1102), where a pass
+// rows, two layers, 489 to 500 us, 488 to 477 TFLOP/s (an 8192^3 product reaches 1102), where a pass
 // of two row tiles is 212 vector and 48 matrix instructions, a third of these for the
 // weights' second part.  One tile a wavefront reads K and V from LDS twice as often (64
 // chunks of 64 nodes 807 us, 612 with two); three, at two wavefronts a SIMD, do not fit
