@@ -183,7 +183,8 @@ int murmur_decode_attn_tree_workspace(int32_t n_layers, int32_t B, int32_t Hq, i
  *   ws_dev, ws_bytes: see murmur_decode_attn_tree_workspace;
  *   every other argument as murmur_decode_step.
  * Accumulation is fp32 throughout.  Errors as murmur_decode_attn.  Device errors, each
- * with NaN outputs for the sequence's nodes: MURMUR_DEVERR_POLICY, MURMUR_DEVERR_TREE,
+ * with NaN outputs for the sequence's nodes: MURMUR_DEVERR_POLICY (also for a layout
+ * that ends within 64 positions of 2^31, or a list within 96), MURMUR_DEVERR_TREE,
  * MURMUR_DEVERR_POSITION (a retained position outside [0, max_len)),
  * MURMUR_DEVERR_BLOCK (one without a block, or past max_blocks). */
 int murmur_decode_attn_tree(const murmur_seg *seg_dev, const murmur_policy *pol_dev, int32_t pol_per_seq,

@@ -127,6 +127,7 @@ static __device__ __forceinline__ TreeList tree_list(const murmur_seg &s, const 
     l.b1 = pre + rg[3] + rg[5];
     l.c0 = l.b1 + mid + sinks;
     l.n0 = l.b1 + mid + rg[9] + rg[11];
+    if (l.n0 > 0x7fffffff - kMaxNodes - kWaveTile) l.err |= MURMUR_DEVERR_POLICY;  // ranks, to the end of the last pass, are 32 bits
     l.count = l.n0 + l.live;
     return l;
 }

@@ -76,3 +76,25 @@ def test_weights_of_fp32_outputs(name):
             w = np.exp(-SCALE * t)
             assert np.abs(case.out.cpu().numpy() * (1 + w) / w - 1).max() <= BOUND, (top, low, t)
             assert np.abs(case.lse.cpu().numpy() - np.log1p(w)).max() <= BOUND, (top, low, t)
+
+
+@pytest.mark.parametrize("total,pol,good", [(2 ** 31 - 65, [20, 3, 1, 9, 0], True), (2 ** 31 - 64, [20, 3, 1, 9, 0], False),
+                                            (2 ** 31 - 65, ALL, False), (2 ** 31 - 1, ALL, False)])
+def test_the_longest_layouts(total, pol, good):
+    """Positions to the deepest node's, and the ranks of a list to the end of its last pass, are 32-bit numbers: what is longer
+    is an error, and nothing of it is read."""
+    print(f"\n[case] layout of {total}, policy {pol}", flush=True)
+    T, block = 40, 1 << 16
+    case = TreeCase(1, [[2, 100, 0, 30]], [20, 3, 1, 9, 0], random_tree(np.random.default_rng(40), T), hq=4, hkv=1, block=block)
+    case.k.nan_to_num_(nan=0.25)
+    case.v.nan_to_num_(nan=-0.5)
+    # every column of a table to 2^31 names one block
+    case.cols, case.table = 1 << 15, case.table.expand(1, 1 << 15).contiguous()
+    case.seg[0] = torch.tensor([0, 50, 0, total - 50], dtype=torch.int32)
+    case.pol.copy_(torch.tensor(pol, dtype=torch.int32))
+    case.run()
+    assert M.murmur_device_error() == (0 if good else M.MURMUR_DEVERR_POLICY)
+    assert bool(torch.isfinite(case.out).all()) == good and bool(torch.isnan(case.out).all()) != good
+    if good:  # as many blocks fewer: the same rows, since the window is all that is kept of the outputs
+        case.seg_np, case.table_np = case.seg.cpu().numpy() - [0, 0, 0, 32766 * block], case.table.cpu().numpy()
+        case.check(12)
